@@ -387,6 +387,87 @@ int blink_sample_top_p(const float* logits, int rows, int vocab, const int32_t* 
 int blink_sample_noalloc(const float* logits, int rows, int vocab, const int32_t* top_k, const float* temperature,
                          const uint64_t* ticket, const int32_t* gen_index, const uint64_t* seed, int32_t* out);
 
+/* ---- the operators of a speculative step, alone -----------------------------------------------------------------
+ * What a program runs that takes its own steps beside the loop, over a pool of the loop's layout: request lengths become block
+ * tables and a slot map (blink_build_tables), projected queries and keys are normed, rotated and cached
+ * (blink_qk_norm_rope), the new rows attend over the cache (blink_window_attention), and drafted tokens are held against the
+ * target's logits (blink_verify_drafts).  The paper names speculative decoding among the extensions of its loop
+ * (Section 7); a layer with a sliding window, or with norms of queries and keys, is what the loop's own attention does not have.
+ *
+ * All of them: arrays are DEVICE memory of the current device, `stream` is a cudaStream_t of it (NULL: the default stream).  A call
+ * checks what the host can see, enqueues its kernels and returns; it does not wait, allocates nothing, keeps nothing
+ * and can be captured.  Lengths and tables are read by the kernels, so that a captured call serves the lengths of the moment.  A
+ * workspace holds nothing between calls; one that two calls use must not be used by both at once.  `rows` counts the rows of the
+ * arrays; those from row_start[n_requests] on belong to nobody and are left as they were.  Limit: 4096 requests a call
+ * (BLINK_ETOOBIG). */
+
+/* Block tables and slot map of a step.  Request r has ctx_len[r] tokens in the cache and new_len[r] >= 0 rows in the step;
+ * the first blocks_held[r] entries of its row block_table[r * table_stride ..] are its blocks.  It is given
+ * max(0, ceil((ctx_len + new_len) / 16) - blocks_held) more, in ascending r, each the topmost of the stack free_blocks
+ * [*free_count entries, free_capacity at most]: free_blocks[*free_count - 1] first, as the loop pops its own.
+ *   row_start [n_requests + 1]  first row of each request, and the number of rows
+ *   kv_len [n_requests]         ctx_len + new_len
+ *   positions, slot_map [max_rows]  of row i of request r: ctx_len[r] + i, and block * 16 + position % 16 (-1 where the table's entry
+ *                               is no block); -1 in all rows behind the last one
+ *   blocks_held_out [n_requests], free_count_out [1]  may be the memory of blocks_held and free_count
+ *   status [1]                  BLINK_OK, or why nothing was handed out: BLINK_EINVAL (a negative length or count, a count
+ *                               above free_capacity), BLINK_ETOOBIG (more rows than max_rows, or blocks than table_stride),
+ *                               BLINK_ENOMEM (not enough free blocks).  Then row_start and kv_len are 0, all rows -1, and
+ *                               tables, held blocks and the count as they were.
+ * Blocks of drafts that were refused stay held and serve the next step. */
+int blink_build_tables(const int32_t* ctx_len, const int32_t* new_len, const int32_t* blocks_held, int n_requests,
+                       const int32_t* free_blocks, int free_capacity, const int32_t* free_count, int32_t* block_table,
+                       int table_stride, int max_rows, int32_t* blocks_held_out, int32_t* free_count_out, int32_t* row_start,
+                       int32_t* kv_len, int32_t* positions, int32_t* slot_map, int32_t* status, void* stream);
+
+/* Norms of queries and keys for each head, the rotation of the row's position, and the new keys and values into layer
+ * `layer` of the pool, in one pass.  qkv: [rows][(Hq + 2 Hkv) * hd] (q, k, v heads), qkv_stride elements between rows, of
+ * qkv_dtype: the model's, or fp32 beside a bf16 model.  Heads of q and k become x / sqrt(mean(x^2) + rms_eps) * gain (fp32
+ * [hd]; NULL: not normed), then pairs (i, i + hd/2) are turned by position * rope_theta^(-2i/hd) (angles in 64 bits).  q
+ * goes to q_out [rows][Hq * hd] (model dtype, q_stride), which may be qkv itself (same dtype and stride) but not overlap it
+ * otherwise; k and v to the row's slot.  A row whose slot is not one of the pool's is not cached; a row with a negative
+ * position is left alone.  Two rows of one slot: either of them.  Pointers 16-byte aligned, strides multiples of 8. */
+int blink_qk_norm_rope(const blink_model_cfg* model, const blink_kv_pool* kv, int layer, const void* qkv, int qkv_dtype,
+                       int64_t qkv_stride, const float* q_gain, const float* k_gain, const int32_t* positions,
+                       const int32_t* slot_map, int rows, void* q_out, int64_t q_stride, void* stream);
+
+/* Bytes of workspace that blink_window_attention needs for a model and requests of up to max_new rows (0: bad argument). */
+uint64_t blink_window_attention_workspace(const blink_model_cfg* model, int max_new);
+
+/* Attention of the step's rows over layer `layer` of the pool, whose keys and values hold those rows already.  Row i of request r is at
+ * position p = kv_len[r] - (row_start[r + 1] - row_start[r]) + i and sees key j <= p when j > p - window, or j < sinks
+ * (window 0: every j <= p); scores are scaled by 1/sqrt(hd), query head h reads kv head h / (Hq / Hkv).  A row that
+ * sees nothing (a negative position) becomes zeros.  q, out: [rows][Hq * hd] of the model dtype, q_stride and out_stride elements
+ * between rows; out may be q (same stride).  Blocks that no row of the request sees are not read: their table entries may be
+ * anything.  An entry that is seen but is no block of the pool is read as zeros.  What stands in the cache where no row of
+ * the request sees it (the rest of the last block, keys before the window) does not matter; an infinity or NaN that one of
+ * its rows sees may reach all of its rows.  max_new: rows of the longest request, for the choice of kernels; longer ones are
+ * served too.  Pointers 16-byte (workspace 256-byte) aligned, strides multiples of 8. */
+int blink_window_attention(const blink_model_cfg* model, const blink_kv_pool* kv, int layer, const void* q, int64_t q_stride, int rows,
+                           const int32_t* row_start, const int32_t* kv_len, int n_requests, const int32_t* block_table, int table_stride,
+                           int window, int sinks, int max_new, void* out, int64_t out_stride, void* workspace, uint64_t workspace_bytes,
+                           void* stream);
+
+/* Bytes of workspace that blink_verify_drafts needs (0: bad argument). */
+uint64_t blink_verify_workspace(int rows, int vocab);
+
+/* Verification of drafted tokens.  Request r has the logits rows row_start[r] .. row_start[r + 1] - 1: one for each of its k drafted
+ * tokens draft_tokens[row], and one more.  With p = softmax(logits / temperature[r]) of row i and q = draft_probs of row i (NULL: all of
+ * it on the drafted token), draft x is accepted while u_accept[row] * q(x) < p(x).  At the first refusal a token is drawn from
+ * max(0, p - q) (from p where that is empty; entries of q that are no number or negative count as 0), behind k accepted drafts from p of the
+ * last row: the lowest index at which the running sum exceeds u_pick[r] times the sum (none: the last with any weight).  temperature not
+ * above 0, or not finite: greedy, a draft is accepted when it is the row's largest (the first of equals), which is also the token drawn; a row
+ * whose largest entry is infinite, or that holds no number, is taken so too (token 0 in the latter).  A logit of NaN counts as -inf; a
+ * token outside the vocabulary is refused.
+ *   out_tokens [rows]          the accepted drafts, the token drawn, then -1
+ *   n_accepted [n_requests]    0 .. k (a request without rows: 0)
+ * Acceptance compares in 64 bits (the sum of exponentials to about 1e-8), the draw is in 64 bits throughout.  fp32 [rows][vocab] logits
+ * and probabilities with their strides; draft_probs is not read in a request's last row. */
+int blink_verify_drafts(const float* logits, int64_t logits_stride, int rows, int vocab, const int32_t* row_start, int n_requests,
+                        const int32_t* draft_tokens, const float* draft_probs, int64_t probs_stride, const float* temperature,
+                        const float* u_accept, const float* u_pick, int32_t* out_tokens, int32_t* n_accepted, void* workspace,
+                        uint64_t workspace_bytes, void* stream);
+
 const char* blink_strerror(int code);
 
 #ifdef __cplusplus

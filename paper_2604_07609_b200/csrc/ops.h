@@ -1,0 +1,84 @@
+// What the operators that can be called alone (ops_*.cu) share on the host: checks of their arguments and launches.
+#pragma once
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/blink.h"
+
+namespace blink {
+
+constexpr int OPS_BLOCK = 16;            // tokens of a KV block
+constexpr int OPS_MAX_REQUESTS = 4096;   // their prefix sums are kept in shared memory
+
+// One layer of a paged KV pool, [2][n_blocks][Hkv][16][hd] each, as the kernels address it.
+struct OpsPool {
+  char* k;           // block 0 of the layer's keys
+  char* v;
+  int64_t n_blocks;
+  int Hq, Hkv, rep, hd, dtype;
+};
+
+inline bool ops_aligned(const void* p, uintptr_t to) { return p != nullptr && ((uintptr_t)p & (to - 1)) == 0; }
+
+inline int ops_pool(const blink_model_cfg* m, const blink_kv_pool* kv, int layer, OpsPool* out) {
+  if (!m || !kv || kv->size != sizeof(blink_kv_pool) || kv->block_size != OPS_BLOCK) return BLINK_EINVAL;
+  const int64_t nb = blink_kv_blocks_for_bytes(m, OPS_BLOCK, kv->bytes);   // (refuses a bad model)
+  if (nb < 0) return BLINK_EINVAL;
+  if (nb == 0) return BLINK_ENOMEM;
+  if (layer < 0 || layer >= m->n_layers || !ops_aligned(kv->base, 256)) return BLINK_EINVAL;
+  // slots and rows of 64 elements are counted in 32 bits
+  if (nb * OPS_BLOCK * m->n_kv_heads > 0x7fffffffll) return BLINK_ETOOBIG;
+  const int64_t esz = m->dtype == BLINK_DTYPE_BF16 ? 2 : 4;
+  const int64_t plane = nb * m->n_kv_heads * OPS_BLOCK * m->head_dim * esz;
+  out->k = static_cast<char*>(kv->base) + 2 * layer * plane;
+  out->v = out->k + plane;
+  out->n_blocks = nb;
+  out->Hq = m->n_q_heads;
+  out->Hkv = m->n_kv_heads;
+  out->rep = m->n_q_heads / m->n_kv_heads;
+  out->hd = m->head_dim;
+  out->dtype = m->dtype;
+  return BLINK_OK;
+}
+
+// An error that a launch left behind is taken away, so that no later call reports it as its own.
+inline int ops_launched(cudaError_t e) {
+  if (e == cudaSuccess) e = cudaGetLastError();
+  else (void)cudaGetLastError();
+  return e == cudaSuccess ? BLINK_OK : BLINK_ECUDA;
+}
+
+// cluster > 0: CTAs of a cluster.  after: the kernel may be set up while the one before it in the stream still runs; it waits for that
+// kernel's results itself (griddepcontrol.wait).
+template <typename... P, typename... A>
+inline int ops_launch(void (*kernel)(P...), int64_t grid, int threads, size_t smem, void* stream, int cluster, bool after, A... args) {
+  if (grid < 1) return BLINK_OK;
+  if (grid > 0x7fffffffll) return BLINK_ETOOBIG;
+  if (smem > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return ops_launched(e);
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = static_cast<cudaStream_t>(stream);
+  cudaLaunchAttribute at[2];
+  int n = 0;
+  if (cluster > 0) {
+    at[n].id = cudaLaunchAttributeClusterDimension;
+    at[n].val.clusterDim.x = (unsigned)cluster;
+    at[n].val.clusterDim.y = at[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  if (after) {
+    at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[n].val.programmaticStreamSerializationAllowed = 1;
+    ++n;
+  }
+  cfg.attrs = at;
+  cfg.numAttrs = (unsigned)n;
+  return ops_launched(cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...));
+}
+
+}  // namespace blink

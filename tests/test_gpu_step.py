@@ -1,0 +1,501 @@
+"""The operators of a speculative step against their oracle in 64 bits, through the binding."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import step as O
+from paper_2604_07609_b200 import binding as B
+from synth import model_cfg
+
+pytestmark = pytest.mark.gpu
+
+BS = 16
+DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
+HALF = {"bf16": 2.0 ** -8, "fp32": 2.0 ** -24}     # half a step, relative to the value
+U = 2.0 ** -24
+
+
+def ints(a):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+def shape(rep=4, hkv=2, hd=128, dtype="bf16", layers=2):
+    return model_cfg(1, n_layers=layers, n_q_heads=rep * hkv, n_kv_heads=hkv, head_dim=hd, dtype=dtype)
+
+
+def new_pool(m, blocks, fill=float("nan")):
+    return torch.full((m.n_layers, 2, blocks, m.n_kv_heads, BS, m.head_dim), fill, dtype=DT[m.dtype], device="cuda")
+
+
+# ---- tables -----------------------------------------------------------------------------------------------------------
+def tables_case(rng, n, ctx_hi, new_hi, spare, zero=0.2):
+    ctx, new = rng.integers(0, ctx_hi + 1, n), rng.integers(0, new_hi + 1, n)
+    new[rng.random(n) < zero] = 0
+    held = np.array([-(-c // BS) + int(rng.integers(0, 3)) for c in ctx])
+    stride = int(max(max(held), (-(-(ctx + new) // BS)).max())) + int(rng.integers(0, 3))
+    ids = rng.permutation(int(held.sum()) + int((ctx + new).sum()) // BS + n + 5)
+    table, at = np.full((n, max(stride, 1)), -1), 0
+    for r in range(n):
+        table[r, :held[r]] = ids[at:at + held[r]]
+        at += held[r]
+    return ctx, new, held, ids[at:], len(ids) - at, table, int(new.sum()) + spare
+
+
+def check_tables(ctx, new, held, free, count, table, rows, out=None, cap=None):
+    want = O.build_tables(list(map(int, ctx)), list(map(int, new)), list(map(int, held)), free, count, table, rows)
+    dev = ints(table)
+    t = B.blink_build_tables(ints(ctx), ints(new), ints(held), ints(free), ints([count]), dev, max_rows=rows) if out is None else out(dev)
+    got = [x.cpu().numpy() for x in t]
+    for name, w, g in zip(("row_start", "kv_len", "positions", "slots", "held", "count", "status"), want, got):
+        assert np.array_equal(np.atleast_1d(w), g), name
+    assert np.array_equal(dev.cpu().numpy(), want[7])
+
+
+@pytest.mark.parametrize("n,ctx,new,spare", [(1, 0, 1, 0), (1, 40, 1, 3), (3, 20, 40, 5), (31, 100, 3, 0), (256, 300, 8, 77), (257, 60, 33, 1),
+                                             (1025, 50, 2, 0), (4096, 30, 3, 9), (40, 2000, 700, 100)])
+def test_tables(n, ctx, new, spare):
+    case = list(tables_case(np.random.default_rng(n), n, ctx, new, spare))
+    case[6] = max(1, case[6])
+    check_tables(*case)
+
+
+def test_tables_hand_out_nothing_when_refused():
+    rng = np.random.default_rng(5)
+    ctx, new, held, free, count, table, rows = tables_case(rng, 40, 50, 40, 3, zero=0)
+    need = int(np.maximum(0, -(-(ctx + new) // BS) - held).sum())
+    check_tables(ctx, new, held, free, need, table, rows)            # exactly enough
+    check_tables(ctx, new, held, free, need - 1, table, rows)
+    check_tables(ctx, new, held, free, len(free) + 1, table, rows)
+    check_tables(ctx, new, held, free, -1, table, rows)
+    check_tables(ctx, new, held, free, count, table, int(new.sum()) - 1)
+    check_tables(ctx, new, held, free, count, table[:, :-(-int((ctx + new).max()) // BS) - 1], rows) if (held < table.shape[1] - 1).all() else None
+    for a in (ctx, new, held):
+        b = a.copy()
+        b[17] = -1
+        args = [b if x is a else x for x in (ctx, new, held)]
+        check_tables(*args, free, count, table, rows)
+
+
+def test_tables_in_place_and_entries_that_are_no_block():
+    rng = np.random.default_rng(6)
+    ctx, new, held, free, count, table, rows = tables_case(rng, 300, 90, 20, 40)
+    table[5, 0], table[9, 0] = -1, 1 << 28
+    ctx[5] = ctx[9] = 0
+    held[5] = held[9] = 1
+
+    def run(dev):
+        h, c = ints(held), ints([count])
+        out = B.make_step_tables(len(ctx), rows, "cuda")._replace(blocks_held=h, free_count=c)
+        return B.blink_build_tables(ints(ctx), ints(new), h, ints(free), c, dev, out=out)
+    check_tables(ctx, new, held, free, count, table, rows, run)
+
+
+# ---- norms, rotation, cache -------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("rows", [1, 3, 64, 300])
+@pytest.mark.parametrize("rep,hkv,hd,dtype,qkv", [(4, 2, 128, "bf16", "bf16"), (1, 3, 64, "bf16", "bf16"), (8, 1, 128, "bf16", "fp32"), (2, 2, 64, "fp32", "fp32"),
+                                                  (4, 8, 64, "bf16", "fp32"), (1, 1, 128, "fp32", "fp32")])
+@pytest.mark.parametrize("gains", ["both", "q", None])
+def test_norm_rope(rows, rep, hkv, hd, dtype, qkv, gains):
+    m = shape(rep, hkv, hd, dtype, layers=3).with_(rope_theta=5e5)
+    rng = np.random.default_rng(rows * 7 + hd)
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x = torch.randn(rows, m.qkv_dim + 8, device="cuda", generator=g).mul_(2).to(DT[qkv])[:, :m.qkv_dim]     # rows further apart
+    qg = 1 + 0.3 * torch.randn(hd, device="cuda", generator=g) if gains else None
+    kg = 1 + 0.3 * torch.randn(hd, device="cuda", generator=g) if gains == "both" else None
+    pos = rng.integers(0, 1 << 30, rows) if rows == 64 else rng.integers(0, 6000, rows)
+    blocks = rows // BS + 4
+    slots = rng.permutation(blocks * BS)[:rows]
+    pool = new_pool(m, blocks, 3.0)
+    out = torch.full((rows, m.q_dim + 16), 5.0, dtype=DT[dtype], device="cuda")
+    if rows > 2:
+        pos[1] = -1                              # left alone
+        slots[2] = -1 if rows < 100 else blocks * BS
+    B.blink_qk_norm_rope(m, pool, 1, x, qg, kg, ints(pos), ints(slots), out=out[:, :m.q_dim])
+    xs = f64(x).reshape(rows, m.n_q_heads + 2 * hkv, hd)
+    Hq = m.n_q_heads
+    # sums of hd squares in runs of 16 and a tree (20 roundings, halved by the root), rsqrtf 2 ulp, three products, angles to 2 ulp of
+    # one and two products and a sum of the rotation: 24 roundings of the terms' size at most
+    for heads, gain, got in ((slice(0, Hq), qg, f64(out[:, :m.q_dim]).reshape(rows, Hq, hd)),
+                             (slice(Hq, Hq + hkv), kg, None), (slice(Hq + hkv, None), "v", None)):
+        y, size = (xs[:, heads], 0 * xs[:, heads]) if isinstance(gain, str) else O.norm_rope(xs[:, heads], None if gain is None else f64(gain), np.maximum(pos, 0), 5e5, m.rms_eps)
+        tol = HALF[dtype] * abs(y) + 24 * U * size
+        if got is not None:
+            live = pos >= 0
+            assert (abs(got - y)[live] <= tol[live]).all()
+            assert (got[~live] == 5.0).all()
+        else:
+            kv = f64(pool[1, 1 if isinstance(gain, str) else 0]).transpose(0, 2, 1, 3).reshape(blocks * BS, hkv, hd)
+            live = (pos >= 0) & (slots >= 0) & (slots < blocks * BS)
+            assert (abs(kv[slots[live]] - y[live]) <= tol[live]).all()
+            kv[slots[live]] = 3.0
+            assert (kv == 3.0).all()             # nothing else was written
+    assert (out[:, m.q_dim:] == 5.0).all() and (pool[0] == 3.0).all() and (pool[2] == 3.0).all()
+
+
+def test_norm_rope_in_place_and_special_rows():
+    m = shape(2, 2, 64)
+    x = torch.randn(40, m.qkv_dim, device="cuda").bfloat16()
+    x[3] = 0                                     # a head of zeros stays one: eps
+    x[5, 70] = float("inf")
+    pos, slots = ints(np.arange(40)), ints(np.arange(40))
+    want = B.blink_qk_norm_rope(m, new_pool(m, 3, 0.0), 0, x.clone(), torch.ones(64, device="cuda"), torch.ones(64, device="cuda"), pos, slots)
+    assert (want[3] == 0).all() and torch.isnan(want[5, 64:128]).any() and not torch.isnan(want[5, :64]).any()
+    y = x.clone()
+    B.blink_qk_norm_rope(m, new_pool(m, 3, 0.0), 0, y, torch.ones(64, device="cuda"), torch.ones(64, device="cuda"), pos, slots, out=y[:, :m.q_dim])
+    assert torch.equal(y[:, :m.q_dim].nan_to_num(7.0), want.nan_to_num(7.0)) and torch.equal(y[:, m.q_dim:], x[:, m.q_dim:])
+
+
+# ---- attention --------------------------------------------------------------------------------------------------------
+def attention_case(m, ctx, new, window, sinks, seed=0, pad=0, layer=1, q_pad=0, scale=1.0):
+    """Inputs of requests with ctx cached tokens and new rows; everything that no row of its request sees is NaN, and blocks that hold
+    nothing else have no entry in the table."""
+    rng = np.random.default_rng(seed)
+    ctx, new = np.asarray(ctx), np.asarray(new)
+    n, hd, hkv = len(ctx), m.head_dim, m.n_kv_heads
+    start = np.concatenate([[0], np.cumsum(new)])
+    rows = int(start[-1]) + pad
+    seen = [sorted(set().union(*[O.visible(c + i, window, sinks) for i in range(k)]) if k else []) for c, k in zip(ctx, new)]
+    used = [sorted({j // BS for j in s}) for s in seen]
+    total = sum(map(len, used)) + 3
+    ids = rng.permutation(total)
+    table = np.where(rng.random((n, int(max(1, (-(-(ctx + new) // BS)).max())) + 1)) < 0.5, -1, 1 << 30)
+    pool = new_pool(m, total)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    at, kv = 0, []
+    for r in range(n):
+        table[r, used[r]] = ids[at:at + len(used[r])]
+        at += len(used[r])
+        k, v = (torch.randn(len(seen[r]), hkv, hd, device="cuda", generator=g).to(pool.dtype) for _ in (0, 1))
+        if seen[r]:
+            j = np.array(seen[r])
+            block = torch.from_numpy(table[r, j // BS]).cuda()
+            pool[layer, 0][block, :, torch.from_numpy(j % BS).cuda()] = k
+            pool[layer, 1][block, :, torch.from_numpy(j % BS).cuda()] = v
+        full = np.full((2, int(ctx[r] + new[r]), hkv, hd), np.nan)
+        if seen[r]:
+            full[0, j], full[1, j] = f64(k), f64(v)
+        kv.append(full)
+    q = (scale * torch.randn(max(1, rows), m.q_dim + q_pad, device="cuda", generator=g)).to(pool.dtype)[:, :m.q_dim]
+    return dict(m=m, pool=pool, layer=layer, q=q, row_start=ints(start), kv_len=ints(ctx + new), table=ints(table), window=window, sinks=sinks, start=start, ctx=ctx, kv=kv)
+
+
+def run_attention(c, max_new=None, **kw):
+    longest = max(1, int(np.diff(c["start"]).max()))
+    return B.blink_window_attention(c["m"], c["pool"], c["layer"], c["q"], c["row_start"], c["kv_len"], c["table"], c["window"], c["sinks"],
+                                    longest if max_new is None else max_new, **kw)
+
+
+def check_attention(c, out, only=None):
+    """Bound of the error: half a step of the output; in bf16 half a step of each probability in its product with the values (their sum
+    is taken before that rounding); scores to (hd + 8) roundings of their products' sum, which enter a probability as they are; 2^-20
+    for the exponentials, and a rounding per key of the running sums."""
+    m, start = c["m"], c["start"]
+    q, got = f64(c["q"]), f64(out)
+    for r in range(len(c["ctx"])) if only is None else only:
+        a, b = start[r], start[r + 1]
+        if a == b:
+            continue
+        keys, values = c["kv"][r]
+        want, size, spread = O.window_attention(q[a:b].reshape(b - a, m.n_q_heads, m.head_dim), keys, values, c["ctx"][r], c["window"], c["sinks"])
+        p = 2.0 ** -8 if m.dtype == "bf16" else 0.0
+        tol = HALF[m.dtype] * abs(want) + size * (p * 1.01 + 2 * (m.head_dim + 8) * U * spread[..., None] + 2.0 ** -20 + len(keys) * U)
+        err = abs(got[a:b].reshape(want.shape) - want)
+        assert (err <= tol).all(), f"request {r}: {np.nanmax(err / np.maximum(tol, 1e-30)):.2f} of the bound, {np.isnan(err).sum()} NaN"
+
+
+SHAPES = [(4, 2, 128, "bf16"), (1, 2, 128, "bf16"), (8, 1, 64, "bf16"), (2, 3, 64, "bf16"), (4, 1, 64, "fp32"), (8, 1, 128, "fp32"), (1, 2, 128, "fp32")]
+
+
+@pytest.mark.parametrize("rep,hkv,hd,dtype", SHAPES)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (16, 4), (17, 1), (50, 20), (1000, 4), (33, 64)])
+def test_attention_single_rows(rep, hkv, hd, dtype, window, sinks):
+    c = attention_case(shape(rep, hkv, hd, dtype), [0, 1, 14, 15, 16, 31, 47, 63, 200, 333], [1] * 10, window, sinks, seed=window)
+    check_attention(c, run_attention(c))
+
+
+@pytest.mark.parametrize("rep,hkv,hd,dtype", SHAPES)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 2), (20, 4), (64, 0), (150, 33)])
+def test_attention_drafts(rep, hkv, hd, dtype, window, sinks):
+    c = attention_case(shape(rep, hkv, hd, dtype), [0, 15, 100, 7, 260, 64, 30], [3, 4, 1, 0, 2, 5, 8], window, sinks, seed=window, pad=2, q_pad=8)
+    out = torch.full((c["q"].shape[0], c["m"].q_dim + 8), 9.0, dtype=c["q"].dtype, device="cuda")
+    run_attention(c, out=out[:, :c["m"].q_dim])
+    check_attention(c, out[:, :c["m"].q_dim])
+    assert (out[-2:] == 9.0).all() and (out[:, c["m"].q_dim:] == 9.0).all()
+
+
+@pytest.mark.parametrize("rep,hkv,hd,dtype", SHAPES)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (64, 4), (130, 0), (1, 1), (0, 7)])
+def test_attention_prompts(rep, hkv, hd, dtype, window, sinks):
+    c = attention_case(shape(rep, hkv, hd, dtype), [0, 33, 0, 5, 200], [65, 40, 129, 1, 100], window, sinks, seed=window, pad=3)
+    out = torch.full((c["q"].shape[0], c["m"].q_dim), 9.0, dtype=c["q"].dtype, device="cuda")
+    run_attention(c, out=out)
+    check_attention(c, out)
+    assert (out[-3:] == 9.0).all()
+
+
+@pytest.mark.parametrize("rep,hkv,hd,dtype", [(4, 1, 128, "bf16"), (8, 2, 64, "bf16"), (4, 1, 64, "fp32"), (1, 1, 128, "fp32")])
+def test_attention_a_long_context_is_shared_out_and_joined(rep, hkv, hd, dtype):
+    for window, sinks in ((0, 0), (4000, 5)):
+        c = attention_case(shape(rep, hkv, hd, dtype), [6001, 3, 2500], [1, 1, 2], window, sinks, seed=3)
+        check_attention(c, run_attention(c))
+
+
+def test_attention_rows_that_see_nothing_are_zeros():
+    """More rows than cached tokens: positions below zero."""
+    for dtype in ("bf16", "fp32"):
+        for new in (3, 40):
+            c = attention_case(shape(4, 2, 64, dtype), [0, 20], [new, 2], 8, 2, seed=1)
+            kv_len = c["kv_len"].clone()
+            kv_len[0] = 1                                      # the last of its rows alone is at position 0
+            out = B.blink_window_attention(c["m"], c["pool"], 1, c["q"], c["row_start"], kv_len, c["table"], 8, 2, new)
+            assert (out[:new - 1] == 0).all()
+            check_attention(c, out, only=[1])
+            kv_len[0] = 0
+            assert (B.blink_window_attention(c["m"], c["pool"], 1, c["q"], c["row_start"], kv_len, c["table"], 8, 2, new)[:new] == 0).all()
+
+
+def test_attention_blocks_that_are_none_are_zeros():
+    """A seen entry that is no block of the pool: keys and values of zeros, wherever the rows go."""
+    for new in (1, 3, 70):
+        c = attention_case(shape(4, 2, 128), [100, 50], [new, 1], 0, 0, seed=2)
+        for bad in (-1, c["pool"].shape[2], 1 << 30, -(1 << 31)):
+            table = c["table"].clone()
+            table[0, 2] = bad
+            out = B.blink_window_attention(c["m"], c["pool"], 1, c["q"], c["row_start"], c["kv_len"], table, 0, 0, new)
+            d = dict(c, kv=[c["kv"][0].copy(), c["kv"][1]])
+            d["kv"][0][:, 32:48] = 0
+            check_attention(d, out)
+
+
+def test_attention_large_scores_and_out_over_q():
+    c = attention_case(shape(4, 2, 128), [700, 20, 3], [1, 4, 60], 0, 0, seed=4, scale=12.0)
+    out = run_attention(c)
+    check_attention(c, out)
+    q = c["q"].contiguous().clone()
+    assert B.blink_window_attention(c["m"], c["pool"], 1, q, c["row_start"], c["kv_len"], c["table"], 0, 0, 60, out=q) is q
+    assert torch.equal(q, out)
+
+
+def test_attention_max_new_is_a_hint():
+    c = attention_case(shape(4, 2, 128), [90, 20, 300], [1, 90, 6], 64, 4, seed=5)
+    for hint in (1, 2, 5, 90, 10000):
+        check_attention(c, run_attention(c, max_new=hint))
+
+
+def test_attention_many_requests():
+    rng = np.random.default_rng(8)
+    c = attention_case(shape(4, 1, 64), rng.integers(0, 60, 4096), (rng.random(4096) < 0.7).astype(int), 24, 2, seed=6)
+    out = run_attention(c)
+    check_attention(c, out, only=[0, 1, 2, 100, 2000, 4000, 4094, 4095])
+    some = rng.permutation(4096)[:200]
+    check_attention(c, out, only=some)
+
+
+# ---- verification -----------------------------------------------------------------------------------------------------
+def verify_case(rng, k, V, probs, temps, spread=2.0, stride=0):
+    n, rows = len(k), int(np.sum(k)) + len(k)
+    z = (spread * rng.normal(size=(rows, V + stride))).astype(np.float32)
+    T = np.asarray(temps, np.float32)
+    start = np.concatenate([[0], np.cumsum(np.asarray(k) + 1)])
+    q = np.stack([O.target_probs(z[i, :V] + 0.5 * rng.normal(size=V), 1.0 if T[r] == 0 else T[r])[0] for r in range(n) for i in range(start[r], start[r + 1])])
+    draft = np.array([rng.choice(V, p=x / x.sum()) for x in q])
+    for r in range(n):
+        if T[r] == 0:
+            for i in range(start[r], start[r + 1]):
+                if rng.random() < 0.8:
+                    draft[i] = int(z[i, :V].argmax())
+    return dict(z=z, V=V, start=start, draft=draft, q=q.astype(np.float32) if probs else None, T=T, ua=rng.random(rows).astype(np.float32),
+                up=rng.random(n).astype(np.float32))
+
+
+def run_verify(c, **kw):
+    z = torch.from_numpy(c["z"]).cuda()[:, :c["V"]]
+    f = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).cuda()
+    return B.blink_verify_drafts(z, ints(c["start"]), ints(c["draft"]), f(c["q"]) if c["q"] is not None else None, f(c["T"]), f(c["ua"]), f(c["up"]), **kw)
+
+
+def check_verify(c, tokens, accepted):
+    tokens, accepted = tokens.cpu().numpy(), accepted.cpu().numpy()
+    for r in range(len(c["T"])):
+        a, b = c["start"][r], c["start"][r + 1]
+        if a == b:
+            assert accepted[r] == 0
+            continue
+        want, n, near = O.verify_request(c["z"][a:b, :c["V"]], c["draft"][a:b - 1], None if c["q"] is None else c["q"][a:b], c["T"][r], c["ua"][a:b], c["up"][r])
+        # a decision within 1e-7 (acceptance: the sum of 32-bit exponentials; the draw itself is good to 1e-13) is anybody's
+        if near > 1e-7:
+            assert accepted[r] == n and np.array_equal(tokens[a:b], want), (r, n, accepted[r], want, tokens[a:b], near)
+
+
+@pytest.mark.parametrize("V", [2, 31, 257, 1000, 4096, 4097, 32000])
+@pytest.mark.parametrize("probs", [True, False])
+def test_verify(V, probs):
+    rng = np.random.default_rng(V)
+    k = [0, 1, 4, 7, 2, 0, 3, 5]
+    c = verify_case(rng, k, V, probs, [1.0, 0.7, 0.0, 0.9, 1.3, 0.0, 0.05, 2.0], stride=V % 3)
+    check_verify(c, *run_verify(c))
+
+
+def test_verify_the_largest_vocabulary_of_the_configurations_and_one_beyond_shared_memory():
+    rng = np.random.default_rng(1)
+    for V in (128256, 210001):
+        c = verify_case(rng, [3, 0, 6], V, True, [0.8, 1.0, 0.9], spread=1.5)
+        check_verify(c, *run_verify(c))
+
+
+def test_verify_many_draws_of_flat_rows():
+    """Rows whose neighbours are as close as they come: the draw has to find the right one of some thousand."""
+    rng = np.random.default_rng(2)
+    c = verify_case(rng, [1] * 150, 5000, True, [1.0] * 150, spread=0.05)
+    check_verify(c, *run_verify(c))
+
+
+def test_verify_special_entries():
+    rng = np.random.default_rng(3)
+    V, n = 300, 12
+    c = verify_case(rng, [2] * n, V, True, [0.9] * n)
+    z, q, s = c["z"], c["q"], c["start"]
+    z[s[0], :] = -np.inf                     # no number: greedy, token 0
+    z[s[1], 50:] = np.nan                    # counts as -inf
+    z[s[2], 7] = z[s[2], 9] = np.inf         # greedy, the first of them
+    c["draft"][s[2]] = 7
+    c["draft"][s[3]] = -1                    # outside the vocabulary
+    c["draft"][s[4]] = V
+    q[s[5]] = 2.0                            # q covers p: from p itself
+    c["ua"][s[5]] = 0.99
+    q[s[6], :100] = np.nan
+    q[s[6], 100:200] = -1.0
+    c["ua"][s[6]] = 1e9
+    c["up"][7] = 1.5                         # past the end: the last with any weight
+    c["up"][8], c["up"][9], c["up"][10] = 0.0, np.nan, -3.0
+    c["T"][11] = np.inf
+    c["ua"][s[9]] = np.nan
+    z[s[10]:s[11], 100:] = -np.inf           # most of the row without weight
+    check_verify(c, *run_verify(c))
+
+
+def test_verify_rows_behind_the_last_request_and_requests_without_rows():
+    rng = np.random.default_rng(4)
+    c = verify_case(rng, [2, 3, 1, 2], 500, True, [1.0, 0.8, 0.7, 0.9])
+    c["start"] = np.array([0, 3, 3, 7, 9])           # the second has none; two rows behind the last
+    tokens = torch.full((c["z"].shape[0],), 77, dtype=torch.int32, device="cuda")
+    out = run_verify(c, out_tokens=tokens)
+    assert out[0] is tokens and (tokens[9:] == 77).all()
+    check_verify(c, *out)
+
+
+# ---- together, streams, graphs ----------------------------------------------------------------------------------------
+def spec_step(m, st, stream_safe=True):
+    """One step of all of them, as a program takes it; everything in st is on the device."""
+    t = B.blink_build_tables(st["ctx"], st["new"], st["tables"].blocks_held, st["free"], st["tables"].free_count, st["table"], out=st["tables"])
+    B.blink_qk_norm_rope(m, st["pool"], 0, st["qkv"], st["qg"], st["kg"], t.positions, t.slot_map, out=st["q"])
+    B.blink_window_attention(m, st["pool"], 0, st["q"], t.row_start, t.kv_len, st["table"], st["window"], st["sinks"], st["max_new"], out=st["o"], workspace=st["ws"])
+    st["logits"] = torch.matmul(st["o"].float(), st["head"], out=st["logits"])
+    B.blink_verify_drafts(st["logits"], t.row_start, st["draft"], None, st["T"], st["ua"], st["up"], out_tokens=st["tok"], n_accepted=st["acc"], workspace=st["ws2"])
+
+
+def spec_state(m, n, max_new, V=500, blocks=200, window=40, sinks=2, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rows = n * max_new
+    r = lambda *s: torch.randn(*s, device="cuda", generator=g)
+    dt = DT[m.dtype]
+    return dict(ctx=torch.zeros(n, dtype=torch.int32, device="cuda"), new=torch.full((n,), max_new, dtype=torch.int32, device="cuda"),
+                tables=B.make_step_tables(n, rows, "cuda")._replace(free_count=ints([blocks])), free=ints(np.random.default_rng(seed).permutation(blocks)),
+                table=torch.full((n, 24), -1, dtype=torch.int32, device="cuda"), pool=new_pool(m, blocks), qkv=r(rows, m.qkv_dim).to(dt),
+                qg=1 + 0.1 * r(m.head_dim), kg=1 + 0.1 * r(m.head_dim), q=torch.zeros(rows, m.q_dim, dtype=dt, device="cuda"),
+                o=torch.zeros(rows, m.q_dim, dtype=dt, device="cuda"), head=r(m.q_dim, V), logits=torch.zeros(rows, V, device="cuda"),
+                draft=torch.zeros(rows, dtype=torch.int32, device="cuda"), T=torch.zeros(n, device="cuda"), ua=torch.rand(rows, device="cuda", generator=g),
+                up=torch.rand(n, device="cuda", generator=g), tok=torch.zeros(rows, dtype=torch.int32, device="cuda"),
+                acc=torch.zeros(n, dtype=torch.int32, device="cuda"), max_new=max_new, window=window, sinks=sinks, V=V,
+                ws=torch.empty(B.blink_window_attention_workspace(m, max_new), dtype=torch.uint8, device="cuda"),
+                ws2=torch.empty(B.blink_verify_workspace(rows, V), dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_a_run_of_steps_is_the_same_captured_and_eager_and_follows_the_oracle(dtype):
+    """Prompts, then drafts of one to four rows a request; lengths change from step to step under one graph, tokens that are refused are
+    forgotten and their blocks used again."""
+    m = shape(4, 2, 64, dtype, layers=1)
+    n, most = 5, 30
+    states = [spec_state(m, n, most), spec_state(m, n, most)]
+    spec_step(m, states[1])                                    # (once outside the capture: modules are loaded)
+    states[1] = spec_state(m, n, most)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        spec_step(m, states[1])
+    torch.cuda.synchronize()
+    history = [[] for _ in range(n)]                           # (k, v) of a request's tokens, in 64 bits, as cached
+    for step in range(8):
+        rng = np.random.default_rng(step)
+        new = np.array([30, 17, 1, 0, 25]) if step == 0 else rng.integers(0, 5, n)
+        ctx = np.array([len(h) for h in history])
+        g = torch.Generator(device="cuda").manual_seed(100 + step)
+        qkv = torch.randn(n * most, m.qkv_dim, device="cuda", generator=g).to(DT[dtype])
+        draft = torch.randint(0, 500, (n * most,), device="cuda", generator=g, dtype=torch.int32)
+        for st in states:
+            st["ctx"].copy_(ints(ctx)); st["new"].copy_(ints(new)); st["qkv"].copy_(qkv); st["draft"].copy_(draft)
+        torch.cuda.synchronize()
+        spec_step(m, states[0])
+        graph.replay()
+        torch.cuda.synchronize()
+        a, b = states
+        for key in ("tok", "acc", "o", "table", "q"):
+            assert torch.equal(a[key], b[key]), (step, key)
+        assert all(torch.equal(x, y) for x, y in zip(a["tables"], b["tables"])) and int(a["tables"].status) == 0
+        start = np.concatenate([[0], np.cumsum(new)])
+        # the cache as the kernels left it is the oracle's input; every row's attention and verification follows from it
+        slots, o = a["tables"].slot_map.cpu().numpy(), f64(a["o"])
+        flat = [f64(a["pool"][0, i]).transpose(0, 2, 1, 3).reshape(-1, m.n_kv_heads, m.head_dim) for i in (0, 1)]
+        case = dict(m=m, q=a["q"], start=start, ctx=ctx, window=40, sinks=2, kv=[])
+        acc, tok = a["acc"].cpu().numpy(), a["tok"].cpu().numpy()
+        for r in range(n):
+            h = history[r] + [(flat[0][s], flat[1][s]) for s in slots[start[r]:start[r + 1]]]
+            case["kv"].append(np.stack([np.stack([x[i] for x in h]) if h else np.zeros((0, m.n_kv_heads, m.head_dim)) for i in (0, 1)]))
+            if new[r]:
+                z = a["logits"][start[r]:start[r + 1]].cpu().numpy()
+                want, k, _ = O.verify_request(z, draft[start[r]:start[r + 1] - 1].cpu().numpy(), None, 0.0, np.zeros(most), 0.0)
+                assert acc[r] == k and np.array_equal(tok[start[r]:start[r + 1]], want)
+            history[r] = h if step == 0 else h[:len(history[r]) + (int(acc[r]) + 1 if new[r] else 0)]
+        check_attention(case, a["o"])
+        held = a["tables"].blocks_held.cpu().numpy()
+        table = a["table"].cpu().numpy()
+        owned = np.concatenate([table[r, :held[r]] for r in range(n)])
+        assert len(set(owned)) == len(owned) and int(a["tables"].free_count) + len(owned) == 200
+
+
+def test_other_streams_than_the_default_one():
+    m = shape(4, 2, 128)
+    c = attention_case(m, [300, 20], [1, 60], 100, 4, seed=9)
+    want = run_attention(c)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        c["q"].mul_(1.0)
+        got = [run_attention(c) for _ in range(3)]
+    side.synchronize()
+    assert all(torch.equal(want, g) for g in got)
+
+
+def test_the_binding_refuses_what_does_not_fit():
+    m = shape(4, 2, 128)
+    c = attention_case(m, [20, 3], [1, 2], 0, 0)
+    args = (c["m"], c["pool"], 0, c["q"], c["row_start"], c["kv_len"], c["table"], 0, 0, 2)
+
+    def swap(i, x):
+        return args[:i] + (x,) + args[i + 1:]
+    for bad in (swap(3, c["q"].float()), swap(3, c["q"][:, :-8]), swap(4, c["row_start"][:-1]), swap(5, c["kv_len"].long()), swap(6, c["table"][:1])):
+        with pytest.raises(ValueError):
+            B.blink_window_attention(*bad)
+    for bad in (swap(2, 2), swap(7, -1), swap(9, 0)):
+        with pytest.raises(B.BlinkError) as e:
+            B.blink_window_attention(*bad)
+        assert e.value.code == B.BLINK_EINVAL
+    with pytest.raises(B.BlinkError):
+        B.blink_window_attention(*args, workspace=torch.empty(1024, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(ValueError):
+        B.blink_window_attention(*args, out=c["q"][:1].clone())
