@@ -9,7 +9,6 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
-from functools import lru_cache
 from typing import NamedTuple
 
 import numpy as np
@@ -258,57 +257,23 @@ def blink_sample_noalloc(logits, top_k, temperature, ticket, gen_index, seed, ra
 
 
 # ---- operators of a speculative step: everything on the device, enqueued on torch's current stream ---------------------
-@lru_cache(maxsize=64)
-def _cfg_ref(m):
-    """The shape's struct by the shape's value (weights play no part in the operators)."""
-    cfg = make_model_cfg(m)
-    return cfg, C.addressof(cfg)
+_marshal_module = None
 
 
-def _on_device(*tensors):
-    """torch, and the device that all of them live on."""
-    import torch
-    dev = tensors[0].device
-    for t in tensors:
-        if t is not None and t.device != dev:
-            raise ValueError(f"tensors on {dev} and {t.device}")
-    if dev.type != "cuda":
-        raise ValueError(f"tensors on {dev}: the operators run on a CUDA device")
-    return torch, dev
-
-
-def _need(ok, what):
-    if not ok:
-        raise ValueError(what)
-
-
-def _ints(what, t, n=None):
-    import torch
-    _need(t.dtype == torch.int32 and t.dim() == 1 and (t.is_contiguous()) and (n is None or t.numel() == n),
-          f"{what}: contiguous int32 vector" + (f" of {n}" if n is not None else ""))
-
-
-def _rows_of(what, t, cols, dtype):
-    _need(t.dim() == 2 and t.shape[1] == cols and t.dtype == dtype and (t.stride(1) == 1 or cols == 1), f"{what}: [rows][{cols}] of {dtype}, rows contiguous")
-    return t.stride(0) if t.shape[0] > 1 else max(cols, t.stride(0))
-
-
-def _call(dev, name, *args):
-    """One call on torch's current stream of `dev`, with that device current."""
-    import torch
-    if torch.cuda.current_device() == dev.index:
-        rc = getattr(lib(), name)(*args, torch.cuda.current_stream(dev).cuda_stream)
-    else:
-        with torch.cuda.device(dev):
-            rc = getattr(lib(), name)(*args, torch.cuda.current_stream(dev).cuda_stream)
-    if rc != BLINK_OK:
-        raise BlinkError(rc, name)
-
-
-def _pool_ref(kv_pool):
-    kv = blink_kv_pool(C.sizeof(blink_kv_pool), 16, kv_pool.data_ptr(), kv_pool.numel() * kv_pool.element_size())
-    _need(kv_pool.is_contiguous(), "kv_pool: contiguous")
-    return kv, C.addressof(kv)
+def _marshal():
+    """The module that hands torch tensors to libblink.so (shapes and types are checked there, the call runs on torch's current stream of
+    the tensors' device)."""
+    global _marshal_module
+    if _marshal_module is None:
+        lib()
+        import torch  # noqa: F401  (its libraries are what the module links against)
+        try:
+            from . import _marshal as module
+        except ImportError as e:
+            raise RuntimeError("_marshal.so is missing or was built for another torch: run `python -m paper_2604_07609_b200.build` "
+                               f"(there is no fallback): {e}") from e
+        _marshal_module = module
+    return _marshal_module
 
 
 class StepTables(NamedTuple):
@@ -333,50 +298,34 @@ def blink_build_tables(ctx_len, new_len, blocks_held, free_blocks, free_count, b
     """Block tables and slot map of a step from the requests' lengths (torch CUDA int32 tensors; block_table [n][stride] gets the new
     blocks in place).  out: buffers to fill, as of make_step_tables (blocks_held and free_count may be the inputs); else
     max_rows says how many rows there can be."""
-    torch, dev = _on_device(ctx_len, new_len, blocks_held, free_blocks, free_count, block_table, *(out or ()))
-    n = ctx_len.numel()
-    for what, t, k in (("ctx_len", ctx_len, None), ("new_len", new_len, n), ("blocks_held", blocks_held, n), ("free_blocks", free_blocks, None),
-                       ("free_count", free_count, 1)):
-        _ints(what, t, k)
-    _need(block_table.dtype == torch.int32 and block_table.dim() == 2 and block_table.shape[0] == n and block_table.is_contiguous(),
-          f"block_table: contiguous int32 [{n}][stride]")
     if out is None:
-        _need(max_rows is not None, "max_rows: how many rows there can be (or out)")
-        out = make_step_tables(n, max_rows, dev)
-    out = StepTables(*out)
-    rows = out.positions.numel()
-    for what, t, k in zip(StepTables._fields, out, (n + 1, n, rows, rows, n, 1, 1)):
-        _ints(what, t, k)
-    _call(dev, "blink_build_tables", ctx_len.data_ptr(), new_len.data_ptr(), blocks_held.data_ptr(), n, free_blocks.data_ptr(), free_blocks.numel(),
-          free_count.data_ptr(), block_table.data_ptr(), block_table.shape[1], rows, out.blocks_held.data_ptr(), out.free_count.data_ptr(),
-          out.row_start.data_ptr(), out.kv_len.data_ptr(), out.positions.data_ptr(), out.slot_map.data_ptr(), out.status.data_ptr())
-    return out
+        if max_rows is None:
+            raise ValueError("max_rows: how many rows there can be (or out)")
+        out = make_step_tables(ctx_len.numel(), max_rows, ctx_len.device)
+    rc = (_marshal_module or _marshal()).build_tables(ctx_len, new_len, blocks_held, free_blocks, free_count, block_table, *out)
+    if rc != BLINK_OK:
+        raise BlinkError(rc, "blink_build_tables")
+    return out if type(out) is StepTables else StepTables(*out)
+
+
+def _torch_dtype(m):
+    import torch
+    return torch.bfloat16 if m.dtype == "bf16" else torch.float32
 
 
 def blink_qk_norm_rope(m, kv_pool, layer: int, qkv, q_gain, k_gain, positions, slot_map, out=None):
     """Norms of queries and keys per head (gains fp32 [head_dim], or None), rotation, new keys and values into the pool's layer.
     qkv [rows][(Hq + 2 Hkv) * hd] of the model dtype, or fp32.  Returns the queries, [rows][Hq * hd] of the model dtype."""
-    torch, dev = _on_device(kv_pool, qkv, positions, slot_map, q_gain, k_gain, out)
-    rows, q_dim = qkv.shape[0], m.n_q_heads * m.head_dim
-    dt = torch.bfloat16 if m.dtype == "bf16" else torch.float32
-    _need(qkv.dtype == dt or qkv.dtype == torch.float32, f"qkv: {dt} or float32")
-    stride = _rows_of("qkv", qkv, q_dim + 2 * m.n_kv_heads * m.head_dim, qkv.dtype)
-    for what, g in (("q_gain", q_gain), ("k_gain", k_gain)):
-        _need(g is None or (g.dtype == torch.float32 and g.shape == (m.head_dim,) and g.is_contiguous()), f"{what}: contiguous float32 [{m.head_dim}]")
-    _ints("positions", positions, rows)
-    _ints("slot_map", slot_map, rows)
     if out is None:
-        out = torch.empty(rows, q_dim, dtype=dt, device=dev)
-    _need(out.shape[0] == rows, f"out: {rows} rows")
-    cfg, kv = _cfg_ref(m), _pool_ref(kv_pool)
-    _call(dev, "blink_qk_norm_rope", cfg[1], kv[1], layer, qkv.data_ptr(), DTYPE_BF16 if qkv.dtype == torch.bfloat16 else DTYPE_FP32, stride,
-          q_gain.data_ptr() if q_gain is not None else None, k_gain.data_ptr() if k_gain is not None else None, positions.data_ptr(),
-          slot_map.data_ptr(), rows, out.data_ptr(), _rows_of("out", out, q_dim, dt))
+        out = qkv.new_empty(qkv.shape[0], m.n_q_heads * m.head_dim, dtype=_torch_dtype(m))
+    rc = (_marshal_module or _marshal()).qk_norm_rope(m, kv_pool, layer, qkv, q_gain, k_gain, positions, slot_map, out)
+    if rc != BLINK_OK:
+        raise BlinkError(rc, "blink_qk_norm_rope")
     return out
 
 
 def blink_window_attention_workspace(m, max_new: int) -> int:
-    return int(lib().blink_window_attention_workspace(_cfg_ref(m)[1], max_new))
+    return int(lib().blink_window_attention_workspace(C.byref(make_model_cfg(m)), max_new))
 
 
 def blink_window_attention(m, kv_pool, layer: int, q, row_start, kv_len, block_table, window: int, sinks: int, max_new: int, out=None,
@@ -384,24 +333,11 @@ def blink_window_attention(m, kv_pool, layer: int, q, row_start, kv_len, block_t
     """Attention of the step's rows q [rows][Hq * hd] over a layer of the paged pool: a row sees the keys up to its own position, the last
     `window` of them (0: all) and the first `sinks`.  max_new: rows of the longest request.  workspace: bytes on the device
     (blink_window_attention_workspace), one is taken from torch when None."""
-    torch, dev = _on_device(kv_pool, q, row_start, kv_len, block_table, out, workspace)
-    q_dim, n = m.n_q_heads * m.head_dim, kv_len.numel()
-    dt = torch.bfloat16 if m.dtype == "bf16" else torch.float32
-    stride = _rows_of("q", q, q_dim, dt)
-    _ints("kv_len", kv_len)
-    _ints("row_start", row_start, n + 1)
-    _need(block_table.dtype == torch.int32 and block_table.dim() == 2 and block_table.shape[0] == n and block_table.is_contiguous(),
-          f"block_table: contiguous int32 [{n}][stride]")
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    _need(out.shape[0] == q.shape[0], f"out: {q.shape[0]} rows")
-    cfg, kv = _cfg_ref(m), _pool_ref(kv_pool)
-    if workspace is None:
-        workspace = torch.empty(lib().blink_window_attention_workspace(cfg[1], max_new), dtype=torch.uint8, device=dev)
-    _need(workspace.is_contiguous(), "workspace: contiguous")
-    _call(dev, "blink_window_attention", cfg[1], kv[1], layer, q.data_ptr(), stride, q.shape[0], row_start.data_ptr(), kv_len.data_ptr(), n,
-          block_table.data_ptr(), block_table.shape[1], window, sinks, max_new, out.data_ptr(), _rows_of("out", out, q_dim, dt),
-          workspace.data_ptr(), workspace.numel() * workspace.element_size())
+        out = q.new_empty(q.shape)
+    rc = (_marshal_module or _marshal()).window_attention(m, kv_pool, layer, q, row_start, kv_len, block_table, window, sinks, max_new, out, workspace)
+    if rc != BLINK_OK:
+        raise BlinkError(rc, "blink_window_attention")
     return out
 
 
@@ -414,29 +350,13 @@ def blink_verify_drafts(logits, row_start, draft_tokens, draft_probs, temperatur
     """Drafted tokens against the target's logits [rows][vocab] (fp32), from given random numbers: u_accept [rows], u_pick [n], fp32.
     draft_probs: fp32 [rows][vocab], or None when drafts are certain.  temperature fp32 [n], 0: greedy.  Returns
     (tokens [rows]: accepted drafts, the token drawn, -1; number of accepted drafts [n])."""
-    torch, dev = _on_device(logits, row_start, draft_tokens, draft_probs, temperature, u_accept, u_pick, out_tokens, n_accepted, workspace)
-    rows, vocab = logits.shape
-    n = temperature.numel()
-    stride = _rows_of("logits", logits, vocab, torch.float32)
-    if draft_probs is not None:
-        _need(draft_probs.shape[0] == rows, f"draft_probs: {rows} rows")
-    _ints("row_start", row_start, n + 1)
-    _ints("draft_tokens", draft_tokens, rows)
-    for what, t, k in (("temperature", temperature, n), ("u_accept", u_accept, rows), ("u_pick", u_pick, n)):
-        _need(t.dtype == torch.float32 and t.shape == (k,) and t.is_contiguous(), f"{what}: contiguous float32 [{k}]")
     if out_tokens is None:
-        out_tokens = torch.empty(rows, dtype=torch.int32, device=dev)
+        out_tokens = draft_tokens.new_empty(draft_tokens.shape)
     if n_accepted is None:
-        n_accepted = torch.empty(n, dtype=torch.int32, device=dev)
-    _ints("out_tokens", out_tokens, rows)
-    _ints("n_accepted", n_accepted, n)
-    if workspace is None:
-        workspace = torch.empty(lib().blink_verify_workspace(rows, vocab), dtype=torch.uint8, device=dev)
-    _need(workspace.is_contiguous(), "workspace: contiguous")
-    _call(dev, "blink_verify_drafts", logits.data_ptr(), stride, rows, vocab, row_start.data_ptr(), n, draft_tokens.data_ptr(),
-          draft_probs.data_ptr() if draft_probs is not None else None, _rows_of("draft_probs", draft_probs, vocab, torch.float32) if draft_probs is not None else 0,
-          temperature.data_ptr(), u_accept.data_ptr(), u_pick.data_ptr(), out_tokens.data_ptr(), n_accepted.data_ptr(), workspace.data_ptr(),
-          workspace.numel() * workspace.element_size())
+        n_accepted = draft_tokens.new_empty(temperature.shape)
+    rc = (_marshal_module or _marshal()).verify_drafts(logits, row_start, draft_tokens, draft_probs, temperature, u_accept, u_pick, out_tokens, n_accepted, workspace)
+    if rc != BLINK_OK:
+        raise BlinkError(rc, "blink_verify_drafts")
     return out_tokens, n_accepted
 
 

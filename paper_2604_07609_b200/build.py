@@ -1,15 +1,17 @@
-"""Build libblink.so (CUDA kernels + C ABI) in-tree for sm_100a with nvcc."""
+"""Build libblink.so (CUDA kernels + C ABI) in-tree for sm_100a with nvcc, and beside it _marshal.so, which hands torch tensors to it."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libblink.so")
 OBJ = os.path.join(HERE, "_build")
+MARSHAL = os.path.join(HERE, "_marshal.so")
 
 
 def _newest(paths):
@@ -22,7 +24,32 @@ def sources():
     return out
 
 
+def build_marshal(force: bool = False) -> str:
+    """The operators' argument marshalling, against torch's headers (g++; no device code)."""
+    src = os.path.join(CSRC, "marshal.cpp")
+    if not force and os.path.exists(MARSHAL) and os.path.getmtime(MARSHAL) >= _newest([src, os.path.join(os.path.dirname(HERE), "include", "blink.h")]):
+        return MARSHAL
+    import torch
+    home = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+    cmd += ["-isystem" + d for d in (os.path.join(home, "include"), os.path.join(cuda, "include"), sysconfig.get_paths()["include"])]
+    cmd += [src, "-o", MARSHAL, "-L" + HERE, "-l:libblink.so", "-Wl,-rpath,$ORIGIN", "-L" + os.path.join(home, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu",
+            "-ltorch_python"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        sys.stderr.write(r.stdout + r.stderr)
+        raise RuntimeError("g++ failed building _marshal.so")
+    return MARSHAL
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
+    lib = build_library(force, verbose)
+    build_marshal(force)
+    return lib
+
+
+def build_library(force: bool = False, verbose: bool = False) -> str:
     srcs = sources()
     if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _newest(srcs):
         return LIB
