@@ -121,21 +121,42 @@ __global__ void __launch_bounds__(TAB_THREADS) blink_tables_kernel(const TablesA
     }
   }
   const int live = ok ? (int)tot_rows : 0;
-  for (int i = rank * TAB_THREADS + tid; i < a.max_rows; i += ctas * TAB_THREADS) {
-    int pos = -1, slot = -1;
-    if (i < live) {
-      int lo = 0, hi = a.n;
+  // rows, four in a row per thread: one search, the four blocks on their way together, 16 bytes a store
+  const bool vec = ((reinterpret_cast<uintptr_t>(a.positions) | reinterpret_cast<uintptr_t>(a.slot_map)) & 15) == 0;
+  for (int i0 = 4 * (rank * TAB_THREADS + tid); i0 < a.max_rows; i0 += 4 * ctas * TAB_THREADS) {
+    int lo = 0;
+    if (i0 < live) {
+      int hi = a.n;   // the last request that begins at or before the row
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (s_row[mid] <= i) lo = mid; else hi = mid;
+        if (s_row[mid] <= i0) lo = mid; else hi = mid;
       }
-      pos = s_ctx[lo] + (i - s_row[lo]);
-      const int b = pos / OPS_BLOCK, fresh = b - s_held[lo];
-      const int id = fresh >= 0 ? a.free_blocks[count - 1 - (s_need[lo] + fresh)] : a.block_table[(size_t)lo * a.stride + b];
-      if (id >= 0 && id <= TAB_MAX_BLOCK) slot = id * OPS_BLOCK + pos % OPS_BLOCK;
     }
-    a.positions[i] = pos;
-    a.slot_map[i] = slot;
+    int pos[4], slot[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int i = i0 + j;
+      pos[j] = slot[j] = -1;
+      if (i < live) {
+        while (s_row[lo + 1] <= i) ++lo;
+        pos[j] = s_ctx[lo] + (i - s_row[lo]);
+        const int b = pos[j] / OPS_BLOCK, fresh = b - s_held[lo];
+        slot[j] = fresh >= 0 ? a.free_blocks[count - 1 - (s_need[lo] + fresh)] : a.block_table[(size_t)lo * a.stride + b];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) slot[j] = slot[j] >= 0 && slot[j] <= TAB_MAX_BLOCK ? slot[j] * OPS_BLOCK + pos[j] % OPS_BLOCK : -1;
+    if (vec && i0 + 4 <= a.max_rows) {
+      *reinterpret_cast<int4*>(a.positions + i0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+      *reinterpret_cast<int4*>(a.slot_map + i0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (i0 + j < a.max_rows) {
+          a.positions[i0 + j] = pos[j];
+          a.slot_map[i0 + j] = slot[j];
+        }
+    }
   }
 }
 
@@ -154,7 +175,7 @@ extern "C" int blink_build_tables(const int32_t* ctx_len, const int32_t* new_len
   if (n_requests > OPS_MAX_REQUESTS || max_rows > 0x3fffffff) return BLINK_ETOOBIG;
   const TablesArgs a = {ctx_len, new_len, blocks_held, free_blocks, free_count, n_requests, free_capacity, table_stride, max_rows,
                         block_table, blocks_held_out, free_count_out, row_start, kv_len, positions, slot_map, status};
-  const int cluster = max_rows > 2 * TAB_THREADS || n_requests > TAB_THREADS ? 8 : 1;
+  const int cluster = max_rows > 4 * TAB_THREADS || n_requests > TAB_THREADS ? 8 : 1;
   const size_t smem = (size_t)(4 * n_requests + 2) * 4;
   return ops_launch(blink_tables_kernel, cluster, TAB_THREADS, smem, stream, cluster, false, a);
 }

@@ -4,23 +4,24 @@
 //   first refused i: a token from max(0, p_i - q_i), none refused: from p of the last row; by the inverse of its running sum in the order of
 //   the indexes: the first j with sum_{<= j} > v * sum
 //
-// Two kernels.  (1) Largest value, its index and the sum of exponentials of every chunk of every row: one pass over the logits, which is what
-// bounds the whole (HBM: 4 bytes an entry).  Exponentials in 32 bits, sums of a thread's entries in 32, everything above in 64: the
-// acceptance test is off by some 1e-8.  (2) A cluster of eight CTAs a request: the chunks become rows, the first refused draft is found, and
-// its row alone is drawn from.  That row's sums decide between neighbours that are as close as 1e-6, so its exponentials, sums and the running sum
-// are in 64 bits; a CTA keeps its eighth of them in shared memory, and sums go from CTA to CTA through distributed shared memory.  Sums
+// Two kernels.  (1) Largest value, its index and the sum of exponentials of pieces of 1024 entries of every row, a warp each: one pass over
+// the logits, which is what bounds the whole (HBM: 4 bytes an entry).  A lane has its 32 entries on their way at once, and sums against its own
+// largest, so that nothing waits for another warp.  Exponentials in 32 bits, sums of a lane's entries in 32, everything above in 64: the
+// acceptance test is off by some 1e-8.  (2) A cluster of 16 CTAs a request: pieces become rows, the first refused draft is found, and
+// its row alone is drawn from.  That row's sums decide between neighbours that are as close as 1e-6, so its exponentials, sums and the running
+// sum are in 64 bits; a thread keeps its 16 of them in registers, and sums go from CTA to CTA through distributed shared memory.  Sums
 // are taken in an order that sizes alone fix: the same call gives the same token.
 #include <cooperative_groups.h>
 
-#include <cmath>
+#include <utility>
 
 #include "ops.h"
 
 namespace blink {
 
-constexpr int VER_THREADS = 256, VER_EACH = 16, VER_CHUNK = VER_THREADS * VER_EACH;   // (1)
-constexpr int PICK_THREADS = 512, PICK_WARPS = PICK_THREADS / 32, PICK_CTAS = 8;      // (2)
-constexpr int PICK_SMEM = 200 * 1024;   // exponentials of up to 8 * 25600 entries are kept
+constexpr int VER_WARPS = 8, VER_EACH = 32, VER_CHUNK = 32 * VER_EACH;                             // (1): entries of a lane, of a warp
+constexpr int PICK_THREADS = 512, PICK_WARPS = 16, PICK_CTAS = 16;   // (2)
+constexpr int PICK_ROWS = 64;   // rows of a request whose largest values are kept until it is known which one is drawn from
 
 struct VerChunk {
   double sum;   // of exp((z - max) / T)
@@ -36,7 +37,8 @@ struct VerifyArgs {
   const float *temperature, *u_accept, *u_pick;
   int32_t *tokens, *accepted;
   VerChunk* chunks_of;   // [rows][chunks]
-  int n, rows, vocab, chunks, kept;
+  int n, rows, vocab, chunks;
+  bool vec, probs_vec;   // rows on 16-byte boundaries
 };
 
 // No number: as if the entry were not there.
@@ -47,97 +49,139 @@ __device__ __forceinline__ void ver_larger(float& m, int& i, float m2, int i2) {
   if (m2 > m || (m2 == m && i2 < i)) { m = m2; i = i2; }
 }
 
-template <bool VEC>
-__global__ void __launch_bounds__(VER_THREADS) blink_verify_rows_kernel(const VerifyArgs a) {
-  __shared__ float s_m[VER_THREADS / 32];
-  __shared__ int s_i[VER_THREADS / 32], s_req;
-  __shared__ double s_sum[VER_THREADS / 32];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int row = (int)(blockIdx.x / (unsigned)a.chunks), chunk = (int)(blockIdx.x - (unsigned)row * a.chunks);
-  const float* z = a.logits + row * a.logits_stride + (long long)chunk * VER_CHUNK;
-  const int n = min(VER_CHUNK, a.vocab - chunk * VER_CHUNK);
-  float v[VER_EACH];
+// Entries of 4 * lane + 128 * k + 0 .. 3 of a tile that has n of them; 16 bytes at a time where rows are aligned.
+template <int EACH>
+__device__ __forceinline__ void ver_load(float (&v)[EACH], const float* z, int n, bool vec, float behind) {
+  const int lane = threadIdx.x & 31;
 #pragma unroll
-  for (int k = 0; k < VER_EACH / 4; ++k) {
-    const int at = (k * VER_THREADS + tid) * 4;
-    if (VEC && at + 4 <= n) {
+  for (int k = 0; k < EACH / 4; ++k) {
+    const int at = k * 128 + lane * 4;
+    if (vec && at + 4 <= n) {
       const float4 x = __ldcg(reinterpret_cast<const float4*>(z + at));   // (the chosen row is read again, from L2)
       v[4 * k] = x.x; v[4 * k + 1] = x.y; v[4 * k + 2] = x.z; v[4 * k + 3] = x.w;
     } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[4 * k + j] = at + j < n ? __ldcg(z + at + j) : -INFINITY;
+      for (int j = 0; j < 4; ++j) v[4 * k + j] = at + j < n ? __ldcg(z + at + j) : behind;
     }
   }
-  if (tid == 0) s_req = -1;
+}
+
+__global__ void __launch_bounds__(VER_WARPS * 32) blink_verify_rows_kernel(const VerifyArgs a) {
+  __shared__ int s_req;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int groups = (a.chunks + VER_WARPS - 1) / VER_WARPS;
+  const int row = (int)(blockIdx.x / (unsigned)groups), chunk = (int)(blockIdx.x - (unsigned)row * groups) * VER_WARPS + warp;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (the second kernel waits for the whole of this one itself)
+  float v[VER_EACH];
+  if (chunk < a.chunks)
+    ver_load(v, a.logits + row * a.logits_stride + (long long)chunk * VER_CHUNK, min(VER_CHUNK, a.vocab - chunk * VER_CHUNK), a.vec, -INFINITY);
+  if (threadIdx.x == 0) s_req = -1;
   __syncthreads();
-  for (int r = tid; r < a.n; r += VER_THREADS)
+  for (int r = threadIdx.x; r < a.n; r += VER_WARPS * 32)
     if (a.row_start[r] <= row && row < a.row_start[r + 1]) s_req = r;
+  __syncthreads();
+  const int req = s_req;
+  if (req < 0 || chunk >= a.chunks) return;   // (whole warps) a row behind the last request
+  const float T = a.temperature[req];
   float m = -INFINITY;
-  int idx = 0x7fffffff;
 #pragma unroll
   for (int k = 0; k < VER_EACH; ++k) {
     v[k] = ver_entry(v[k]);
-    const int at = ((k >> 2) * VER_THREADS + tid) * 4 + (k & 3);
-    if (v[k] > m || idx == 0x7fffffff) { m = v[k]; idx = at; }   // ascending
+    m = fmaxf(m, v[k]);
   }
+  int idx = 0;
+#pragma unroll
+  for (int k = VER_EACH - 1; k >= 0; --k)
+    if (v[k] == m) idx = (k >> 2) * 128 + lane * 4 + (k & 3);
+  const float mine = m;
 #pragma unroll
   for (int d = 16; d; d >>= 1) {
     const float m2 = __shfl_xor_sync(0xffffffffu, m, d);
     const int i2 = __shfl_xor_sync(0xffffffffu, idx, d);
     ver_larger(m, idx, m2, i2);
   }
-  if (lane == 0) { s_m[warp] = m; s_i[warp] = idx; }
-  __syncthreads();
-  const int req = s_req;
-  if (req < 0) return;   // a row behind the last request
-#pragma unroll
-  for (int w = 0; w < VER_THREADS / 32; ++w) ver_larger(m, idx, s_m[w], s_i[w]);
-  const float T = a.temperature[req];
   double sum = 0.0;
   if (T > 0.f && T < INFINITY && m > -INFINITY && m < INFINITY) {
     const float scale = fminf(1.4426950408889634f / T, 3e38f);
-    float s = 0.f;
+    const float base = mine == -INFINITY ? 0.f : mine;
+    float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-    for (int k = 0; k < VER_EACH; ++k) s += exp2f((v[k] - m) * scale);   // (behind the end: exp2(-inf))
-    sum = (double)s;
+    for (int k = 0; k < VER_EACH; k += 2) {   // (no entry: exp2(-inf))
+      s0 += exp2f((v[k] - base) * scale);
+      s1 += exp2f((v[k + 1] - base) * scale);
+    }
+    sum = (double)(s0 + s1) * (double)exp2f((mine - m) * scale);
 #pragma unroll
     for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    if (lane == 0) s_sum[warp] = sum;
-    __syncthreads();
-    sum = 0.0;
-#pragma unroll
-    for (int w = 0; w < VER_THREADS / 32; ++w) sum += s_sum[w];
   }
-  if (tid == 0) a.chunks_of[(size_t)row * a.chunks + chunk] = VerChunk{sum, m, chunk * VER_CHUNK + idx};
+  if (lane == 0) a.chunks_of[(size_t)row * a.chunks + chunk] = VerChunk{sum, m, chunk * VER_CHUNK + idx};
 }
 
-__global__ void __launch_bounds__(PICK_THREADS) blink_verify_pick_kernel(const VerifyArgs a) {
+// 2^t for t <= 0 in 64 bits: the whole part into the exponent, the rest, at most half, by the series of exp(f ln 2) up to its tenth power
+// (off by (ln 2 / 2)^11 / 11! = 2e-13).  Below 2^-1020: 0.
+__device__ __forceinline__ double ver_exp2(double t) {
+  constexpr double L = 0.693147180559945309417;
+  constexpr double C2 = L * L / 2, C3 = C2 * L / 3, C4 = C3 * L / 4, C5 = C4 * L / 5, C6 = C5 * L / 6, C7 = C6 * L / 7, C8 = C7 * L / 8, C9 = C8 * L / 9,
+                   C10 = C9 * L / 10;
+  constexpr double SHIFT = 6755399441055744.0;   // 1.5 * 2^52: adding it leaves the nearest whole number in the low bits
+  const double s = t + SHIFT, f = t - (s - SHIFT), f2 = f * f;
+  const int n = __double2loint(s);
+  const double a = fma(f2, fma(f2, fma(f2, fma(f2, C10, C8), C6), C4), C2), b = fma(f2, fma(f2, fma(f2, fma(f2, C9, C7), C5), C3), L);
+  const double p = fma(f, b, fma(f2, a, 1.0));   // even and odd powers side by side
+  return t > -1020.0 ? __hiloint2double(__double2hiint(p) + (n << 20), __double2loint(p)) : 0.0;
+}
+
+// The first of 16 parts (a lane each, lanes 16 .. 31 have 0) whose running sum exceeds target, else the last with anything in it; `base` grows by
+// what stands before it.
+__device__ __forceinline__ int ver_part(double part, double target, double& base) {
+  const int lane = threadIdx.x & 31;
+  double c = part;
+#pragma unroll
+  for (int d = 1; d < 16; d <<= 1) {
+    const double u = __shfl_up_sync(0xffffffffu, c, d);
+    if (lane >= d) c += u;
+  }
+  const unsigned hit = __ballot_sync(0xffffffffu, part > 0.0 && base + c > target), any = __ballot_sync(0xffffffffu, part > 0.0);
+  const int at = hit ? __ffs(hit) - 1 : any ? 31 - __clz(any) : 0;
+  const double before = __shfl_sync(0xffffffffu, c, max(at - 1, 0));
+  if (at > 0) base += before;
+  return at;
+}
+
+// EACH: entries of a lane at a time.
+template <int EACH>
+__global__ void __launch_bounds__(PICK_THREADS, 2) blink_verify_pick_kernel(const VerifyArgs a) {
   namespace cg = cooperative_groups;
+  constexpr int TILE = 32 * EACH;
   cg::cluster_group cluster = cg::this_cluster();
-  extern __shared__ double s_e[];            // exp((z - max) / T) of this CTA's entries, when they fit
-  __shared__ double s_part[PICK_WARPS];      // a sum per warp
-  __shared__ double s_all[2][PICK_CTAS];     // a sum per CTA, the same in all of them
-  __shared__ int s_first, s_index, s_one;
-  __shared__ float s_max;
+  __shared__ __align__(16) float s_q[PICK_WARPS][TILE];   // a tile of q per warp, each lane's own entries
+  __shared__ double s_part[PICK_WARPS];                   // a sum per warp
+  __shared__ double s_all[2][PICK_CTAS];                  // a sum per CTA, the same in all of them
+  __shared__ int s_first, s_one[PICK_ROWS], s_index[PICK_ROWS];
+  __shared__ float s_max[PICK_ROWS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = (int)cluster.block_rank(), req = (int)(blockIdx.x / PICK_CTAS);
   const int V = a.vocab;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  // (all but the pieces is there before the first kernel is done)
   const int start = min(max(a.row_start[req], 0), a.rows), end = min(max(a.row_start[req + 1], start), a.rows);
-  if (start == end) {   // (the whole cluster)
+  const int k = end - start - 1;
+  const float T = a.temperature[req];
+  const double to_exp2 = 1.44269504088896340736 / (double)T;
+  if (tid == 0) s_first = k;
+  __syncthreads();
+  if (start == end) {   // (the whole cluster; not before the first kernel, or the next one in the stream could be)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     if (rank == 0 && tid == 0) a.accepted[req] = 0;
     return;
   }
-  const int k = end - start - 1;
-  const float T = a.temperature[req];
-  const double inv_T = 1.0 / (double)T;
 
-  // A row from its chunks: largest value, its index, sum.  A row with an infinite largest value or without any number, and every
+  // A row from its pieces: largest value, its index, sum.  A row with an infinite largest value or without any number, and every
   // row at a T that is not above 0 and finite, stands for its largest entry alone.
-  auto row_of = [&](int row, float& m, int& idx, double& sum) {
+  auto row_of = [&](int row, float& m, int& idx, double& sum, bool with_sum) {
     const VerChunk* c = a.chunks_of + (size_t)row * a.chunks;
     m = -INFINITY;
     idx = 0x7fffffff;
+#pragma unroll 4
     for (int j = lane; j < a.chunks; j += 32) ver_larger(m, idx, c[j].max, c[j].index);
 #pragma unroll
     for (int d = 16; d; d >>= 1) {
@@ -147,155 +191,225 @@ __global__ void __launch_bounds__(PICK_THREADS) blink_verify_pick_kernel(const V
     }
     const bool one = !(T > 0.f && T < INFINITY) || !(m > -INFINITY) || !(m < INFINITY);
     sum = 0.0;
-    if (!one) {
-      for (int j = lane; j < a.chunks; j += 32) sum += c[j].max > -INFINITY ? c[j].sum * exp(((double)c[j].max - (double)m) * inv_T) : 0.0;
+    if (!one && with_sum) {
+#pragma unroll 4
+      for (int j = lane; j < a.chunks; j += 32) sum += c[j].max > -INFINITY ? c[j].sum * ver_exp2(((double)c[j].max - (double)m) * to_exp2) : 0.0;
 #pragma unroll
       for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
     }
     return one;
   };
-  if (tid == 0) s_first = k;
-  __syncthreads();
-  for (int i = warp; i < k; i += PICK_WARPS) {
+  for (int i = warp; i <= k; i += PICK_WARPS) {   // (row k: no draft)
     float m;
     int idx;
     double sum;
-    const int row = start + i, x = a.draft[row];
-    const bool one = row_of(row, m, idx, sum);
-    bool ok = false;
-    if (one) ok = x == idx;
-    else if (x >= 0 && x < V) {
-      const float z = ver_entry(__ldcg(a.logits + row * a.logits_stride + x));
-      const double p = exp(((double)z - (double)m) * inv_T);   // times sum
-      const double q = a.probs ? (double)a.probs[row * a.probs_stride + x] : 1.0;
-      ok = (double)a.u_accept[row] * q * sum < p;
+    const int row = start + i, x = i < k ? a.draft[row] : -1;
+    const bool in = x >= 0 && x < V;
+    const float z = in ? ver_entry(__ldcg(a.logits + row * a.logits_stride + x)) : -INFINITY, q = in && a.probs ? a.probs[row * a.probs_stride + x] : 1.f;
+    const float u = a.u_accept[row];
+    if (i == warp) asm volatile("griddepcontrol.wait;" ::: "memory");
+    const bool one = row_of(row, m, idx, sum, i < k);
+    const bool ok = i == k || (one ? x == idx : in && (double)u * (double)q * sum < ver_exp2(((double)z - (double)m) * to_exp2));
+    if (lane == 0) {
+      if (i < PICK_ROWS) {
+        s_one[i] = one;
+        s_max[i] = m;
+        s_index[i] = idx;
+      }
+      if (!ok) atomicMin(&s_first, i);
     }
-    if (lane == 0 && !ok) atomicMin(&s_first, i);
   }
+  if (warp > k) asm volatile("griddepcontrol.wait;" ::: "memory");
   __syncthreads();
   const int acc = s_first, row = start + acc;
-  if (warp == 0) {
-    float m;
-    int idx;
-    double sum;
-    const bool one = row_of(row, m, idx, sum);
-    if (lane == 0) { s_one = one; s_max = m; s_index = idx; }
-  }
-  __syncthreads();
+  // the row's entries: a run of tiles per warp, in the order of CTAs, warps and tiles
+  const int tiles = (V + PICK_CTAS * PICK_WARPS * TILE - 1) / (PICK_CTAS * PICK_WARPS * TILE);
+  const int w0 = (rank * PICK_WARPS + warp) * tiles * TILE;
+  const float* z = a.logits + row * a.logits_stride;
+  const float* q = acc < k && a.probs ? a.probs + row * a.probs_stride : nullptr;
+  float zv[EACH];   // of the warp's first tile
+  ver_load(zv, z + w0, V - w0, a.vec, -INFINITY);
+  auto fetch_q = [&](int at) {
+#pragma unroll
+    for (int g = 0; g < EACH / 4; ++g) {
+      const int o = g * 128 + lane * 4;
+      const uint32_t dst = (uint32_t)__cvta_generic_to_shared(&s_q[warp][o]);
+      if (a.probs_vec && at + o + 4 <= V) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(q + at + o) : "memory");
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (at + o + j < V) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + 4 * j), "l"(q + at + o + j) : "memory");
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  if (q) fetch_q(w0);
   if (rank == 0) {
     if (tid == 0) a.accepted[req] = acc;
     for (int i = tid; i <= k; i += PICK_THREADS)
       if (i != acc) a.tokens[start + i] = i < acc ? a.draft[start + i] : -1;
   }
-  if (s_one) {
-    if (rank == 0 && tid == 0) a.tokens[row] = s_index;
+  float top;
+  int index;
+  bool one;
+  if (acc < PICK_ROWS) {
+    top = s_max[acc];
+    index = s_index[acc];
+    one = s_one[acc] != 0;
+  } else {
+    double sum;
+    one = row_of(row, top, index, sum, false);
+  }
+  if (one) {
+    if (rank == 0 && tid == 0) a.tokens[row] = index;
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
     return;
   }
+  cg::cluster_group::arrival_token there = cluster.barrier_arrive();   // all CTAs have to be there before they are written to
 
-  cluster.sync();   // all CTAs are there to be written to
-  // the row's sum: this CTA's entries [lo, hi), a run of them per warp
-  const double m = (double)s_max;
-  const float* z = a.logits + row * a.logits_stride;
-  const int per = ((V + PICK_CTAS - 1) / PICK_CTAS + 31) & ~31, run = ((per + PICK_WARPS - 1) / PICK_WARPS + 31) & ~31;
-  const int lo = min(V, rank * per), hi = min(V, lo + per);
-  const int w0 = min(hi, lo + warp * run), w1 = min(hi, w0 + run);
-  const bool kept = a.kept != 0;
-  auto e_of = [&](int j) { return exp(((double)ver_entry(__ldcg(z + j)) - m) * inv_T); };
-  // sum over the warp's run -> over the CTA -> over the cluster; s_part keeps the warps', s_all the CTAs'
+  const double m = (double)top;
+  double e[EACH];
+  auto exps = [&]() {
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) e[i] = ver_exp2(((double)ver_entry(zv[i]) - m) * to_exp2);
+  };
+  auto lane_sum = [&]() {
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < EACH; i += 4) s += (e[i] + e[i + 1]) + (e[i + 2] + e[i + 3]);
+    return s;
+  };
+  // sum over the lanes -> over the CTA -> over the cluster; s_part keeps the warps', s_all the CTAs'
   auto sum_all = [&](double s, int which) {
 #pragma unroll
     for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-    __syncthreads();
     if (lane == 0) s_part[warp] = s;
     __syncthreads();
-    if (tid < PICK_CTAS) {
-      double t = 0.0;
-      for (int w = 0; w < PICK_WARPS; ++w) t += s_part[w];
-      *cluster.map_shared_rank(&s_all[which][rank], tid) = t;
+    if (warp == 0) {
+      double t = s_part[lane & 15];
+#pragma unroll
+      for (int d = 8; d; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
+      if (lane < PICK_CTAS) *cluster.map_shared_rank(&s_all[which][rank], lane) = t;
     }
     cluster.sync();
-    double t = 0.0;
-    for (int c = 0; c < PICK_CTAS; ++c) t += s_all[which][c];
+    double t = s_all[which][lane & 15];
+#pragma unroll
+    for (int d = 8; d; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
     return t;
   };
+  auto load_more = [&](int t) {   // tiles behind the first are read again in every pass
+    const int at = w0 + t * TILE;
+    ver_load(zv, z + at, V - at, a.vec, -INFINITY);
+    if (q) fetch_q(at);
+  };
   double s = 0.0;
-  for (int j = w0 + lane; j < w1; j += 32) {
-    const double e = e_of(j);
-    if (kept) s_e[j - lo] = e;
-    s += e;
+#pragma unroll 1
+  for (int t = tiles - 1; t >= 0; --t) {   // (the first last: it stays)
+    if (tiles > 1) load_more(t);
+    exps();
+    s += lane_sum();
   }
+  cluster.barrier_wait(std::move(there));
   const double inv_S = 1.0 / sum_all(s, 0);
 
   // what is drawn from: p - q where a draft was refused (what is no number or negative in q counts as 0), p otherwise
-  const float* q = acc < k && a.probs ? a.probs + row * a.probs_stride : nullptr;
   int x = acc < k && !a.probs ? a.draft[row] : -1;
-  auto rest_of = [&](int j) {
-    const double p = (kept ? s_e[j - lo] : e_of(j)) * inv_S;
+  auto rests = [&](int t) {   // of tile t, whose exponentials are in e
+    const int at = w0 + t * TILE + lane * 4;
     if (q) {
-      const float t = __ldg(q + j);
-      return t > 0.f ? fmax(p - (double)t, 0.0) : p;
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
+#pragma unroll
+      for (int i = 0; i < EACH; i += 4) {
+        const float4 v = *reinterpret_cast<const float4*>(&s_q[warp][i * 32 + lane * 4]);
+        const float w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const double p = e[i + j] * inv_S;
+          e[i + j] = w[j] > 0.f && at + i * 32 + j < V ? fmax(p - (double)w[j], 0.0) : p;   // (behind the end: nothing was fetched, and p is 0)
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) {
+        const double p = e[i] * inv_S;
+        e[i] = at + (i >> 2) * 128 + (i & 3) == x ? 0.0 : p;
+      }
     }
-    return j == x ? 0.0 : p;
   };
+  bool have = tiles == 1;   // the exponentials of the only tile are in e
   auto rest_sum = [&]() {
-    double t = 0.0;
-    for (int j = w0 + lane; j < w1; j += 32) t += rest_of(j);
-    return sum_all(t, 1);
+    double r = 0.0;
+#pragma unroll 1
+    for (int t = tiles - 1; t >= 0; --t) {
+      if (!have) {
+        load_more(t);
+        exps();
+      }
+      rests(t);
+      r += lane_sum();
+    }
+    return sum_all(r, 1);
   };
-  double total = rest_sum();
-  if (!(total > 0.0)) {   // q covers p everywhere: from p itself
-    q = nullptr;
-    x = -1;
-    cluster.sync();       // (everybody has read the sums)
+  double total;
+#pragma unroll 1
+  while (true) {
     total = rest_sum();
+    if (total > 0.0 || (!q && x < 0)) break;
+    q = nullptr;          // q covers p everywhere: from p itself
+    x = -1;
+    have = false;
+    cluster.sync();       // (everybody has read the sums)
   }
   const double target = (double)a.u_pick[req] * total;
   // the CTA, and the warp in it, whose run takes the sum past the target; else the last with anything in it
-  int cta = -1, last_cta = 0;
-  double before = 0.0, base = 0.0, last_base = 0.0;
-  for (int c = 0; c < PICK_CTAS; ++c) {
-    const double t = s_all[1][c];
-    if (t > 0.0) {
-      last_cta = c;
-      last_base = before;
-      if (cta < 0 && before + t > target) { cta = c; base = before; }
+  double base = 0.0;
+  if (ver_part(lane < PICK_CTAS ? s_all[1][lane] : 0.0, target, base) != rank) return;
+  if (ver_part(lane < PICK_WARPS ? s_part[lane] : 0.0, target, base) != warp) return;
+  int token = -1, last = 0;
+#pragma unroll 1
+  for (int t = 0; t < tiles && token < 0; ++t) {
+    if (tiles > 1) {   // (one tile: its are in e)
+      load_more(t);
+      exps();
+      rests(t);
     }
-    before += t;
-  }
-  if (cta < 0) { cta = last_cta; base = last_base; }
-  if (cta == rank) {
-    int w = -1, last_w = 0;
-    double at = base, w_base = base, last_w_base = base;
-    for (int c = 0; c < PICK_WARPS; ++c) {
-      const double t = s_part[c];
-      if (t > 0.0) {
-        last_w = c;
-        last_w_base = at;
-        if (w < 0 && at + t > target) { w = c; w_base = at; }
-      }
-      at += t;
-    }
-    if (w < 0) { w = last_w; w_base = last_w_base; }
-    if (w == warp) {
-      int token = -1, last = w0;
-      for (int j0 = w0; j0 < w1 && token < 0; j0 += 32) {
-        const int j = j0 + lane;
-        const double r = j < w1 ? rest_of(j) : 0.0;
-        double c = r;
+    double c[EACH / 4];   // running sums over the lanes, of each group of 128
 #pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-          const double u = __shfl_up_sync(0xffffffffu, c, d);
-          if (lane >= d) c += u;
-        }
-        const unsigned hit = __ballot_sync(0xffffffffu, r > 0.0 && w_base + c > target), some = __ballot_sync(0xffffffffu, r > 0.0);
-        if (hit) token = j0 + __ffs(hit) - 1;
-        else if (some) last = j0 + 31 - __clz(some);
-        w_base += __shfl_sync(0xffffffffu, c, 31);
+    for (int g = 0; g < EACH / 4; ++g) c[g] = (e[4 * g] + e[4 * g + 1]) + (e[4 * g + 2] + e[4 * g + 3]);
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+#pragma unroll
+      for (int g = 0; g < EACH / 4; ++g) {
+        const double u = __shfl_up_sync(0xffffffffu, c[g], d);
+        if (lane >= d) c[g] += u;
       }
-      if (lane == 0) a.tokens[row] = token >= 0 ? token : last;
+    }
+#pragma unroll
+    for (int g = 0; g < EACH / 4; ++g) {
+      const double up = __shfl_up_sync(0xffffffffu, c[g], 1);
+      double run = lane ? base + up : base;
+      int hit = 4, some = -1;   // of the lane's four
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        run += e[4 * g + j];
+        if (e[4 * g + j] > 0.0) {
+          some = j;
+          if (hit == 4 && run > target) hit = j;
+        }
+      }
+      const unsigned hits = __ballot_sync(0xffffffffu, hit < 4), any = __ballot_sync(0xffffffffu, some >= 0);
+      const int at = w0 + t * TILE + g * 128;
+      const int l = hits ? __ffs(hits) - 1 : any ? 31 - __clz(any) : 0;
+      const int h = __shfl_sync(0xffffffffu, hit, l), o = __shfl_sync(0xffffffffu, some, l);
+      if (token < 0) {
+        if (hits) token = at + l * 4 + h;
+        else if (any) last = at + l * 4 + o;
+      }
+      base += __shfl_sync(0xffffffffu, c[g], 31);
     }
   }
-  cluster.sync();   // nobody leaves while another may still write into its shared memory
+  if (lane == 0) a.tokens[row] = token >= 0 ? token : last;
 }
 
 static int64_t verify_chunks(int vocab) { return ((int64_t)vocab + VER_CHUNK - 1) / VER_CHUNK; }
@@ -338,13 +452,16 @@ int blink_verify_drafts(const float* logits, int64_t logits_stride, int rows, in
   a.rows = rows;
   a.vocab = vocab;
   a.chunks = (int)verify_chunks(vocab);
-  const int64_t slice = (((int64_t)vocab + PICK_CTAS - 1) / PICK_CTAS + 31) & ~31ll;
-  a.kept = slice * 8 <= PICK_SMEM;
-  const bool vec = logits_stride % 4 == 0 && ops_aligned(logits, 16);
-  const int64_t grid = (int64_t)rows * a.chunks;
-  int rc = ops_launch(vec ? blink_verify_rows_kernel<true> : blink_verify_rows_kernel<false>, grid, VER_THREADS, 0, stream, 0, false, a);
+  a.vec = logits_stride % 4 == 0 && ops_aligned(logits, 16);
+  a.probs_vec = draft_probs && probs_stride % 4 == 0 && ops_aligned(draft_probs, 16);
+  const int64_t grid = (int64_t)rows * ((a.chunks + VER_WARPS - 1) / VER_WARPS);
+  int rc = ops_launch(blink_verify_rows_kernel, grid, VER_WARPS * 32, 0, stream, 0, false, a);
   if (rc != BLINK_OK) return rc;
-  return ops_launch(blink_verify_pick_kernel, (int64_t)n_requests * PICK_CTAS, PICK_THREADS, a.kept ? (size_t)slice * 8 : 0, stream, PICK_CTAS, true, a);
+  // as few entries of a lane as hold the row in one go: 32768 entries in 16 CTAs of 16 warps with four, 131072 with 16 (beyond that, runs of tiles)
+  const int64_t ctas = (int64_t)n_requests * PICK_CTAS;
+  if (vocab <= 32768) return ops_launch(blink_verify_pick_kernel<4>, ctas, PICK_THREADS, 0, stream, PICK_CTAS, true, a);
+  if (vocab <= 65536) return ops_launch(blink_verify_pick_kernel<8>, ctas, PICK_THREADS, 0, stream, PICK_CTAS, true, a);
+  return ops_launch(blink_verify_pick_kernel<16>, ctas, PICK_THREADS, 0, stream, PICK_CTAS, true, a);
 }
 
 }  // extern "C"
