@@ -34,8 +34,8 @@ struct FewCut {
   int row, m0, m1, h;    // first row of the request, rows (of row * rep + head) m0 .. m1 - 1, kv head
 };
 
-// workspace: cuts [FEW_MAX_CTAS], (maximum, sum) [2 * FEW_MAX_CTAS][MR], values [2 * FEW_MAX_CTAS][MR][HD]
-__host__ __device__ constexpr size_t few_ml_at() { return (sizeof(FewCut) * FEW_MAX_CTAS + 255) / 256 * 256; }
+// workspace: status, cuts [FEW_MAX_CTAS], (maximum, sum) [2 * FEW_MAX_CTAS][MR], values [2 * FEW_MAX_CTAS][MR][HD]
+__host__ __device__ constexpr size_t few_ml_at() { return ATTN_STATUS_BYTES + (sizeof(FewCut) * FEW_MAX_CTAS + 255) / 256 * 256; }
 __host__ __device__ constexpr size_t few_acc_at(int mr) { return few_ml_at() + (size_t)2 * FEW_MAX_CTAS * mr * 8; }
 __host__ __device__ constexpr size_t few_bytes(int mr, int hd) { return few_acc_at(mr) + (size_t)2 * FEW_MAX_CTAS * mr * hd * 4; }
 
@@ -349,6 +349,10 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) blink_attn_few_kernel(const
   int2* s_len = reinterpret_cast<int2*>(s_pre + a.n + 1);                                // [n] first row, kv_len
   __shared__ long long s_warp[FEW_WARPS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (blockIdx.x == 0 && tid == 0) {
+    *reinterpret_cast<int*>(a.ws) = 0;
+    __threadfence();
+  }
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (the join waits for the whole of this kernel itself)
 
   // the sequence of tiles: a run of requests per thread
@@ -458,7 +462,7 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) blink_attn_few_kernel(const
     if (t0 == 0 && !whole) cut = FewCut{(int)((at + shape.tiles - 1) / per) - (int)blockIdx.x + 1, req.start, m0, m1, h};
     at += t1 - t0;
   }
-  if (tid == 0) reinterpret_cast<FewCut*>(a.ws)[blockIdx.x] = cut;
+  if (tid == 0) reinterpret_cast<FewCut*>(a.ws + ATTN_STATUS_BYTES)[blockIdx.x] = cut;
 }
 
 // The parts of the unit that begins, but does not end, in the run of CTA blockIdx.x.  A row's parts are shared out over warps, and these joined
@@ -468,8 +472,8 @@ __global__ void __launch_bounds__(JOIN_THREADS) blink_attn_join_kernel(const __g
   constexpr int WARPS = JOIN_THREADS / 32, V = HD / 32;   // values of a row per lane
   __shared__ float s_acc[WARPS][HD];
   __shared__ float2 s_ml[WARPS];
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  const FewCut cut = reinterpret_cast<const FewCut*>(a.ws)[blockIdx.x];
+  asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
+  const FewCut cut = reinterpret_cast<const FewCut*>(a.ws + ATTN_STATUS_BYTES)[blockIdx.x];
   if (cut.parts == 0) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const float2* ml = reinterpret_cast<const float2*>(a.ws + few_ml_at());
@@ -548,7 +552,7 @@ static int few_bf16(const AttnArgs& a, int nt, int sms, void* stream) {
 }
 
 // Instructions' worth of rows (eight each) that a unit of the few-rows kernel holds.
-static int few_nt(int64_t m_rows) { return m_rows <= 8 ? 1 : m_rows <= 16 ? 2 : m_rows <= 24 ? 3 : 4; }
+static int few_nt(int64_t m_rows) { return m_rows <= 8 ? 1 : m_rows <= 16 || m_rows > 32 ? 2 : m_rows <= 24 ? 3 : 4; }
 
 static int few_rows_of(const blink_model_cfg* m, int max_new) {
   if (m->dtype == BLINK_DTYPE_FP32) return m->head_dim == 128 ? 4 : 8;
@@ -599,7 +603,10 @@ int blink_window_attention(const blink_model_cfg* model, const blink_kv_pool* kv
   if (model->dtype == BLINK_DTYPE_FP32)
     return a.pool.hd == 128 ? few_run<float, 128, FewFp32<128>, 2>(a, sms, stream) : few_run<float, 64, FewFp32<64>, 2>(a, sms, stream);
   const int nt = few_nt((int64_t)max_new * a.pool.rep);
-  return a.pool.hd == 128 ? few_bf16<128>(a, nt, sms, stream) : few_bf16<64>(a, nt, sms, stream);
+  const bool tiles = (int64_t)max_new * a.pool.rep > 32;
+  if (tiles) a.few = 8 * nt / a.pool.rep;
+  const int done = a.pool.hd == 128 ? few_bf16<128>(a, nt, sms, stream) : few_bf16<64>(a, nt, sms, stream);
+  return done != BLINK_OK || !tiles ? done : attn_tiles(a, sms, stream);
 }
 
 }  // extern "C"

@@ -47,6 +47,11 @@ __device__ __forceinline__ bool attn_sees(const AttnArgs& a, int key, int pos) {
   return key <= pos && (a.window == 0 || key > pos - a.window || key < a.sinks);
 }
 
+// The workspace begins with a word that is 0, or BLINK_ETIMEDOUT when a wait inside the kernels ran out.
+constexpr size_t ATTN_STATUS_BYTES = 256;
+// Requests of more than a.few rows on tcgen05 (ops_attn_tiles.cu); the others are in the stream before it.
+int attn_tiles(const AttnArgs& a, int sms, void* stream);
+
 __device__ __forceinline__ float attn_ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -1,0 +1,661 @@
+// blink_window_attention for requests of many rows (prompts and their chunks), on tcgen05.
+//
+// A unit is a request, a kv head and 2 * 128 (query row, head) rows: two streams of 128, the rep heads of the kv head beside one another, so that a
+// narrow window wastes little (4 heads: 64 query rows read the keys of their window once).  Keys come in tiles of 128: the visible
+// blocks of the unit, sinks first, eight to a tile, whatever lies between them.
+//
+//   warps 0-3 | 4-7   softmax of stream 0 | 1, a thread per row: scores from TMEM, probabilities back to TMEM over the scores
+//   warp 8            issues the MMAs: scores = Q K^T (operands in shared memory), output += P V (P in TMEM, V as it lies in the cache)
+//   warps 9, 10 | 11  copies of the keys' halves | of the values: a copy takes its thread some 100 cycles, a tile has 24
+//
+// While one stream is in its softmax the tensor core works for the other; the next scores of a stream are issued behind its output MMAs, so a
+// stream's scores being complete also says that its accumulator is.  The maximum in use follows the largest score only when that has grown
+// by more than 2^8 (the sum takes up smaller growth); then the scores, still in TMEM, are gone over once more and the accumulator is rescaled by
+// the thread that owns the row.  CTAs are persistent; keys of the next unit are on their way while the last tile of one is worked on.
+//
+// What bounds it: the softmax's exponentials: 128 rows x 128 keys are 1024 cycles of the unit that computes them, two streams 2048 a
+// tile, against 1024 of the tensor core.
+#include <cuda.h>
+
+#include <cmath>
+
+#include "ops_attention.cuh"
+
+namespace blink {
+
+constexpr int TIL_KEYS = 128, TIL_BLOCKS = TIL_KEYS / OPS_BLOCK;
+constexpr int TIL_WARPS = 12, TIL_THREADS = TIL_WARPS * 32;
+constexpr long long TIL_WAIT_CYCLES = 1ll << 32;   // some two seconds
+
+template <int HD>
+struct TilShape {
+  static constexpr int SLABS = HD / 64;                 // of 64 dims (128-byte rows)
+  static constexpr int TILE = TIL_KEYS * HD * 2;        // bytes of 128 rows
+  static constexpr int RING = 131072 / (2 * TILE);      // tiles of keys, and of values, in shared memory
+  static constexpr int Q = 0, K = 2 * TILE, V = K + RING * TILE, END = V + RING * TILE;
+};
+
+struct TilShared {
+  uint64_t q_full[2], s_full[2], p_full[2], o_full[2];
+  uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], v_land;
+  uint32_t tmem;
+  int dead;
+  int warp_sum[TIL_WARPS];
+};
+
+__device__ __forceinline__ uint32_t til_smem(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void til_init(uint64_t* bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(til_smem(bar)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void til_expect(uint64_t* bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(til_smem(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void til_arrive(uint64_t* bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(til_smem(bar)) : "memory");
+}
+__device__ __forceinline__ bool til_try(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok)
+               : "r"(til_smem(bar)), "r"(parity)
+               : "memory");
+  return ok != 0;
+}
+// A whole warp waits, with one answer for all lanes; bounded.  Whoever runs out of time says so, and everybody gives up.
+static __device__ __noinline__ bool til_wait_slow(uint64_t* bar, uint32_t parity, int* dead, int* status) {
+  const long long t0 = clock64();
+  unsigned spins = 0;
+  while (!__all_sync(0xffffffffu, til_try(bar, parity))) {
+    if ((++spins & 63u) == 0) {
+      bool stop = *(volatile int*)dead != 0;
+      if (!stop && clock64() - t0 > TIL_WAIT_CYCLES) {
+        *(volatile int*)dead = 1;
+        *(volatile int*)status = BLINK_ETIMEDOUT;
+        stop = true;
+      }
+      if (__any_sync(0xffffffffu, stop)) return false;
+    }
+  }
+  return true;
+}
+__device__ __forceinline__ bool til_elect() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
+}
+__device__ __forceinline__ uint32_t til_uniform(uint32_t v) { return __reduce_max_sync(0xffffffffu, v); }
+__device__ __forceinline__ void til_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void til_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void til_proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// 16 keys of the pool: 64 dims from x on, or (values) all dims as slabs of 64 one behind the other
+__device__ __forceinline__ void til_copy(uint32_t dst, const CUtensorMap* map, int row, int slab, int plane, uint64_t* bar, uint64_t policy) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4, %5}], [%6], %7;" ::"r"(dst),
+               "l"(map), "r"(0), "r"(row), "r"(slab), "r"(plane), "r"(til_smem(bar)), "l"(policy)
+               : "memory");
+}
+// D (+)= A B^T, both in shared memory
+__device__ __forceinline__ void til_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
+               "r"(accumulate)
+               : "memory");
+}
+// the same with A in TMEM
+__device__ __forceinline__ void til_mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc),
+               "r"(accumulate)
+               : "memory");
+}
+__device__ __forceinline__ void til_commit(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(til_smem(bar)) : "memory");
+}
+// Shared-memory operands with 128-byte swizzle.  K-major (128-byte rows of 64 bf16 along K): groups of eight rows 1024 bytes apart.
+// MN-major (128-byte rows of 64 along N): groups of eight K-rows 1024 bytes apart, the next 64 along N `slab` bytes on.
+__device__ __forceinline__ uint64_t til_desc(uint32_t saddr, uint32_t slab) {
+  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)(slab >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+__device__ __forceinline__ uint32_t til_idesc(int n) {   // bf16 operands, fp32 accumulator, M = 128
+  return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+}
+
+// 32 lanes x 32 columns, without the wait: nothing may touch the registers before til_wait_ld() has named them.
+__device__ __forceinline__ void til_ld32(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
+      "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+        "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+        "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+#define BLINK_RW8(r, i) "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7])
+__device__ __forceinline__ void tmem_wait_ld_til(uint32_t (&a)[32], uint32_t (&b)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : BLINK_RW8(a, 0), BLINK_RW8(a, 8), BLINK_RW8(a, 16), BLINK_RW8(a, 24), BLINK_RW8(b, 0), BLINK_RW8(b, 8), BLINK_RW8(b, 16),
+                 BLINK_RW8(b, 24)
+               :
+               : "memory");
+}
+#undef BLINK_RW8
+__device__ __forceinline__ void til_st32(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, "
+      "%22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
+      "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void til_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float2 til_fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 til_add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+
+// What a row sees of a tile: key x of block g of it (position at[g] + x) when x <= hi, and x > lo or x < sink.
+struct TilMask {
+  int pos, window, sinks, first_block, n_sinks, from;   // of the row; of the tile's first block in the unit's list; of the list
+};
+__device__ __forceinline__ void til_mask(uint32_t (&r)[32], const TilMask& k, int quarter) {
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const int i = k.first_block + quarter * 2 + b;
+    const int at = (i < k.n_sinks ? i : k.from + i - k.n_sinks) * OPS_BLOCK;
+    const int hi = k.pos - at, lo = k.window > 0 ? hi - k.window : -1, sink = k.sinks - at;
+#pragma unroll
+    for (int x = 0; x < OPS_BLOCK; ++x)
+      if (!(x <= hi && (x > lo || x < sink))) r[b * OPS_BLOCK + x] = 0xff800000u;
+  }
+}
+
+// One row of a score tile -> 64 words of probabilities (bf16 pairs), their sum, and the largest score.
+template <bool MASKED>
+__device__ __forceinline__ void til_probs(uint32_t t_s, float qscale, float neg, const TilMask& mask, uint32_t (&p)[64], float& mx, float& sum) {
+  const float2 scale2 = make_float2(qscale, qscale), neg2 = make_float2(neg, neg);
+  float mx0 = -INFINITY, mx1 = -INFINITY;
+  float2 s0 = make_float2(0.f, 0.f), s1 = s0;
+  auto quarter = [&](uint32_t (&r)[32], int k) {
+    if constexpr (MASKED) til_mask(r, mask, k);
+#pragma unroll
+    for (int x = 0; x < 32; x += 4) {
+      mx0 = fmaxf(fmaxf(mx0, __uint_as_float(r[x])), __uint_as_float(r[x + 1]));
+      mx1 = fmaxf(fmaxf(mx1, __uint_as_float(r[x + 2])), __uint_as_float(r[x + 3]));
+    }
+#pragma unroll
+    for (int x = 0; x < 32; x += 2) {
+      float2 e = til_fma2(make_float2(__uint_as_float(r[x]), __uint_as_float(r[x + 1])), scale2, neg2);
+      e.x = attn_ex2(e.x);
+      e.y = attn_ex2(e.y);
+      if (x & 2) s1 = til_add2(s1, e); else s0 = til_add2(s0, e);
+      const __nv_bfloat162 b2 = __floats2bfloat162_rn(e.x, e.y);
+      p[k * 16 + x / 2] = *reinterpret_cast<const uint32_t*>(&b2);
+    }
+  };
+  uint32_t va[32], vb[32], vc[32], vd[32];
+  til_ld32(t_s, va);
+  til_ld32(t_s + 32u, vb);
+  tmem_wait_ld_til(va, vb);
+  til_ld32(t_s + 64u, vc);
+  til_ld32(t_s + 96u, vd);
+  quarter(va, 0);
+  quarter(vb, 1);
+  tmem_wait_ld_til(vc, vd);
+  quarter(vc, 2);
+  quarter(vd, 3);
+  mx = fmaxf(mx0, mx1);
+  const float2 s = til_add2(s0, s1);
+  sum = s.x + s.y;
+}
+// The largest score alone, for a row's first tile.
+__device__ __forceinline__ float til_max(uint32_t t_s, bool masked, const TilMask& mask) {
+  float mx = -INFINITY;
+#pragma unroll 1
+  for (int k = 0; k < 4; k += 2) {
+    uint32_t va[32], vb[32];
+    til_ld32(t_s + 32u * k, va);
+    til_ld32(t_s + 32u * k + 32u, vb);
+    tmem_wait_ld_til(va, vb);
+    if (masked) {
+      til_mask(va, mask, k);
+      til_mask(vb, mask, k + 1);
+    }
+#pragma unroll
+    for (int x = 0; x < 32; ++x) mx = fmaxf(fmaxf(mx, __uint_as_float(va[x])), __uint_as_float(vb[x]));
+  }
+  return mx;
+}
+
+// A unit, and which of its tiles each stream takes.
+struct TilUnit {
+  int req, h;
+  int row, live[2];        // first of its rows; rows of each stream's
+  int pos;                 // position of the first row
+  AttnSpan span;
+  int last;                // position of the last row
+  int begin[2], end[2];    // tiles of each stream
+};
+
+template <int HD>
+__global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap key_map,
+                                                                          const __grid_constant__ CUtensorMap value_map) {
+  using S = TilShape<HD>;
+  extern __shared__ char s_raw[];
+  char* base = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(s_raw) + 1023) & ~(uintptr_t)1023);
+  int* s_pre = reinterpret_cast<int*>(base + S::END);   // [n + 1] units before a request
+  __shared__ __align__(16) TilShared sh;
+  const int w = (int)til_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  int* status = reinterpret_cast<int*>(a.ws);
+  const int P = 128 / a.pool.rep;                       // query rows of a stream
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < 2; ++s) {
+      til_init(&sh.q_full[s], 4);
+      til_init(&sh.s_full[s], 1);
+      til_init(&sh.p_full[s], 4);
+      til_init(&sh.o_full[s], 1);
+    }
+    for (int i = 0; i < 4; ++i) {
+      til_init(&sh.k_full[i], S::SLABS);
+      til_init(&sh.k_empty[i], 1);
+      til_init(&sh.v_full[i], 1);
+      til_init(&sh.v_empty[i], 1);
+    }
+    til_init(&sh.v_land, 1);
+    sh.dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (w == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(til_smem(&sh.tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  // the sequence of units: a run of requests per thread
+  {
+    const int each = (a.n + TIL_THREADS - 1) / TIL_THREADS;
+    const int r0 = min(a.n, (int)threadIdx.x * each), r1 = min(a.n, r0 + each);
+    int mine = 0;
+    for (int r = r0; r < r1; ++r) {
+      const AttnReq q = attn_req(a, a.row_start[r], a.row_start[r + 1], a.kv_len[r]);
+      s_pre[r] = mine;
+      if (q.rows > a.few) mine += (q.rows + 2 * P - 1) / (2 * P) * a.pool.Hkv;
+    }
+    int x = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, x, d);
+      if (lane >= d) x += y;
+    }
+    if (lane == 31) sh.warp_sum[w] = x;
+    __syncthreads();
+    for (int i = 0; i < w; ++i) x += sh.warp_sum[i];
+    for (int r = r0; r < r1; ++r) s_pre[r] += x - mine;
+    if (threadIdx.x == TIL_THREADS - 1) s_pre[a.n] = x;
+  }
+  til_fence_before();
+  __syncthreads();
+  til_fence_after();
+  const uint32_t tmem = til_uniform(*(volatile uint32_t*)&sh.tmem);
+  const int n_units = s_pre[a.n];
+
+  bool ok = true;   // false once a wait has run out
+  auto wait = [&](uint64_t* bar, uint32_t parity) {
+    if (ok && !__all_sync(0xffffffffu, til_try(bar, parity))) ok = til_wait_slow(bar, parity, &sh.dead, status);
+    return ok;
+  };
+  auto unit_of = [&](int u) {
+    TilUnit t;
+    int lo = 0, hi = a.n;   // the last request that begins at or before it
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (s_pre[mid] <= u) lo = mid; else hi = mid;
+    }
+    const AttnReq q = attn_req(a, a.row_start[lo], a.row_start[lo + 1], a.kv_len[lo]);
+    const int blocks = (q.rows + 2 * P - 1) / (2 * P);
+    const int i = u - s_pre[lo], b = blocks - 1 - i / a.pool.Hkv;   // later rows, which see more, first
+    t.req = lo;
+    t.h = i % a.pool.Hkv;
+    t.row = q.start + b * 2 * P;
+    const int rows = min(2 * P, q.rows - b * 2 * P);
+    t.live[0] = min(P, rows);
+    t.live[1] = rows - t.live[0];
+    t.pos = q.ctx + b * 2 * P;
+    t.last = t.pos + rows - 1;
+    t.span = attn_span(a, t.pos, t.last);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int first = t.pos + s * P, last = max(0, first + t.live[s] - 1);
+      const int from = a.window > 0 ? max(0, first - a.window + 1) / OPS_BLOCK : 0;
+      t.begin[s] = a.sinks > 0 ? 0 :   // (the sinks may lie in the unit's window, and not in the stream's)
+                                   min(max(0, from - t.span.from), t.span.n - 1) / TIL_BLOCKS;
+      t.end[s] = min(t.span.n - 1, max(0, t.span.sinks + last / OPS_BLOCK - t.span.from)) / TIL_BLOCKS + 1;
+      if (t.live[s] == 0) t.begin[s] = t.end[s] = 0;
+    }
+    return t;
+  };
+  auto tiles_of = [&](const TilUnit& t) { return max(t.end[0], t.end[1]); };   // (the first tile is one of stream 0, which always has rows)
+  // the tile of the list's blocks 8 j .. is read by streams [first, second)
+  auto takes = [&](const TilUnit& t, int s, int j) { return j >= t.begin[s] && j < t.end[s]; };
+
+  if (w < 8) {
+    // ---- softmax ----
+    const int s = w >> 2, q = w & 3, m = q * 32 + lane, rep = a.pool.rep;
+    const uint32_t t_row = (uint32_t)(q * 32) << 16;
+    const uint32_t t_s = tmem + (uint32_t)s * 128u + t_row, t_o = tmem + 256u + (uint32_t)(s * HD) + t_row;
+    const uint32_t b_q = til_smem(base) + S::Q + s * S::TILE;
+    uint32_t n_s = 0, n_o = 0;
+    auto load_q = [&](const TilUnit& t) {
+      constexpr int CH = HD / 8;   // 16-byte pieces of a row
+#pragma unroll 4
+      for (int k = 0; k < CH; ++k) {
+        const int i = k * 128 + (int)(threadIdx.x & 127), row = i / CH, ck = i % CH;
+        const int r = row / rep;
+        const bool live = r < t.live[s];
+        const char* src = static_cast<const char*>(a.q) + ((long long)(t.row + (live ? s * P + r : 0)) * a.q_stride + (t.h * rep + row % rep) * HD + ck * 8) * 2;
+        const uint32_t dst = b_q + (ck >> 3) * 16384 + row * 128 + (((ck & 7) ^ (row & 7)) << 4);
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16u : 0u) : "memory");
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    auto q_there = [&]() {
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
+      til_proxy_fence();
+      til_fence_before();   // (what was read of the accumulator comes before its next use)
+      __syncwarp();
+      if (lane == 0) til_arrive(&sh.q_full[s]);
+    };
+    int u = blockIdx.x;
+    TilUnit t, next;
+    if (u < n_units) {
+      t = unit_of(u);
+      if (t.live[s]) {
+        load_q(t);
+        q_there();
+      }
+    }
+    while (u < n_units) {
+      const int un = u + (int)gridDim.x;
+      if (un < n_units) next = unit_of(un);
+      const bool more = un < n_units && next.live[s] > 0;
+      if (t.live[s]) {
+        const int r = m / rep;
+        TilMask mask;
+        mask.pos = r < t.live[s] ? t.pos + s * P + r : -1;
+        mask.window = a.window;
+        mask.sinks = a.sinks;
+        mask.n_sinks = t.span.sinks;
+        mask.from = t.span.from;
+        const int p_lo = t.pos + s * P + (q * 32) / rep, p_hi = t.pos + s * P + (q * 32 + 31) / rep;
+        float mx_used = -INFINITY, l = 0.f;
+        for (int j = t.begin[s]; j < t.end[s]; ++j) {
+          mask.first_block = j * TIL_BLOCKS;
+          const int i0 = mask.first_block, i1 = i0 + TIL_BLOCKS - 1;
+          const int lowest = i1 < mask.n_sinks ? a.window + p_hi : (mask.from + max(0, i0 - mask.n_sinks)) * OPS_BLOCK;   // of its blocks behind the sinks
+          const int highest = (mask.from + i1 - mask.n_sinks) * OPS_BLOCK + OPS_BLOCK - 1;
+          const bool masked = highest > p_lo || (a.window > 0 && lowest <= p_hi - a.window) || (i0 < mask.n_sinks && (a.sinks & (OPS_BLOCK - 1)));
+          wait(&sh.s_full[s], n_s & 1u);
+          ++n_s;
+          til_fence_after();
+          if (j == t.begin[s]) {
+            const float x = til_max(t_s, masked, mask) * a.qscale;
+            mx_used = x;
+          }
+          uint32_t p[64];
+          float sum;
+#pragma unroll 1
+          while (true) {
+            float mx;
+            const float neg = mx_used == -INFINITY ? 0.f : -mx_used;
+            if (masked) til_probs<true>(t_s, a.qscale, neg, mask, p, mx, sum);
+            else til_probs<false>(t_s, a.qscale, neg, mask, p, mx, sum);
+            mx *= a.qscale;
+            if (!__any_sync(0xffffffffu, mx > mx_used + 8.f)) break;
+            const float top = fmaxf(mx_used, mx);
+            const float f = top == -INFINITY ? 1.f : attn_ex2(mx_used - top);
+            mx_used = top;
+            l *= f;
+            if (j > t.begin[s]) {   // the stream's accumulator is complete: its MMAs came before these scores'
+#pragma unroll 1
+              for (int k = 0; k < HD; k += 64) {
+                uint32_t x[32], y[32];
+                til_ld32(t_o + (uint32_t)k, x);
+                til_ld32(t_o + (uint32_t)k + 32u, y);
+                tmem_wait_ld_til(x, y);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                  x[i] = __float_as_uint(__uint_as_float(x[i]) * f);
+                  y[i] = __float_as_uint(__uint_as_float(y[i]) * f);
+                }
+                til_st32(t_o + (uint32_t)k, x);
+                til_st32(t_o + (uint32_t)k + 32u, y);
+              }
+              til_wait_st();
+            }
+          }
+          l += sum;
+          til_st32(t_s, p);
+          til_st32(t_s + 32u, p + 32);
+          til_wait_st();
+          til_fence_before();
+          __syncwarp();
+          if (lane == 0) til_arrive(&sh.p_full[s]);
+        }
+        if (more) load_q(next);   // (its scores are complete: the queries have been read)
+        wait(&sh.o_full[s], n_o & 1u);
+        ++n_o;
+        til_fence_after();
+        const float inv = l > 0.f ? __fdividef(1.0f, l) : 0.f;
+        const bool store = r < t.live[s] && ok;
+        char* dst = static_cast<char*>(a.out) + ((long long)(t.row + s * P + (store ? r : 0)) * a.out_stride + (t.h * rep + m % rep) * HD) * 2;
+#pragma unroll 1
+        for (int k = 0; k < HD; k += 64) {
+          uint32_t x[32], y[32];
+          til_ld32(t_o + (uint32_t)k, x);
+          til_ld32(t_o + (uint32_t)k + 32u, y);
+          tmem_wait_ld_til(x, y);
+          auto put = [&](const uint32_t(&v)[32], int at) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) {
+              uint32_t o[4];
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {
+                const __nv_bfloat162 b2 = __floats2bfloat162_rn(__uint_as_float(v[i + 2 * c]) * inv, __uint_as_float(v[i + 2 * c + 1]) * inv);
+                o[c] = *reinterpret_cast<const uint32_t*>(&b2);
+              }
+              if (store) *reinterpret_cast<uint4*>(dst + (at + i) * 2) = make_uint4(o[0], o[1], o[2], o[3]);
+            }
+          };
+          put(x, k);
+          put(y, k + 32);
+        }
+        if (more) q_there();
+      } else if (more) {
+        load_q(next);
+        q_there();
+      }
+      t = next;
+      u = un;
+    }
+  } else if (w == 8) {
+    // ---- MMAs ----
+    const uint32_t idesc_s = til_idesc(TIL_KEYS), idesc_o = til_idesc(HD) | (1u << 16);   // (bit 16: B is MN-major)
+    const uint32_t b0 = til_smem(base);
+    uint32_t n_tile = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0};
+    for (int u = blockIdx.x; u < n_units && ok; u += (int)gridDim.x) {
+      const TilUnit t = unit_of(u);
+      const int tiles = tiles_of(t);
+      auto scores = [&](int s, int j) {
+        const uint32_t n = n_tile + (uint32_t)j, slot = n % S::RING;
+        wait(&sh.k_full[slot], (n / S::RING) & 1u);
+        if (!ok) return;
+        til_fence_after();
+        const uint64_t dq = til_desc(b0 + S::Q + s * S::TILE, 16), dk = til_desc(b0 + S::K + slot * S::TILE, 16);
+        if (til_elect()) {
+#pragma unroll
+          for (int i = 0; i < HD / 16; ++i)
+            til_mma(tmem + (uint32_t)s * 128u, dq + (uint64_t)((i >> 2) * 1024 + (i & 3) * 2), dk + (uint64_t)((i >> 2) * 1024 + (i & 3) * 2), idesc_s, i ? 1u : 0u);
+          til_commit(&sh.s_full[s]);
+          if (s == 1 || !takes(t, 1, j)) til_commit(&sh.k_empty[slot]);
+        }
+        __syncwarp();
+      };
+#pragma unroll 1
+      for (int s = 0; s < 2; ++s) {
+        if (!t.live[s]) continue;
+        wait(&sh.q_full[s], n_q[s] & 1u);
+        ++n_q[s];
+        til_fence_after();
+        if (t.begin[s] == 0) scores(s, 0);
+      }
+#pragma unroll 1
+      for (int j = 0; j < tiles && ok; ++j) {
+        const uint32_t n = n_tile + (uint32_t)j, slot = n % S::RING;
+#pragma unroll 1
+        for (int s = 0; s < 2; ++s) {
+          if (takes(t, s, j)) {
+            wait(&sh.p_full[s], n_p[s] & 1u);
+            ++n_p[s];
+            wait(&sh.v_full[slot], (n / S::RING) & 1u);
+            if (!ok) break;
+            til_fence_after();
+            if (til_elect()) {
+#pragma unroll
+              for (int i = 0; i < TIL_BLOCKS; ++i)   // 16 keys each, a block of the cache
+                til_mma_tmem(tmem + 256u + (uint32_t)(s * HD), tmem + (uint32_t)s * 128u + (uint32_t)(i * 8),
+                             til_desc(b0 + S::V + slot * S::TILE + i * (S::TILE / TIL_BLOCKS), 2048), idesc_o, (j > t.begin[s] || i) ? 1u : 0u);
+              if (j + 1 == t.end[s]) til_commit(&sh.o_full[s]);
+              if (s == 1 || !takes(t, 1, j)) til_commit(&sh.v_empty[slot]);
+            }
+            __syncwarp();
+          }
+          if (j + 1 < tiles && takes(t, s, j + 1)) scores(s, j + 1);
+        }
+      }
+      n_tile += (uint32_t)tiles;
+    }
+  } else {
+    // ---- copies ----
+    const int part = w - 9;   // 0, 1: halves of the keys; 2: values
+    if (part == 2 || part < S::SLABS) {
+      uint64_t policy;
+      asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
+      const CUtensorMap* map = part == 2 ? &value_map : &key_map;
+      const int rows_block = a.pool.Hkv * OPS_BLOCK, none = (int)a.pool.n_blocks * rows_block;   // (a row behind the pool: zeros)
+      uint32_t n_tile = 0, n_land = 0;
+      for (int u = blockIdx.x; u < n_units && ok; u += (int)gridDim.x) {
+        const TilUnit t = unit_of(u);
+        const int tiles = tiles_of(t);
+        const int32_t* table = a.table + (long long)t.req * a.stride;
+        auto block_id = [&](int j) {   // lane: block of the tile; behind the list the last one again (nobody sees it there)
+          const int i = min(j * TIL_BLOCKS + (lane & 7), t.span.n - 1);
+          return t.last >= 0 ? table[i < t.span.sinks ? i : t.span.from + i - t.span.sinks] : -1;
+        };
+        int id = block_id(0);
+#pragma unroll 1
+        for (int j = 0; j < tiles; ++j) {
+          const int mine = (unsigned)id < (unsigned)a.pool.n_blocks ? id * rows_block + t.h * OPS_BLOCK : none;
+          if (j + 1 < tiles) id = block_id(j + 1);
+          const uint32_t n = n_tile + (uint32_t)j, slot = n % S::RING, use = n / S::RING;
+          uint64_t* empty = part == 2 ? &sh.v_empty[slot] : &sh.k_empty[slot];
+          if (use > 0) wait(empty, (use - 1u) & 1u);
+          if (!ok) break;
+          const uint32_t dst = til_smem(base) + (part == 2 ? S::V : S::K + part * 16384) + slot * S::TILE;
+          bool clean = true;   // some row sees every key of the tile, so that its values are numbers
+          if (part == 2) {
+            const int i0 = j * TIL_BLOCKS, i1 = i0 + TIL_BLOCKS - 1;
+            clean = t.last >= (t.span.from + i1 - t.span.sinks) * OPS_BLOCK + OPS_BLOCK - 1 && !(i0 < t.span.sinks && (a.sinks & (OPS_BLOCK - 1))) &&
+                    !(a.window > 0 && i1 >= t.span.sinks && (t.span.from + max(0, i0 - t.span.sinks)) * OPS_BLOCK <= t.pos - a.window);
+          }
+          uint64_t* full = part < 2 ? &sh.k_full[slot] : clean ? &sh.v_full[slot] : &sh.v_land;
+          if (til_elect()) til_expect(full, part < 2 ? 16384u : (uint32_t)S::TILE);
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < TIL_BLOCKS; ++i) {
+            const int row = (int)til_uniform((uint32_t)__shfl_sync(0xffffffffu, mine, i));
+            if (til_elect()) til_copy(dst + i * (part < 2 ? 2048 : S::TILE / TIL_BLOCKS), map, row, part < 2 ? part : 0, part == 2, full, policy);
+            __syncwarp();
+          }
+          if (part == 2 && !clean) {   // what no row sees may be anything, and 0 x NaN is not 0
+            wait(&sh.v_land, n_land & 1u);
+            ++n_land;
+            char* v = base + S::V + slot * S::TILE;
+#pragma unroll 1
+            for (int x = 0; x < TIL_KEYS; ++x) {
+              const int i = j * TIL_BLOCKS + x / OPS_BLOCK;
+              const int at = (i < t.span.sinks ? i : t.span.from + i - t.span.sinks) * OPS_BLOCK + x % OPS_BLOCK;
+              if (at <= t.last && (a.window == 0 || at > t.pos - a.window || at < a.sinks)) continue;
+              if (lane < HD / 8)
+                *reinterpret_cast<uint4*>(v + (x / OPS_BLOCK) * (S::TILE / TIL_BLOCKS) + (lane >> 3) * 2048 + (x % OPS_BLOCK) * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+            }
+            til_proxy_fence();
+            __syncwarp();
+            if (lane == 0) til_arrive(&sh.v_full[slot]);
+          }
+        }
+        n_tile += (uint32_t)tiles;
+      }
+    }
+  }
+  // copies that are still on their way after a wait has run out land before the shared memory is given up
+  if (!ok) {
+    const long long t0 = clock64();
+    while (clock64() - t0 < 200000ll) {}
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  til_fence_before();
+  __syncthreads();
+  if (w == 8) {
+    til_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+  asm volatile("griddepcontrol.wait;" ::: "memory");   // the kernels before it in the call may still run; this one is not done before they are
+}
+
+typedef CUresult (*TilEncode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                              CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+static TilEncode til_encode() {
+  static const TilEncode f = [] {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult how;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &how) != cudaSuccess || how != cudaDriverEntryPointSuccess) return (TilEncode) nullptr;
+    return reinterpret_cast<TilEncode>(fn);
+  }();
+  return f;
+}
+
+template <int HD>
+static int tiles_run(const AttnArgs& a, int sms, int64_t most_units, void* stream) {
+  using S = TilShape<HD>;
+  const TilEncode encode = til_encode();
+  if (!encode) return BLINK_ECUDA;
+  // the layer's keys and values as {64 dims, rows of a head's block, halves, keys | values}; a copy brings 16 keys, of one half (keys) or both (values)
+  const cuuint64_t rows = (cuuint64_t)a.pool.n_blocks * a.pool.Hkv * OPS_BLOCK;
+  const cuuint64_t dims[4] = {64, rows, HD / 64, 2}, strides[3] = {HD * 2, 128, rows * HD * 2};
+  const cuuint32_t key_box[4] = {64, OPS_BLOCK, 1, 1}, value_box[4] = {64, OPS_BLOCK, HD / 64, 1}, one[4] = {1, 1, 1, 1};
+  CUtensorMap maps[2];
+  for (int i = 0; i < 2; ++i)
+    if (encode(&maps[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, a.pool.k, dims, strides, i ? value_box : key_box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return BLINK_ECUDA;
+  const size_t smem = (size_t)S::END + 1024 + (size_t)(a.n + 1) * 4;
+  const int64_t grid = most_units < sms ? most_units : sms;
+  return ops_launch(blink_attn_tiles_kernel<HD>, grid, TIL_THREADS, smem, stream, 0, true, a, maps[0], maps[1]);
+}
+
+int attn_tiles(const AttnArgs& a, int sms, void* stream) {
+  const int64_t most_units = ((int64_t)a.rows * a.pool.rep / 256 + a.n) * a.pool.Hkv;
+  return a.pool.hd == 128 ? tiles_run<128>(a, sms, most_units, stream) : tiles_run<64>(a, sms, most_units, stream);
+}
+
+}  // namespace blink
