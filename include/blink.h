@@ -449,7 +449,7 @@ int blink_window_attention(const blink_model_cfg* model, const blink_kv_pool* kv
                            void* stream);
 
 /* Bytes of workspace that blink_verify_drafts needs (0: bad argument). */
-uint64_t blink_verify_workspace(int rows, int vocab);
+uint64_t blink_verify_workspace(int rows, int n_requests, int vocab);
 
 /* Verification of drafted tokens.  Request r has the logits rows row_start[r] .. row_start[r + 1] - 1: one for each of its k drafted
  * tokens draft_tokens[row], and one more.  With p = softmax(logits / temperature[r]) of row i and q = draft_probs of row i (NULL: all of

@@ -159,7 +159,7 @@ def lib():
     L.blink_window_attention.restype = I
     L.blink_window_attention.argtypes = [V, V, I, V, I64, I, V, V, I, V, I, I, I, I, V, I64, V, U64, V]
     L.blink_verify_workspace.restype = U64
-    L.blink_verify_workspace.argtypes = [I, I]
+    L.blink_verify_workspace.argtypes = [I, I, I]
     L.blink_verify_drafts.restype = I
     L.blink_verify_drafts.argtypes = [V, I64, I, I, V, I, V, V, I64, V, V, V, V, V, V, U64, V]
     L.blink_strerror.restype = C.c_char_p
@@ -341,8 +341,8 @@ def blink_window_attention(m, kv_pool, layer: int, q, row_start, kv_len, block_t
     return out
 
 
-def blink_verify_workspace(rows: int, vocab: int) -> int:
-    return int(lib().blink_verify_workspace(rows, vocab))
+def blink_verify_workspace(rows: int, n_requests: int, vocab: int) -> int:
+    return int(lib().blink_verify_workspace(rows, n_requests, vocab))
 
 
 def blink_verify_drafts(logits, row_start, draft_tokens, draft_probs, temperature, u_accept, u_pick, out_tokens=None, n_accepted=None,

@@ -234,7 +234,7 @@ PyObject* verify_drafts(PyObject*, PyObject* const* arg, Py_ssize_t nargs) {
   if (!a.ok) return nullptr;
   at::Tensor mine;
   if (!given) {
-    mine = make({(int64_t)blink_verify_workspace((int)rows, (int)vocab)}, at::kByte, a);
+    mine = make({(int64_t)blink_verify_workspace((int)rows, (int)n, (int)vocab)}, at::kByte, a);
     given = &mine;
   }
   return call(a, [&](void* stream) {

@@ -26,6 +26,7 @@ namespace blink {
 constexpr int FEW_WARPS = 4, FEW_THREADS = FEW_WARPS * 32;
 constexpr int FEW_MAX_CTAS = 640;    // of a launch; the records are laid out for so many
 constexpr int FEW_MIN_TILES = 4;     // of a CTA's run, while there are any
+constexpr int FEW_UNIT_TILES = 4;    // what a unit costs beside its tiles, in tiles
 constexpr int JOIN_THREADS = 256;
 
 // What the join needs of a unit that was cut, written by the CTA in whose run it begins.
@@ -62,9 +63,11 @@ struct FewBf16 {
   uint32_t q[NT][CH][4];
   float acc[NT][U][4][4], m[NT][2], l[NT][2];
   int pos[NT][2];
+  int live;   // instructions' worth of rows in use
 
   __device__ __forceinline__ void begin(const AttnArgs& a, const AttnReq& r, int h, int m0, int m1) {
     const int g = (threadIdx.x & 31) >> 2, c = threadIdx.x & 3, rep = a.pool.rep;
+    live = (m1 - m0 + 7) / 8;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int mq = m0 + nt * 8 + g;
@@ -94,6 +97,20 @@ struct FewBf16 {
   // Block b of the request; k, v: its keys and values of this head, null: zeros.  edge: some row does not see all of it; first, last: positions
   // of the first and the last row.
   __device__ __forceinline__ void tile(const AttnArgs& a, int b, const char* k, const char* v, bool edge, int first, int last) {
+    if constexpr (NT >= 4) {
+      if (live == 4) return tile_of<4>(a, b, k, v, edge, first, last);
+    }
+    if constexpr (NT >= 3) {
+      if (live == 3) return tile_of<3>(a, b, k, v, edge, first, last);
+    }
+    if constexpr (NT >= 2) {
+      if (live == 2) return tile_of<2>(a, b, k, v, edge, first, last);
+    }
+    tile_of<1>(a, b, k, v, edge, first, last);
+  }
+  // (code of its own for each number of instructions that a unit's rows take: conditions around them cost registers, and spills)
+  template <int LIVE>
+  __device__ __forceinline__ void tile_of(const AttnArgs& a, int b, const char* k, const char* v, bool edge, int first, int last) {
     const int g = (threadIdx.x & 31) >> 2, c = threadIdx.x & 3;
     uint4 kk[2][CH], vv[U][4];
     const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
@@ -105,9 +122,9 @@ struct FewBf16 {
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int i = 0; i < 4; ++i) vv[u][i] = v ? few_ld(v + (2 * c + (i & 1) + 8 * (i >> 1)) * (HD * 2) + u * 128 + g * 16) : zero;
-    float s[NT][4];
+    float s[LIVE][4];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
+    for (int nt = 0; nt < LIVE; ++nt) {
       s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
 #pragma unroll
       for (int x = 0; x < CH; ++x) {
@@ -118,7 +135,7 @@ struct FewBf16 {
     const int key = b * OPS_BLOCK + g;
     bool grown = false;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int nt = 0; nt < LIVE; ++nt)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {   // i: key g + 8 * (i / 2), row 2 c + i % 2
         s[nt][i] *= a.qscale;
@@ -127,7 +144,7 @@ struct FewBf16 {
       }
     if (__any_sync(0xffffffffu, grown)) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+      for (int nt = 0; nt < LIVE; ++nt)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           float x = fmaxf(s[nt][i], s[nt][i + 2]);
@@ -146,9 +163,9 @@ struct FewBf16 {
             }
         }
     }
-    uint32_t p[NT][2];
+    uint32_t p[LIVE][2];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
+    for (int nt = 0; nt < LIVE; ++nt) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         s[nt][i] = attn_ex2(s[nt][i] - (m[nt][i & 1] == -INFINITY ? 0.f : m[nt][i & 1]));
@@ -181,7 +198,7 @@ struct FewBf16 {
         const uint32_t a0 = __byte_perm(x[0], x[1], 0x5410), a1 = __byte_perm(x[0], x[1], 0x7632), a2 = __byte_perm(x[2], x[3], 0x5410),
                        a3 = __byte_perm(x[2], x[3], 0x7632);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) few_mma(acc[nt][u][t], a0, a1, a2, a3, p[nt][0], p[nt][1]);
+        for (int nt = 0; nt < LIVE; ++nt) few_mma(acc[nt][u][t], a0, a1, a2, a3, p[nt][0], p[nt][1]);
       }
   }
 
@@ -324,7 +341,8 @@ __device__ __forceinline__ void few_store(__nv_bfloat16* p, float4 x) {
 __device__ __forceinline__ void few_store(float* p, float4 x) { *reinterpret_cast<float4*>(p) = x; }
 
 // Groups of MR rows of a request, and tiles of each (the same number for all of them, so that a place in the sequence is found by division;
-// a group that has fewer leaves the rest out).
+// a group that has fewer leaves the rest out).  A unit's start and end cost as much as some tiles and count as such, behind its
+// tiles: without them CTAs that got many short units were the last (200 rows of 20 to 5000 keys: 148 us, 92 with them).
 struct FewShape {
   int groups, tiles;
 };
@@ -333,10 +351,10 @@ __device__ __forceinline__ FewShape few_shape(const AttnArgs& a, const AttnReq& 
   if (r.rows == 0 || r.rows > a.few) return {0, 0};
   const long long m = (long long)r.rows * a.pool.rep;
   const int groups = (int)((m + MR - 1) / MR), last = r.ctx + r.rows - 1;
-  if (groups == 1) return {1, attn_span(a, r.ctx, last).n};
+  if (groups == 1) return {1, attn_span(a, r.ctx, last).n + FEW_UNIT_TILES};
   int tiles = attn_span(a, r.ctx, last).n;   // every group's are among these
   if (a.window > 0) tiles = min(tiles, (a.sinks + OPS_BLOCK - 1) / OPS_BLOCK + (int)min(0x7ffff000ll, (long long)a.window + MR / a.pool.rep + 1) / OPS_BLOCK + 2);
-  return {groups, tiles};
+  return {groups, tiles + FEW_UNIT_TILES};
 }
 
 template <typename T, int HD, typename W, int CTAS>
@@ -409,6 +427,10 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) blink_attn_few_kernel(const
     const int first = req.ctx + m0 / a.pool.rep, last = req.ctx + (m1 - 1) / a.pool.rep;
     const AttnSpan span = attn_span(a, first, last);
     const int stop = min(t1, span.n);
+    if (t0 >= span.n) {   // nothing of it is left
+      at += t1 - t0;
+      continue;
+    }
     const int32_t* table = a.table + (long long)r * a.stride;
 
     auto block_of = [&](int t) { return t < span.sinks ? t : span.from + t - span.sinks; };
@@ -431,7 +453,7 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) blink_attn_few_kernel(const
     __syncthreads();   // (what was left there for the segment before has been read)
     w.leave(s_acc + warp * MR * PITCH, s_ml + warp * MR);
     __syncthreads();
-    const bool whole = t0 == 0 && t1 == shape.tiles;
+    const bool whole = t0 == 0 && t1 >= span.n;
     const size_t rec = 2 * blockIdx.x + (t0 == 0 ? 1 : 0);
     float2* rec_ml = reinterpret_cast<float2*>(a.ws + few_ml_at()) + rec * MR;
     float* rec_acc = reinterpret_cast<float*>(a.ws + few_acc_at(MR)) + rec * MR * HD;
@@ -459,7 +481,7 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) blink_attn_few_kernel(const
         if (d == 0) rec_ml[row] = make_float2(M, L);
       }
     }
-    if (t0 == 0 && !whole) cut = FewCut{(int)((at + shape.tiles - 1) / per) - (int)blockIdx.x + 1, req.start, m0, m1, h};
+    if (t0 == 0 && !whole) cut = FewCut{(int)((at + span.n - 1) / per) - (int)blockIdx.x + 1, req.start, m0, m1, h};
     at += t1 - t0;
   }
   if (tid == 0) reinterpret_cast<FewCut*>(a.ws + ATTN_STATUS_BYTES)[blockIdx.x] = cut;

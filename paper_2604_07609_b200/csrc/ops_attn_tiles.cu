@@ -590,12 +590,13 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
             ++n_land;
             char* v = base + S::V + slot * S::TILE;
 #pragma unroll 1
-            for (int x = 0; x < TIL_KEYS; ++x) {
+            for (int x = lane; x < TIL_KEYS; x += 32) {
               const int i = j * TIL_BLOCKS + x / OPS_BLOCK;
               const int at = (i < t.span.sinks ? i : t.span.from + i - t.span.sinks) * OPS_BLOCK + x % OPS_BLOCK;
               if (at <= t.last && (a.window == 0 || at > t.pos - a.window || at < a.sinks)) continue;
-              if (lane < HD / 8)
-                *reinterpret_cast<uint4*>(v + (x / OPS_BLOCK) * (S::TILE / TIL_BLOCKS) + (lane >> 3) * 2048 + (x % OPS_BLOCK) * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+              char* to = v + (x / OPS_BLOCK) * (S::TILE / TIL_BLOCKS) + (x % OPS_BLOCK) * 128;
+#pragma unroll
+              for (int c = 0; c < HD / 8; ++c) *reinterpret_cast<uint4*>(to + (c >> 3) * 2048 + ((c + lane) & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
             }
             til_proxy_fence();
             __syncwarp();

@@ -4,29 +4,40 @@
 //   first refused i: a token from max(0, p_i - q_i), none refused: from p of the last row; by the inverse of its running sum in the order of
 //   the indexes: the first j with sum_{<= j} > v * sum
 //
-// Two kernels.  (1) Largest value, its index and the sum of exponentials of pieces of 1024 entries of every row, a warp each: one pass over
-// the logits, which is what bounds the whole (HBM: 4 bytes an entry).  A lane has its 32 entries on their way at once, and sums against its own
-// largest, so that nothing waits for another warp.  Exponentials in 32 bits, sums of a lane's entries in 32, everything above in 64: the
-// acceptance test is off by some 1e-8.  (2) A cluster of 16 CTAs a request: pieces become rows, the first refused draft is found, and
-// its row alone is drawn from.  That row's sums decide between neighbours that are as close as 1e-6, so its exponentials, sums and the running
-// sum are in 64 bits; a thread keeps its 16 of them in registers, and sums go from CTA to CTA through distributed shared memory.  Sums
-// are taken in an order that sizes alone fix: the same call gives the same token.
-#include <cooperative_groups.h>
-
-#include <utility>
+// Four kernels, each waiting for the one before it only where it needs its results.
+//   rows    largest value and sum of exponentials of pieces of 1024 entries of every row, a warp each: one pass over the logits, which is what
+//           bounds the whole (HBM: 4 bytes an entry).  A lane has its 32 entries on their way at once and sums against its own largest
+//           value, so that nothing waits for another warp.  Exponentials in 32 bits, sums of a lane's entries in 32, everything above in
+//           64: the acceptance test is off by some 1e-8.
+//   choose  a CTA per request: the first refused draft, from the pieces
+//   sums    the exponentials of that row, 256 entries a warp
+//   draw    the same entries once more: weights max(0, p - q) and their sum per warp; the last CTA of a request to come finds the run of 256 in
+//           which the running sum passes its target, and goes over that run again
+// The chosen row's sums decide between neighbours that are as close as 1e-6, so its exponentials, sums and running sum are in 64 bits.  Sums are
+// taken in an order that sizes alone fix, whoever comes last: the same call gives the same token.
+#include <cmath>
 
 #include "ops.h"
 
 namespace blink {
 
-constexpr int VER_WARPS = 8, VER_EACH = 32, VER_CHUNK = 32 * VER_EACH;                             // (1): entries of a lane, of a warp
-constexpr int PICK_THREADS = 512, PICK_WARPS = 16, PICK_CTAS = 16;   // (2)
-constexpr int PICK_ROWS = 64;   // rows of a request whose largest values are kept until it is known which one is drawn from
+constexpr int VER_WARPS = 8, VER_THREADS = VER_WARPS * 32;
+constexpr int VER_EACH = 32, VER_CHUNK = 32 * VER_EACH;   // rows: entries of a lane, a warp
+constexpr int VER_FEW = 8, VER_RUN = 32 * VER_FEW, VER_PART = VER_WARPS * VER_RUN;            // sums, draw
 
 struct VerChunk {
   double sum;   // of exp((z - max) / T)
   float max;
-  int index;    // first of the largest
+  int index;    // first of the largest, where that may matter (see ver_one)
+};
+struct VerChoice {
+  int row;      // that is drawn from; -1: none, or one that stands for its largest entry alone
+  int refused;  // a draft of it was
+  float max;
+  int unused;
+};
+struct VerRun {
+  double rest, all;   // sums over a warp's run: of the weights, and of p
 };
 
 struct VerifyArgs {
@@ -37,12 +48,37 @@ struct VerifyArgs {
   const float *temperature, *u_accept, *u_pick;
   int32_t *tokens, *accepted;
   VerChunk* chunks_of;   // [rows][chunks]
-  int n, rows, vocab, chunks;
+  double* sums;          // [n][parts]
+  VerRun* runs;          // [n][parts * VER_WARPS], and behind them the same for whole parts, [n][parts]
+  VerRun* part_runs;
+  VerChoice* choice;     // [n]
+  unsigned* arrived;     // [n]
+  int n, rows, vocab, chunks, groups, parts;
   bool vec, probs_vec;   // rows on 16-byte boundaries
 };
 
 // No number: as if the entry were not there.
 __device__ __forceinline__ float ver_entry(float z) { return z == z ? z : -INFINITY; }
+
+__device__ __forceinline__ float ver_ex2(float x) {
+  float y;
+  asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float2 ver_add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 ver_mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
 
 // The larger of two, of equal ones that of the lower index.
 __device__ __forceinline__ void ver_larger(float& m, int& i, float m2, int i2) {
@@ -66,51 +102,73 @@ __device__ __forceinline__ void ver_load(float (&v)[EACH], const float* z, int n
   }
 }
 
-__global__ void __launch_bounds__(VER_WARPS * 32) blink_verify_rows_kernel(const VerifyArgs a) {
+// At a temperature that is not above 0 and finite a row stands for its largest entry alone; so does one whose largest entry is infinite, or that
+// holds no number.
+__device__ __forceinline__ bool ver_one(float T, float m) { return !(T > 0.f && T < INFINITY) || !(m > -INFINITY) || !(m < INFINITY); }
+
+__global__ void __launch_bounds__(VER_THREADS) blink_verify_rows_kernel(const VerifyArgs a) {
   __shared__ int s_req;
+  __shared__ float s_T;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int groups = (a.chunks + VER_WARPS - 1) / VER_WARPS;
-  const int row = (int)(blockIdx.x / (unsigned)groups), chunk = (int)(blockIdx.x - (unsigned)row * groups) * VER_WARPS + warp;
+  const int row = (int)(blockIdx.x / (unsigned)a.groups), chunk = (int)(blockIdx.x - (unsigned)row * a.groups) * VER_WARPS + warp;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (the second kernel waits for the whole of this one itself)
   float v[VER_EACH];
   if (chunk < a.chunks)
     ver_load(v, a.logits + row * a.logits_stride + (long long)chunk * VER_CHUNK, min(VER_CHUNK, a.vocab - chunk * VER_CHUNK), a.vec, -INFINITY);
   if (threadIdx.x == 0) s_req = -1;
   __syncthreads();
-  for (int r = threadIdx.x; r < a.n; r += VER_WARPS * 32)
-    if (a.row_start[r] <= row && row < a.row_start[r + 1]) s_req = r;
+  for (int r = threadIdx.x; r < a.n; r += VER_THREADS) {
+    const int first = a.row_start[r];
+    if (first <= row && row < a.row_start[r + 1]) {
+      s_req = r;
+      s_T = a.temperature[r];
+      if (first == row && chunk < VER_WARPS) a.arrived[r] = 0u;   // for the draw
+    }
+  }
   __syncthreads();
   const int req = s_req;
   if (req < 0 || chunk >= a.chunks) return;   // (whole warps) a row behind the last request
-  const float T = a.temperature[req];
-  float m = -INFINITY;
+  const float T = s_T;
+  float m0 = -INFINITY, m1 = -INFINITY;   // (the larger of a number and none is the number)
 #pragma unroll
-  for (int k = 0; k < VER_EACH; ++k) {
-    v[k] = ver_entry(v[k]);
-    m = fmaxf(m, v[k]);
+  for (int k = 0; k < VER_EACH; k += 4) {
+    m0 = fmaxf(fmaxf(m0, v[k]), v[k + 1]);
+    m1 = fmaxf(fmaxf(m1, v[k + 2]), v[k + 3]);
   }
-  int idx = 0;
+  const float mine = fmaxf(m0, m1);
+  float m = mine;
 #pragma unroll
-  for (int k = VER_EACH - 1; k >= 0; --k)
-    if (v[k] == m) idx = (k >> 2) * 128 + lane * 4 + (k & 3);
-  const float mine = m;
-#pragma unroll
-  for (int d = 16; d; d >>= 1) {
-    const float m2 = __shfl_xor_sync(0xffffffffu, m, d);
-    const int i2 = __shfl_xor_sync(0xffffffffu, idx, d);
-    ver_larger(m, idx, m2, i2);
-  }
+  for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
   double sum = 0.0;
-  if (T > 0.f && T < INFINITY && m > -INFINITY && m < INFINITY) {
+  int idx = 0;
+  if (ver_one(T, m)) {
+    idx = 0x7fffffff;
+#pragma unroll
+    for (int k = VER_EACH - 1; k >= 0; --k)
+      if (ver_entry(v[k]) == m) idx = (k >> 2) * 128 + lane * 4 + (k & 3);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) idx = min(idx, __shfl_xor_sync(0xffffffffu, idx, d));
+  } else {
     const float scale = fminf(1.4426950408889634f / T, 3e38f);
     const float base = mine == -INFINITY ? 0.f : mine;
-    float s0 = 0.f, s1 = 0.f;
+    const float2 scale2 = make_float2(scale, scale), base2 = make_float2(-base, -base);
+    auto lane_sum = [&]() {
+      float2 s0 = make_float2(0.f, 0.f), s1 = s0;
 #pragma unroll
-    for (int k = 0; k < VER_EACH; k += 2) {   // (no entry: exp2(-inf))
-      s0 += exp2f((v[k] - base) * scale);
-      s1 += exp2f((v[k + 1] - base) * scale);
+      for (int k = 0; k < VER_EACH; k += 4) {   // (no entry: 2^-inf)
+        const float2 x = ver_mul2(ver_add2(make_float2(v[k], v[k + 1]), base2), scale2), y = ver_mul2(ver_add2(make_float2(v[k + 2], v[k + 3]), base2), scale2);
+        s0 = ver_add2(s0, make_float2(ver_ex2(x.x), ver_ex2(x.y)));
+        s1 = ver_add2(s1, make_float2(ver_ex2(y.x), ver_ex2(y.y)));
+      }
+      return (s0.x + s0.y) + (s1.x + s1.y);
+    };
+    float s = lane_sum();
+    if (s != s) {   // an entry that is no number
+#pragma unroll
+      for (int k = 0; k < VER_EACH; ++k) v[k] = ver_entry(v[k]);
+      s = lane_sum();
     }
-    sum = (double)(s0 + s1) * (double)exp2f((mine - m) * scale);
+    sum = (double)s * (double)ver_ex2((mine - m) * scale);
 #pragma unroll
     for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
   }
@@ -131,52 +189,25 @@ __device__ __forceinline__ double ver_exp2(double t) {
   return t > -1020.0 ? __hiloint2double(__double2hiint(p) + (n << 20), __double2loint(p)) : 0.0;
 }
 
-// The first of 16 parts (a lane each, lanes 16 .. 31 have 0) whose running sum exceeds target, else the last with anything in it; `base` grows by
-// what stands before it.
-__device__ __forceinline__ int ver_part(double part, double target, double& base) {
-  const int lane = threadIdx.x & 31;
-  double c = part;
-#pragma unroll
-  for (int d = 1; d < 16; d <<= 1) {
-    const double u = __shfl_up_sync(0xffffffffu, c, d);
-    if (lane >= d) c += u;
-  }
-  const unsigned hit = __ballot_sync(0xffffffffu, part > 0.0 && base + c > target), any = __ballot_sync(0xffffffffu, part > 0.0);
-  const int at = hit ? __ffs(hit) - 1 : any ? 31 - __clz(any) : 0;
-  const double before = __shfl_sync(0xffffffffu, c, max(at - 1, 0));
-  if (at > 0) base += before;
-  return at;
+// The request's rows, first and behind the last.
+__device__ __forceinline__ int2 ver_rows(const VerifyArgs& a, int req) {
+  const int start = min(max(a.row_start[req], 0), a.rows);
+  return make_int2(start, min(max(a.row_start[req + 1], start), a.rows));
 }
 
-// EACH: entries of a lane at a time.
-template <int EACH>
-__global__ void __launch_bounds__(PICK_THREADS, 2) blink_verify_pick_kernel(const VerifyArgs a) {
-  namespace cg = cooperative_groups;
-  constexpr int TILE = 32 * EACH;
-  cg::cluster_group cluster = cg::this_cluster();
-  __shared__ __align__(16) float s_q[PICK_WARPS][TILE];   // a tile of q per warp, each lane's own entries
-  __shared__ double s_part[PICK_WARPS];                   // a sum per warp
-  __shared__ double s_all[2][PICK_CTAS];                  // a sum per CTA, the same in all of them
-  __shared__ int s_first, s_one[PICK_ROWS], s_index[PICK_ROWS];
-  __shared__ float s_max[PICK_ROWS];
+__global__ void __launch_bounds__(VER_THREADS) blink_verify_choose_kernel(const VerifyArgs a) {
+  __shared__ int s_first;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int rank = (int)cluster.block_rank(), req = (int)(blockIdx.x / PICK_CTAS);
-  const int V = a.vocab;
+  const int req = (int)blockIdx.x;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   // (all but the pieces is there before the first kernel is done)
-  const int start = min(max(a.row_start[req], 0), a.rows), end = min(max(a.row_start[req + 1], start), a.rows);
-  const int k = end - start - 1;
+  const int2 rows = ver_rows(a, req);
+  const int start = rows.x, k = rows.y - rows.x - 1;
   const float T = a.temperature[req];
   const double to_exp2 = 1.44269504088896340736 / (double)T;
-  if (tid == 0) s_first = k;
+  if (tid == 0) s_first = max(k, 0);
   __syncthreads();
-  if (start == end) {   // (the whole cluster; not before the first kernel, or the next one in the stream could be)
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (rank == 0 && tid == 0) a.accepted[req] = 0;
-    return;
-  }
-
-  // A row from its pieces: largest value, its index, sum.  A row with an infinite largest value or without any number, and every
-  // row at a T that is not above 0 and finite, stands for its largest entry alone.
+  // A row from its pieces: largest value, its index, sum.
   auto row_of = [&](int row, float& m, int& idx, double& sum, bool with_sum) {
     const VerChunk* c = a.chunks_of + (size_t)row * a.chunks;
     m = -INFINITY;
@@ -189,7 +220,7 @@ __global__ void __launch_bounds__(PICK_THREADS, 2) blink_verify_pick_kernel(cons
       const int i2 = __shfl_xor_sync(0xffffffffu, idx, d);
       ver_larger(m, idx, m2, i2);
     }
-    const bool one = !(T > 0.f && T < INFINITY) || !(m > -INFINITY) || !(m < INFINITY);
+    const bool one = ver_one(T, m);
     sum = 0.0;
     if (!one && with_sum) {
 #pragma unroll 4
@@ -199,228 +230,264 @@ __global__ void __launch_bounds__(PICK_THREADS, 2) blink_verify_pick_kernel(cons
     }
     return one;
   };
-  for (int i = warp; i <= k; i += PICK_WARPS) {   // (row k: no draft)
+  bool waited = false;
+  for (int i = warp; i < k; i += VER_WARPS) {
     float m;
     int idx;
     double sum;
-    const int row = start + i, x = i < k ? a.draft[row] : -1;
-    const bool in = x >= 0 && x < V;
+    const int row = start + i, x = a.draft[row];
+    const bool in = x >= 0 && x < a.vocab;
     const float z = in ? ver_entry(__ldcg(a.logits + row * a.logits_stride + x)) : -INFINITY, q = in && a.probs ? a.probs[row * a.probs_stride + x] : 1.f;
     const float u = a.u_accept[row];
-    if (i == warp) asm volatile("griddepcontrol.wait;" ::: "memory");
-    const bool one = row_of(row, m, idx, sum, i < k);
-    const bool ok = i == k || (one ? x == idx : in && (double)u * (double)q * sum < ver_exp2(((double)z - (double)m) * to_exp2));
-    if (lane == 0) {
-      if (i < PICK_ROWS) {
-        s_one[i] = one;
-        s_max[i] = m;
-        s_index[i] = idx;
-      }
-      if (!ok) atomicMin(&s_first, i);
-    }
+    if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
+    waited = true;
+    const bool one = row_of(row, m, idx, sum, true);
+    const bool ok = one ? x == idx : in && (double)u * (double)q * sum < ver_exp2(((double)z - (double)m) * to_exp2);
+    if (lane == 0 && !ok) atomicMin(&s_first, i);
   }
-  if (warp > k) asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
   __syncthreads();
   const int acc = s_first, row = start + acc;
-  // the row's entries: a run of tiles per warp, in the order of CTAs, warps and tiles
-  const int tiles = (V + PICK_CTAS * PICK_WARPS * TILE - 1) / (PICK_CTAS * PICK_WARPS * TILE);
-  const int w0 = (rank * PICK_WARPS + warp) * tiles * TILE;
-  const float* z = a.logits + row * a.logits_stride;
-  const float* q = acc < k && a.probs ? a.probs + row * a.probs_stride : nullptr;
-  float zv[EACH];   // of the warp's first tile
-  ver_load(zv, z + w0, V - w0, a.vec, -INFINITY);
-  auto fetch_q = [&](int at) {
-#pragma unroll
-    for (int g = 0; g < EACH / 4; ++g) {
-      const int o = g * 128 + lane * 4;
-      const uint32_t dst = (uint32_t)__cvta_generic_to_shared(&s_q[warp][o]);
-      if (a.probs_vec && at + o + 4 <= V) {
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(q + at + o) : "memory");
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (at + o + j < V) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + 4 * j), "l"(q + at + o + j) : "memory");
-      }
+  if (k < 0) {   // a request without rows
+    if (tid == 0) {
+      a.accepted[req] = 0;
+      a.choice[req].row = -1;
     }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
-  if (q) fetch_q(w0);
-  if (rank == 0) {
-    if (tid == 0) a.accepted[req] = acc;
-    for (int i = tid; i <= k; i += PICK_THREADS)
-      if (i != acc) a.tokens[start + i] = i < acc ? a.draft[start + i] : -1;
-  }
-  float top;
-  int index;
-  bool one;
-  if (acc < PICK_ROWS) {
-    top = s_max[acc];
-    index = s_index[acc];
-    one = s_one[acc] != 0;
-  } else {
-    double sum;
-    one = row_of(row, top, index, sum, false);
-  }
-  if (one) {
-    if (rank == 0 && tid == 0) a.tokens[row] = index;
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
     return;
   }
-  cg::cluster_group::arrival_token there = cluster.barrier_arrive();   // all CTAs have to be there before they are written to
-
-  const double m = (double)top;
-  double e[EACH];
-  auto exps = [&]() {
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) e[i] = ver_exp2(((double)ver_entry(zv[i]) - m) * to_exp2);
-  };
-  auto lane_sum = [&]() {
-    double s = 0.0;
-#pragma unroll
-    for (int i = 0; i < EACH; i += 4) s += (e[i] + e[i + 1]) + (e[i + 2] + e[i + 3]);
-    return s;
-  };
-  // sum over the lanes -> over the CTA -> over the cluster; s_part keeps the warps', s_all the CTAs'
-  auto sum_all = [&](double s, int which) {
-#pragma unroll
-    for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-    if (lane == 0) s_part[warp] = s;
-    __syncthreads();
-    if (warp == 0) {
-      double t = s_part[lane & 15];
-#pragma unroll
-      for (int d = 8; d; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
-      if (lane < PICK_CTAS) *cluster.map_shared_rank(&s_all[which][rank], lane) = t;
+  if (warp == 0) {
+    float top;
+    int index;
+    double unused;
+    const bool one = row_of(row, top, index, unused, false);
+    if (lane == 0) {
+      a.accepted[req] = acc;
+      a.choice[req] = VerChoice{one ? -1 : row, acc < k, top, 0};
+      if (one) a.tokens[row] = index;
     }
-    cluster.sync();
-    double t = s_all[which][lane & 15];
-#pragma unroll
-    for (int d = 8; d; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
-    return t;
-  };
-  auto load_more = [&](int t) {   // tiles behind the first are read again in every pass
-    const int at = w0 + t * TILE;
-    ver_load(zv, z + at, V - at, a.vec, -INFINITY);
-    if (q) fetch_q(at);
-  };
+  }
+  for (int i = tid; i <= k; i += VER_THREADS)
+    if (i != acc) a.tokens[start + i] = i < acc ? a.draft[start + i] : -1;
+}
+
+__global__ void __launch_bounds__(VER_THREADS) blink_verify_sums_kernel(const VerifyArgs a) {
+  __shared__ double s_part[VER_WARPS];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int req = (int)(blockIdx.x / (unsigned)a.parts), part = (int)(blockIdx.x - (unsigned)req * a.parts);
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const double to_exp2 = 1.44269504088896340736 / (double)a.temperature[req];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const VerChoice c = a.choice[req];
+  if (c.row < 0) return;
+  const int at = part * VER_PART + warp * VER_RUN;   // this warp's run of the row
+  float z[VER_FEW];
+  ver_load(z, a.logits + c.row * a.logits_stride + at, a.vocab - at, a.vec, -INFINITY);
   double s = 0.0;
-#pragma unroll 1
-  for (int t = tiles - 1; t >= 0; --t) {   // (the first last: it stays)
-    if (tiles > 1) load_more(t);
-    exps();
-    s += lane_sum();
+#pragma unroll
+  for (int i = 0; i < VER_FEW; i += 2)
+    s += ver_exp2(((double)ver_entry(z[i]) - (double)c.max) * to_exp2) + ver_exp2(((double)ver_entry(z[i + 1]) - (double)c.max) * to_exp2);
+#pragma unroll
+  for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+  if (lane == 0) s_part[warp] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    s = 0.0;
+#pragma unroll
+    for (int w = 0; w < VER_WARPS; ++w) s += s_part[w];
+    a.sums[(size_t)req * a.parts + part] = s;
   }
-  cluster.barrier_wait(std::move(there));
-  const double inv_S = 1.0 / sum_all(s, 0);
+}
 
-  // what is drawn from: p - q where a draft was refused (what is no number or negative in q counts as 0), p otherwise
-  int x = acc < k && !a.probs ? a.draft[row] : -1;
-  auto rests = [&](int t) {   // of tile t, whose exponentials are in e
-    const int at = w0 + t * TILE + lane * 4;
-    if (q) {
-      asm volatile("cp.async.wait_group 0;" ::: "memory");
+// What a token is drawn from: p - q where a draft was refused (what is no number or negative in q counts as 0), p otherwise.
+struct VerWeights {
+  const float *z, *q;   // the row, and that of q (null: none)
+  int x;                // the entry that a certain draft takes out (-1: none)
+  double top, to_exp2, inv_sum;
+};
+// Entries at + 4 lane + 128 g + j of a run, in 64 bits, and the sum of p over the lane's.
+__device__ __forceinline__ void ver_weights(const VerifyArgs& a, const VerWeights& w, int at, double (&e)[VER_FEW], double& all) {
+  const int lane = threadIdx.x & 31;
+  float z[VER_FEW], q[VER_FEW];
+  ver_load(z, w.z + at, a.vocab - at, a.vec, -INFINITY);
+  if (w.q) ver_load(q, w.q + at, a.vocab - at, a.probs_vec, 0.f);
 #pragma unroll
-      for (int i = 0; i < EACH; i += 4) {
-        const float4 v = *reinterpret_cast<const float4*>(&s_q[warp][i * 32 + lane * 4]);
-        const float w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const double p = e[i + j] * inv_S;
-          e[i + j] = w[j] > 0.f && at + i * 32 + j < V ? fmax(p - (double)w[j], 0.0) : p;   // (behind the end: nothing was fetched, and p is 0)
-        }
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < EACH; ++i) {
-        const double p = e[i] * inv_S;
-        e[i] = at + (i >> 2) * 128 + (i & 3) == x ? 0.0 : p;
-      }
-    }
-  };
-  bool have = tiles == 1;   // the exponentials of the only tile are in e
-  auto rest_sum = [&]() {
-    double r = 0.0;
-#pragma unroll 1
-    for (int t = tiles - 1; t >= 0; --t) {
-      if (!have) {
-        load_more(t);
-        exps();
-      }
-      rests(t);
-      r += lane_sum();
-    }
-    return sum_all(r, 1);
-  };
-  double total;
-#pragma unroll 1
-  while (true) {
-    total = rest_sum();
-    if (total > 0.0 || (!q && x < 0)) break;
-    q = nullptr;          // q covers p everywhere: from p itself
-    x = -1;
-    have = false;
-    cluster.sync();       // (everybody has read the sums)
+  for (int i = 0; i < VER_FEW; ++i) {
+    const double p = ver_exp2(((double)ver_entry(z[i]) - w.top) * w.to_exp2) * w.inv_sum;
+    all += p;
+    if (w.q) e[i] = q[i] > 0.f ? fmax(p - (double)q[i], 0.0) : p;
+    else e[i] = at + lane * 4 + (i >> 2) * 128 + (i & 3) == w.x ? 0.0 : p;
   }
-  const double target = (double)a.u_pick[req] * total;
-  // the CTA, and the warp in it, whose run takes the sum past the target; else the last with anything in it
-  double base = 0.0;
-  if (ver_part(lane < PICK_CTAS ? s_all[1][lane] : 0.0, target, base) != rank) return;
-  if (ver_part(lane < PICK_WARPS ? s_part[lane] : 0.0, target, base) != warp) return;
-  int token = -1, last = 0;
-#pragma unroll 1
-  for (int t = 0; t < tiles && token < 0; ++t) {
-    if (tiles > 1) {   // (one tile: its are in e)
-      load_more(t);
-      exps();
-      rests(t);
-    }
-    double c[EACH / 4];   // running sums over the lanes, of each group of 128
+}
+
+// The first of the CTA's values (`count` of them, in order) at which the running sum exceeds target, else the last with anything in it; `base`
+// grows by what stands before it.  By one warp.
+template <typename F>
+__device__ __forceinline__ int ver_find(F value, int count, double target, double& base) {
+  const int lane = threadIdx.x & 31;
+  int last = 0;
+  double last_base = base;
+  for (int j0 = 0; j0 < count; j0 += 32) {
+    const double v = j0 + lane < count ? value(j0 + lane) : 0.0;
+    double c = v;
 #pragma unroll
-    for (int g = 0; g < EACH / 4; ++g) c[g] = (e[4 * g] + e[4 * g + 1]) + (e[4 * g + 2] + e[4 * g + 3]);
+    for (int d = 1; d < 32; d <<= 1) {
+      const double u = __shfl_up_sync(0xffffffffu, c, d);
+      if (lane >= d) c += u;
+    }
+    const double up = __shfl_up_sync(0xffffffffu, c, 1), before = base + (lane ? up : 0.0);
+    const unsigned hit = __ballot_sync(0xffffffffu, v > 0.0 && base + c > target), any = __ballot_sync(0xffffffffu, v > 0.0);
+    const int l = hit ? __ffs(hit) - 1 : any ? 31 - __clz(any) : 0;
+    const double at = __shfl_sync(0xffffffffu, before, l);
+    if (hit) {
+      base = at;
+      return j0 + l;
+    }
+    if (any) {
+      last = j0 + l;
+      last_base = at;
+    }
+    base += __shfl_sync(0xffffffffu, c, 31);
+  }
+  base = last_base;
+  return last;
+}
+
+__global__ void __launch_bounds__(VER_THREADS) blink_verify_draw_kernel(const VerifyArgs a) {
+  __shared__ bool s_last;
+  __shared__ VerRun s_run[VER_WARPS];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int req = (int)(blockIdx.x / (unsigned)a.parts), part = (int)(blockIdx.x - (unsigned)req * a.parts);
+  const float T = a.temperature[req], u = a.u_pick[req];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const VerChoice c = a.choice[req];
+  if (c.row < 0) return;
+  VerWeights w;
+  w.z = a.logits + c.row * a.logits_stride;
+  w.q = c.refused && a.probs ? a.probs + c.row * a.probs_stride : nullptr;
+  w.x = c.refused && !a.probs ? a.draft[c.row] : -1;
+  w.top = (double)c.max;
+  w.to_exp2 = 1.44269504088896340736 / (double)T;
+  double s = 0.0;
+#pragma unroll 4
+  for (int j = lane; j < a.parts; j += 32) s += a.sums[(size_t)req * a.parts + j];
+#pragma unroll
+  for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+  w.inv_sum = 1.0 / s;
+  double rest = 0.0, all = 0.0, e[VER_FEW];
+  ver_weights(a, w, part * VER_PART + warp * VER_RUN, e, all);
+#pragma unroll
+  for (int i = 0; i < VER_FEW; i += 2) rest += e[i] + e[i + 1];
+#pragma unroll
+  for (int d = 16; d; d >>= 1) {
+    rest += __shfl_xor_sync(0xffffffffu, rest, d);
+    all += __shfl_xor_sync(0xffffffffu, all, d);
+  }
+  if (lane == 0) s_run[warp] = a.runs[((size_t)req * a.parts + part) * VER_WARPS + warp] = VerRun{rest, all};
+  __syncthreads();
+  if (tid == 0) {
+    VerRun r = {0.0, 0.0};
+#pragma unroll
+    for (int i = 0; i < VER_WARPS; ++i) {
+      r.rest += s_run[i].rest;
+      r.all += s_run[i].all;
+    }
+    a.part_runs[(size_t)req * a.parts + part] = r;
+    __threadfence();   // (the CTA's, which the barrier put before this)
+    s_last = atomicAdd(&a.arrived[req], 1u) == (unsigned)a.parts - 1u;
+  }
+  __syncthreads();
+  if (!s_last || warp != 0) return;
+  __threadfence();
+  // the request's last CTA: its first warp draws
+  const VerRun* r = a.part_runs + (size_t)req * a.parts;
+  double total = 0.0, total_all = 0.0;
+#pragma unroll 4
+  for (int j = lane; j < a.parts; j += 32) {
+    total += __ldcg(&r[j].rest);
+    total_all += __ldcg(&r[j].all);
+  }
+#pragma unroll
+  for (int d = 16; d; d >>= 1) {
+    total += __shfl_xor_sync(0xffffffffu, total, d);
+    total_all += __shfl_xor_sync(0xffffffffu, total_all, d);
+  }
+  const bool none = !(total > 0.0);   // q covers p everywhere: from p itself
+  if (none) {
+    w.q = nullptr;
+    w.x = -1;
+    total = total_all;
+  }
+  const double target = (double)u * total;
+  double base = 0.0;
+  const int in = ver_find([&](int j) { return __ldcg(none ? &r[j].all : &r[j].rest); }, a.parts, target, base);
+  r = a.runs + ((size_t)req * a.parts + in) * VER_WARPS;
+  const int run = ver_find([&](int j) { return __ldcg(none ? &r[j].all : &r[j].rest); }, VER_WARPS, target, base);
+  int token = -1, last = 0;
+  {
+    const int from = in * VER_PART + run * VER_RUN;
+    ver_weights(a, w, from, e, all);
+    double sum[VER_FEW / 4];   // running sums over the lanes, of each group of 128
+#pragma unroll
+    for (int g = 0; g < VER_FEW / 4; ++g) sum[g] = (e[4 * g] + e[4 * g + 1]) + (e[4 * g + 2] + e[4 * g + 3]);
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
 #pragma unroll
-      for (int g = 0; g < EACH / 4; ++g) {
-        const double u = __shfl_up_sync(0xffffffffu, c[g], d);
-        if (lane >= d) c[g] += u;
+      for (int g = 0; g < VER_FEW / 4; ++g) {
+        const double x = __shfl_up_sync(0xffffffffu, sum[g], d);
+        if (lane >= d) sum[g] += x;
       }
     }
 #pragma unroll
-    for (int g = 0; g < EACH / 4; ++g) {
-      const double up = __shfl_up_sync(0xffffffffu, c[g], 1);
-      double run = lane ? base + up : base;
+    for (int g = 0; g < VER_FEW / 4; ++g) {
+      const double up = __shfl_up_sync(0xffffffffu, sum[g], 1);
+      double running = lane ? base + up : base;
       int hit = 4, some = -1;   // of the lane's four
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        run += e[4 * g + j];
+        running += e[4 * g + j];
         if (e[4 * g + j] > 0.0) {
           some = j;
-          if (hit == 4 && run > target) hit = j;
+          if (hit == 4 && running > target) hit = j;
         }
       }
       const unsigned hits = __ballot_sync(0xffffffffu, hit < 4), any = __ballot_sync(0xffffffffu, some >= 0);
-      const int at = w0 + t * TILE + g * 128;
       const int l = hits ? __ffs(hits) - 1 : any ? 31 - __clz(any) : 0;
       const int h = __shfl_sync(0xffffffffu, hit, l), o = __shfl_sync(0xffffffffu, some, l);
       if (token < 0) {
-        if (hits) token = at + l * 4 + h;
-        else if (any) last = at + l * 4 + o;
+        if (hits) token = from + g * 128 + l * 4 + h;
+        else if (any) last = from + g * 128 + l * 4 + o;
       }
-      base += __shfl_sync(0xffffffffu, c[g], 31);
+      base += __shfl_sync(0xffffffffu, sum[g], 31);
     }
   }
-  if (lane == 0) a.tokens[row] = token >= 0 ? token : last;
+  if (lane == 0) a.tokens[c.row] = token >= 0 ? token : last;
 }
 
-static int64_t verify_chunks(int vocab) { return ((int64_t)vocab + VER_CHUNK - 1) / VER_CHUNK; }
+struct VerifySpace {
+  uint64_t chunks, sums, runs, part_runs, choice, arrived, end;
+  int64_t n_chunks, n_parts;
+};
+static VerifySpace verify_space(int64_t rows, int64_t n, int64_t vocab) {
+  VerifySpace s;
+  s.n_chunks = (vocab + VER_CHUNK - 1) / VER_CHUNK;
+  s.n_parts = (vocab + VER_PART - 1) / VER_PART;
+  s.chunks = 0;
+  s.sums = s.chunks + (uint64_t)(rows * s.n_chunks) * sizeof(VerChunk);
+  s.runs = (s.sums + (uint64_t)(n * s.n_parts) * 8 + 15) / 16 * 16;
+  s.part_runs = s.runs + (uint64_t)(n * s.n_parts * VER_WARPS) * sizeof(VerRun);
+  s.choice = s.part_runs + (uint64_t)(n * s.n_parts) * sizeof(VerRun);
+  s.arrived = s.choice + (uint64_t)n * sizeof(VerChoice);
+  s.end = s.arrived + (uint64_t)n * 4;
+  return s;
+}
 
 }  // namespace blink
 
 extern "C" {
 
-uint64_t blink_verify_workspace(int rows, int vocab) {
-  if (rows < 0 || vocab < 1) return 0;
-  return (uint64_t)rows * blink::verify_chunks(vocab) * sizeof(blink::VerChunk);
+uint64_t blink_verify_workspace(int rows, int n_requests, int vocab) {
+  if (rows < 1 || n_requests < 1 || vocab < 2) return 0;
+  return blink::verify_space(rows, n_requests, vocab).end;
 }
 
 int blink_verify_drafts(const float* logits, int64_t logits_stride, int rows, int vocab, const int32_t* row_start, int n_requests,
@@ -433,8 +500,10 @@ int blink_verify_drafts(const float* logits, int64_t logits_stride, int rows, in
     if (!ops_aligned(p, 4)) return BLINK_EINVAL;
   if (((uintptr_t)draft_probs & 3) || rows < 1 || vocab < 2 || n_requests < 1 || logits_stride < vocab || (draft_probs && probs_stride < vocab))
     return BLINK_EINVAL;
-  if (vocab > 0x3fffffff) return BLINK_ETOOBIG;
-  if (!ops_aligned(workspace, 16) || workspace_bytes < blink_verify_workspace(rows, vocab)) return BLINK_EINVAL;
+  if (vocab > 0x3fffffff || n_requests > OPS_MAX_REQUESTS) return BLINK_ETOOBIG;
+  const VerifySpace space = verify_space(rows, n_requests, vocab);
+  if (!ops_aligned(workspace, 16) || workspace_bytes < space.end) return BLINK_EINVAL;
+  char* ws = static_cast<char*>(workspace);
   VerifyArgs a;
   a.logits = logits;
   a.probs = draft_probs;
@@ -447,21 +516,25 @@ int blink_verify_drafts(const float* logits, int64_t logits_stride, int rows, in
   a.u_pick = u_pick;
   a.tokens = out_tokens;
   a.accepted = n_accepted;
-  a.chunks_of = static_cast<VerChunk*>(workspace);
+  a.chunks_of = reinterpret_cast<VerChunk*>(ws + space.chunks);
+  a.sums = reinterpret_cast<double*>(ws + space.sums);
+  a.runs = reinterpret_cast<VerRun*>(ws + space.runs);
+  a.part_runs = reinterpret_cast<VerRun*>(ws + space.part_runs);
+  a.choice = reinterpret_cast<VerChoice*>(ws + space.choice);
+  a.arrived = reinterpret_cast<unsigned*>(ws + space.arrived);
   a.n = n_requests;
   a.rows = rows;
   a.vocab = vocab;
-  a.chunks = (int)verify_chunks(vocab);
+  a.chunks = (int)space.n_chunks;
+  a.groups = (int)((space.n_chunks + VER_WARPS - 1) / VER_WARPS);
+  a.parts = (int)space.n_parts;
   a.vec = logits_stride % 4 == 0 && ops_aligned(logits, 16);
   a.probs_vec = draft_probs && probs_stride % 4 == 0 && ops_aligned(draft_probs, 16);
-  const int64_t grid = (int64_t)rows * ((a.chunks + VER_WARPS - 1) / VER_WARPS);
-  int rc = ops_launch(blink_verify_rows_kernel, grid, VER_WARPS * 32, 0, stream, 0, false, a);
-  if (rc != BLINK_OK) return rc;
-  // as few entries of a lane as hold the row in one go: 32768 entries in 16 CTAs of 16 warps with four, 131072 with 16 (beyond that, runs of tiles)
-  const int64_t ctas = (int64_t)n_requests * PICK_CTAS;
-  if (vocab <= 32768) return ops_launch(blink_verify_pick_kernel<4>, ctas, PICK_THREADS, 0, stream, PICK_CTAS, true, a);
-  if (vocab <= 65536) return ops_launch(blink_verify_pick_kernel<8>, ctas, PICK_THREADS, 0, stream, PICK_CTAS, true, a);
-  return ops_launch(blink_verify_pick_kernel<16>, ctas, PICK_THREADS, 0, stream, PICK_CTAS, true, a);
+  int rc = ops_launch(blink_verify_rows_kernel, (int64_t)rows * a.groups, VER_THREADS, 0, stream, 0, false, a);
+  if (rc == BLINK_OK) rc = ops_launch(blink_verify_choose_kernel, n_requests, VER_THREADS, 0, stream, 0, true, a);
+  if (rc == BLINK_OK) rc = ops_launch(blink_verify_sums_kernel, (int64_t)n_requests * a.parts, VER_THREADS, 0, stream, 0, true, a);
+  if (rc == BLINK_OK) rc = ops_launch(blink_verify_draw_kernel, (int64_t)n_requests * a.parts, VER_THREADS, 0, stream, 0, true, a);
+  return rc;
 }
 
 }  // extern "C"

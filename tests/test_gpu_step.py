@@ -412,7 +412,7 @@ def spec_state(m, n, max_new, V=500, blocks=200, window=40, sinks=2, seed=0):
                 up=torch.rand(n, device="cuda", generator=g), tok=torch.zeros(rows, dtype=torch.int32, device="cuda"),
                 acc=torch.zeros(n, dtype=torch.int32, device="cuda"), max_new=max_new, window=window, sinks=sinks, V=V,
                 ws=torch.empty(B.blink_window_attention_workspace(m, max_new), dtype=torch.uint8, device="cuda"),
-                ws2=torch.empty(B.blink_verify_workspace(rows, V), dtype=torch.uint8, device="cuda"))
+                ws2=torch.empty(B.blink_verify_workspace(rows, n, V), dtype=torch.uint8, device="cuda"))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])

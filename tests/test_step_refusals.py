@@ -80,7 +80,7 @@ def test_window_attention_sizes_beyond_its_limits():
 
 def _verify(**kw):
     a = dict(logits=P, stride=1000, rows=8, vocab=1000, row_start=P, n=3, draft=P, probs=P, probs_stride=1000, temperature=P, ua=P, up=P, tokens=P,
-             accepted=P, ws=P, ws_bytes=B.blink_verify_workspace(8, 1000), stream=None)
+             accepted=P, ws=P, ws_bytes=B.blink_verify_workspace(8, 3, 1000), stream=None)
     a.update(kw)
     return B.lib().blink_verify_drafts(*a.values())
 
