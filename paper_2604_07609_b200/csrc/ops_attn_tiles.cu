@@ -168,16 +168,26 @@ __device__ __forceinline__ float2 til_add2(float2 a, float2 b) {
 struct TilMask {
   int pos, window, sinks, first_block, n_sinks, from;   // of the row; of the tile's first block in the unit's list; of the list
 };
-__device__ __forceinline__ void til_mask(uint32_t (&r)[32], const TilMask& k, int quarter) {
+// Bits of the keys of a quarter of the tile (two blocks) that the row sees.
+__device__ __forceinline__ uint32_t til_seen(const TilMask& k, int quarter) {
+  uint32_t bits = 0u;
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
     const int i = k.first_block + quarter * 2 + b;
     const int at = (i < k.n_sinks ? i : k.from + i - k.n_sinks) * OPS_BLOCK;
-    const int hi = k.pos - at, lo = k.window > 0 ? hi - k.window : -1, sink = k.sinks - at;
-#pragma unroll
-    for (int x = 0; x < OPS_BLOCK; ++x)
-      if (!(x <= hi && (x > lo || x < sink))) r[b * OPS_BLOCK + x] = 0xff800000u;
+    const int hi = min(max(k.pos - at + 1, 0), OPS_BLOCK);                                  // keys up to its own
+    const int lo = k.window > 0 ? min(max(k.pos - k.window - at + 1, 0), OPS_BLOCK) : 0;    // keys before its window
+    const int sink = min(max(k.sinks - at, 0), OPS_BLOCK);
+    const uint32_t up_to = (1u << hi) - 1u, before = (1u << lo) - 1u, first = (1u << sink) - 1u;
+    bits |= (up_to & (~before | first)) << (b * OPS_BLOCK);
   }
+  return bits;
+}
+__device__ __forceinline__ void til_mask(uint32_t (&r)[32], const TilMask& k, int quarter) {
+  const uint32_t bits = til_seen(k, quarter);
+#pragma unroll
+  for (int x = 0; x < 32; ++x)
+    if (!(bits & (1u << x))) r[x] = 0xff800000u;
 }
 
 // One row of a score tile -> 64 words of probabilities (bf16 pairs), their sum, and the largest score.
@@ -218,27 +228,24 @@ __device__ __forceinline__ void til_probs(uint32_t t_s, float qscale, float neg,
   const float2 s = til_add2(s0, s1);
   sum = s.x + s.y;
 }
-// The largest score alone, for a row's first tile.
-__device__ __forceinline__ float til_max(uint32_t t_s, bool masked, const TilMask& mask) {
-  float mx = -INFINITY;
-#pragma unroll 1
-  for (int k = 0; k < 4; k += 2) {
-    uint32_t va[32], vb[32];
-    til_ld32(t_s + 32u * k, va);
-    til_ld32(t_s + 32u * k + 32u, vb);
-    tmem_wait_ld_til(va, vb);
-    if (masked) {
-      til_mask(va, mask, k);
-      til_mask(vb, mask, k + 1);
-    }
+// A first maximum: the largest score of a quarter of the row's first tile.
+__device__ __forceinline__ float til_max(uint32_t t_s, int quarter, bool masked, const TilMask& mask) {
+  uint32_t va[32], vb[32];
+  til_ld32(t_s + 32u * (uint32_t)quarter, va);
+  til_ld32(t_s + 32u * (uint32_t)quarter, vb);   // (the wait names two)
+  tmem_wait_ld_til(va, vb);
+  if (masked) til_mask(va, mask, quarter);
+  float m0 = -INFINITY, m1 = -INFINITY;
 #pragma unroll
-    for (int x = 0; x < 32; ++x) mx = fmaxf(fmaxf(mx, __uint_as_float(va[x])), __uint_as_float(vb[x]));
+  for (int x = 0; x < 32; x += 4) {
+    m0 = fmaxf(fmaxf(m0, __uint_as_float(va[x])), __uint_as_float(va[x + 1]));
+    m1 = fmaxf(fmaxf(m1, __uint_as_float(va[x + 2])), __uint_as_float(va[x + 3]));
   }
-  return mx;
+  return fmaxf(m0, m1);
 }
 
 // A unit, and which of its tiles each stream takes.
-struct TilUnit {
+struct alignas(16) TilUnit {
   int req, h;
   int row, live[2];        // first of its rows; rows of each stream's
   int pos;                 // position of the first row
@@ -246,6 +253,7 @@ struct TilUnit {
   int last;                // position of the last row
   int begin[2], end[2];    // tiles of each stream
 };
+constexpr int TIL_UNITS = 192;   // of a CTA, worked out by all threads before the first one
 
 template <int HD>
 __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap key_map,
@@ -253,7 +261,8 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
   using S = TilShape<HD>;
   extern __shared__ char s_raw[];
   char* base = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(s_raw) + 1023) & ~(uintptr_t)1023);
-  int* s_pre = reinterpret_cast<int*>(base + S::END);   // [n + 1] units before a request
+  TilUnit* s_unit = reinterpret_cast<TilUnit*>(base + S::END);         // [TIL_UNITS]
+  int* s_pre = reinterpret_cast<int*>(base + S::END) + TIL_UNITS * (sizeof(TilUnit) / 4);   // [n + 1] units before a request
   __shared__ __align__(16) TilShared sh;
   const int w = (int)til_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   int* status = reinterpret_cast<int*>(a.ws);
@@ -306,14 +315,14 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
   __syncthreads();
   til_fence_after();
   const uint32_t tmem = til_uniform(*(volatile uint32_t*)&sh.tmem);
-  const int n_units = s_pre[a.n];
+  const int n_units = (int)til_uniform((uint32_t)s_pre[a.n]);
 
   bool ok = true;   // false once a wait has run out
   auto wait = [&](uint64_t* bar, uint32_t parity) {
     if (ok && !__all_sync(0xffffffffu, til_try(bar, parity))) ok = til_wait_slow(bar, parity, &sh.dead, status);
     return ok;
   };
-  auto unit_of = [&](int u) {
+  auto make_unit = [&](int u) {
     TilUnit t;
     int lo = 0, hi = a.n;   // the last request that begins at or before it
     while (hi - lo > 1) {
@@ -343,9 +352,13 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
     }
     return t;
   };
+  for (int i = threadIdx.x; i < TIL_UNITS && (long long)blockIdx.x + (long long)i * gridDim.x < n_units; i += TIL_THREADS) s_unit[i] = make_unit((int)(blockIdx.x + i * gridDim.x));
+  __syncthreads();
+  auto unit_of = [&](int u) {
+    const int i = (u - (int)blockIdx.x) / (int)gridDim.x;
+    return i < TIL_UNITS ? s_unit[i] : make_unit(u);
+  };
   auto tiles_of = [&](const TilUnit& t) { return max(t.end[0], t.end[1]); };   // (the first tile is one of stream 0, which always has rows)
-  // the tile of the list's blocks 8 j .. is read by streams [first, second)
-  auto takes = [&](const TilUnit& t, int s, int j) { return j >= t.begin[s] && j < t.end[s]; };
 
   if (w < 8) {
     // ---- softmax ----
@@ -406,10 +419,9 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
           wait(&sh.s_full[s], n_s & 1u);
           ++n_s;
           til_fence_after();
-          if (j == t.begin[s]) {
-            const float x = til_max(t_s, masked, mask) * a.qscale;
-            mx_used = x;
-          }
+          // a row's first maximum: from the keys next to its window's end where its first tile is cut by the window, else from the first ones
+          if (j == t.begin[s]) mx_used = til_max(t_s, a.window > 0 && lowest <= p_hi - a.window ? 3 : 0, masked, mask) * a.qscale;
+          if (j + 1 == t.end[s] && more) load_q(next);   // (its last scores are complete: the queries have been read)
           uint32_t p[64];
           float sum;
 #pragma unroll 1
@@ -450,7 +462,7 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
           __syncwarp();
           if (lane == 0) til_arrive(&sh.p_full[s]);
         }
-        if (more) load_q(next);   // (its scores are complete: the queries have been read)
+        if (more) q_there();
         wait(&sh.o_full[s], n_o & 1u);
         ++n_o;
         til_fence_after();
@@ -478,7 +490,6 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
           put(x, k);
           put(y, k + 32);
         }
-        if (more) q_there();
       } else if (more) {
         load_q(next);
         q_there();
@@ -488,58 +499,63 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
     }
   } else if (w == 8) {
     // ---- MMAs ----
+    // (what they are issued with comes from uniform registers, and their loops turn on uniform values: otherwise an MMA's operands are moved first
+    // and its warp is taken for a diverged one, some 100 cycles each, more than the tensor core takes for it)
     const uint32_t idesc_s = til_idesc(TIL_KEYS), idesc_o = til_idesc(HD) | (1u << 16);   // (bit 16: B is MN-major)
-    const uint32_t b0 = til_smem(base);
-    uint32_t n_tile = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0};
+    const uint32_t b0 = til_uniform(til_smem(base));
+    uint32_t n_tile = 0, n_q0 = 0, n_q1 = 0, n_p0 = 0, n_p1 = 0;
+#pragma unroll 1
     for (int u = blockIdx.x; u < n_units && ok; u += (int)gridDim.x) {
       const TilUnit t = unit_of(u);
-      const int tiles = tiles_of(t);
+      const int begin1 = (int)til_uniform((uint32_t)t.begin[1]), end0 = (int)til_uniform((uint32_t)t.end[0]), end1 = (int)til_uniform((uint32_t)t.end[1]);
+      const int tiles = max(end0, end1);   // (stream 0 takes tiles 0 .. end0 - 1, stream 1 begin1 .. end1 - 1, which is none where it has no rows)
       auto scores = [&](int s, int j) {
         const uint32_t n = n_tile + (uint32_t)j, slot = n % S::RING;
         wait(&sh.k_full[slot], (n / S::RING) & 1u);
         if (!ok) return;
         til_fence_after();
         const uint64_t dq = til_desc(b0 + S::Q + s * S::TILE, 16), dk = til_desc(b0 + S::K + slot * S::TILE, 16);
+        const bool last = s == 1 || j < begin1 || j >= end1;
         if (til_elect()) {
 #pragma unroll
           for (int i = 0; i < HD / 16; ++i)
             til_mma(tmem + (uint32_t)s * 128u, dq + (uint64_t)((i >> 2) * 1024 + (i & 3) * 2), dk + (uint64_t)((i >> 2) * 1024 + (i & 3) * 2), idesc_s, i ? 1u : 0u);
           til_commit(&sh.s_full[s]);
-          if (s == 1 || !takes(t, 1, j)) til_commit(&sh.k_empty[slot]);
+          if (last) til_commit(&sh.k_empty[slot]);
         }
         __syncwarp();
       };
-#pragma unroll 1
-      for (int s = 0; s < 2; ++s) {
-        if (!t.live[s]) continue;
-        wait(&sh.q_full[s], n_q[s] & 1u);
-        ++n_q[s];
+      auto outputs = [&](int s, int j, uint32_t n_p) {
+        const uint32_t n = n_tile + (uint32_t)j, slot = n % S::RING;
+        wait(&sh.p_full[s], n_p & 1u);
+        wait(&sh.v_full[slot], (n / S::RING) & 1u);
+        if (!ok) return;
         til_fence_after();
-        if (t.begin[s] == 0) scores(s, 0);
+        const uint64_t dv = til_desc(b0 + S::V + slot * S::TILE, 2048);
+        const uint32_t keep = j > (s ? begin1 : 0) ? 1u : 0u;
+        const bool end = j + 1 == (s ? end1 : end0), last = s == 1 || j < begin1 || j >= end1;
+        if (til_elect()) {
+#pragma unroll
+          for (int i = 0; i < TIL_BLOCKS; ++i)   // 16 keys each, a block of the cache
+            til_mma_tmem(tmem + 256u + (uint32_t)(s * HD), tmem + (uint32_t)s * 128u + (uint32_t)(i * 8), dv + (uint64_t)(i * (S::TILE / TIL_BLOCKS / 16)), idesc_o,
+                         i ? 1u : keep);
+          if (end) til_commit(&sh.o_full[s]);
+          if (last) til_commit(&sh.v_empty[slot]);
+        }
+        __syncwarp();
+      };
+      wait(&sh.q_full[0], n_q0++ & 1u);
+      scores(0, 0);
+      if (end1 > 0) {
+        wait(&sh.q_full[1], n_q1++ & 1u);
+        if (begin1 == 0) scores(1, 0);
       }
 #pragma unroll 1
       for (int j = 0; j < tiles && ok; ++j) {
-        const uint32_t n = n_tile + (uint32_t)j, slot = n % S::RING;
-#pragma unroll 1
-        for (int s = 0; s < 2; ++s) {
-          if (takes(t, s, j)) {
-            wait(&sh.p_full[s], n_p[s] & 1u);
-            ++n_p[s];
-            wait(&sh.v_full[slot], (n / S::RING) & 1u);
-            if (!ok) break;
-            til_fence_after();
-            if (til_elect()) {
-#pragma unroll
-              for (int i = 0; i < TIL_BLOCKS; ++i)   // 16 keys each, a block of the cache
-                til_mma_tmem(tmem + 256u + (uint32_t)(s * HD), tmem + (uint32_t)s * 128u + (uint32_t)(i * 8),
-                             til_desc(b0 + S::V + slot * S::TILE + i * (S::TILE / TIL_BLOCKS), 2048), idesc_o, (j > t.begin[s] || i) ? 1u : 0u);
-              if (j + 1 == t.end[s]) til_commit(&sh.o_full[s]);
-              if (s == 1 || !takes(t, 1, j)) til_commit(&sh.v_empty[slot]);
-            }
-            __syncwarp();
-          }
-          if (j + 1 < tiles && takes(t, s, j + 1)) scores(s, j + 1);
-        }
+        if (j < end0) outputs(0, j, n_p0++);
+        if (j + 1 < end0) scores(0, j + 1);
+        if (j >= begin1 && j < end1) outputs(1, j, n_p1++);
+        if (j + 1 >= begin1 && j + 1 < end1) scores(1, j + 1);
       }
       n_tile += (uint32_t)tiles;
     }
@@ -552,19 +568,24 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
       const CUtensorMap* map = part == 2 ? &value_map : &key_map;
       const int rows_block = a.pool.Hkv * OPS_BLOCK, none = (int)a.pool.n_blocks * rows_block;   // (a row behind the pool: zeros)
       uint32_t n_tile = 0, n_land = 0;
+      auto block_id = [&](const TilUnit& t, int j) {   // lane: block of the tile; behind the list the last one again (nobody sees it there)
+        const int i = min(j * TIL_BLOCKS + (lane & 7), t.span.n - 1);
+        return t.last >= 0 ? a.table[(long long)t.req * a.stride + (i < t.span.sinks ? i : t.span.from + i - t.span.sinks)] : -1;
+      };
+      TilUnit t, next;
+      int id = 0, next_id = 0;
+      if ((int)blockIdx.x < n_units) {
+        next = unit_of((int)blockIdx.x);
+        next_id = block_id(next, 0);
+      }
       for (int u = blockIdx.x; u < n_units && ok; u += (int)gridDim.x) {
-        const TilUnit t = unit_of(u);
+        t = next;
+        id = next_id;
         const int tiles = tiles_of(t);
-        const int32_t* table = a.table + (long long)t.req * a.stride;
-        auto block_id = [&](int j) {   // lane: block of the tile; behind the list the last one again (nobody sees it there)
-          const int i = min(j * TIL_BLOCKS + (lane & 7), t.span.n - 1);
-          return t.last >= 0 ? table[i < t.span.sinks ? i : t.span.from + i - t.span.sinks] : -1;
-        };
-        int id = block_id(0);
 #pragma unroll 1
         for (int j = 0; j < tiles; ++j) {
           const int mine = (unsigned)id < (unsigned)a.pool.n_blocks ? id * rows_block + t.h * OPS_BLOCK : none;
-          if (j + 1 < tiles) id = block_id(j + 1);
+          if (j + 1 < tiles) id = block_id(t, j + 1);
           const uint32_t n = n_tile + (uint32_t)j, slot = n % S::RING, use = n / S::RING;
           uint64_t* empty = part == 2 ? &sh.v_empty[slot] : &sh.k_empty[slot];
           if (use > 0) wait(empty, (use - 1u) & 1u);
@@ -601,6 +622,10 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
             til_proxy_fence();
             __syncwarp();
             if (lane == 0) til_arrive(&sh.v_full[slot]);
+          }
+          if (j == 0 && u + (int)gridDim.x < n_units) {   // (the copies are on their way)
+            next = unit_of(u + (int)gridDim.x);
+            next_id = block_id(next, 0);
           }
         }
         n_tile += (uint32_t)tiles;
@@ -649,7 +674,7 @@ static int tiles_run(const AttnArgs& a, int sms, int64_t most_units, void* strea
     if (encode(&maps[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, a.pool.k, dims, strides, i ? value_box : key_box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
       return BLINK_ECUDA;
-  const size_t smem = (size_t)S::END + 1024 + (size_t)(a.n + 1) * 4;
+  const size_t smem = (size_t)S::END + 1024 + TIL_UNITS * sizeof(TilUnit) + (size_t)(a.n + 1) * 4;
   const int64_t grid = most_units < sms ? most_units : sms;
   return ops_launch(blink_attn_tiles_kernel<HD>, grid, TIL_THREADS, smem, stream, 0, true, a, maps[0], maps[1]);
 }

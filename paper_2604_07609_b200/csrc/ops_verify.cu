@@ -4,15 +4,16 @@
 //   first refused i: a token from max(0, p_i - q_i), none refused: from p of the last row; by the inverse of its running sum in the order of
 //   the indexes: the first j with sum_{<= j} > v * sum
 //
-// Four kernels, each waiting for the one before it only where it needs its results.
+// Five kernels, each waiting for the one before it only where it needs its results.
 //   rows    largest value and sum of exponentials of pieces of 1024 entries of every row, a warp each: one pass over the logits, which is what
 //           bounds the whole (HBM: 4 bytes an entry).  A lane has its 32 entries on their way at once and sums against its own largest
 //           value, so that nothing waits for another warp.  Exponentials in 32 bits, sums of a lane's entries in 32, everything above in
 //           64: the acceptance test is off by some 1e-8.
 //   choose  a CTA per request: the first refused draft, from the pieces
-//   sums    the exponentials of that row, 256 entries a warp
-//   draw    the same entries once more: weights max(0, p - q) and their sum per warp; the last CTA of a request to come finds the run of 256 in
-//           which the running sum passes its target, and goes over that run again
+//   sums    the exponentials of that row, 512 entries a warp
+//   weights the same entries once more: max(0, p - q), and their sum per warp
+//   draw    a warp per request: the run of 512 in which the running sum passes its target, and the entry of that run
+// (the last two as one kernel, the last CTA of a request to come drawing, were slower: a fence and a counter in every CTA's way)
 // The chosen row's sums decide between neighbours that are as close as 1e-6, so its exponentials, sums and running sum are in 64 bits.  Sums are
 // taken in an order that sizes alone fix, whoever comes last: the same call gives the same token.
 #include <cmath>
@@ -23,7 +24,7 @@ namespace blink {
 
 constexpr int VER_WARPS = 8, VER_THREADS = VER_WARPS * 32;
 constexpr int VER_EACH = 32, VER_CHUNK = 32 * VER_EACH;   // rows: entries of a lane, a warp
-constexpr int VER_FEW = 8, VER_RUN = 32 * VER_FEW, VER_PART = VER_WARPS * VER_RUN;            // sums, draw
+constexpr int VER_FEW = 16, VER_RUN = 32 * VER_FEW, VER_PART = VER_WARPS * VER_RUN;            // sums, weights
 
 struct VerChunk {
   double sum;   // of exp((z - max) / T)
@@ -52,9 +53,9 @@ struct VerifyArgs {
   VerRun* runs;          // [n][parts * VER_WARPS], and behind them the same for whole parts, [n][parts]
   VerRun* part_runs;
   VerChoice* choice;     // [n]
-  unsigned* arrived;     // [n]
   int n, rows, vocab, chunks, groups, parts;
   bool vec, probs_vec;   // rows on 16-byte boundaries
+  double sixteenths[16]; // 2^(i / 16)
 };
 
 // No number: as if the entry were not there.
@@ -118,11 +119,9 @@ __global__ void __launch_bounds__(VER_THREADS) blink_verify_rows_kernel(const Ve
   if (threadIdx.x == 0) s_req = -1;
   __syncthreads();
   for (int r = threadIdx.x; r < a.n; r += VER_THREADS) {
-    const int first = a.row_start[r];
-    if (first <= row && row < a.row_start[r + 1]) {
+    if (a.row_start[r] <= row && row < a.row_start[r + 1]) {
       s_req = r;
       s_T = a.temperature[r];
-      if (first == row && chunk < VER_WARPS) a.arrived[r] = 0u;   // for the draw
     }
   }
   __syncthreads();
@@ -175,18 +174,33 @@ __global__ void __launch_bounds__(VER_THREADS) blink_verify_rows_kernel(const Ve
   if (lane == 0) a.chunks_of[(size_t)row * a.chunks + chunk] = VerChunk{sum, m, chunk * VER_CHUNK + idx};
 }
 
-// 2^t for t <= 0 in 64 bits: the whole part into the exponent, the rest, at most half, by the series of exp(f ln 2) up to its tenth power
-// (off by (ln 2 / 2)^11 / 11! = 2e-13).  Below 2^-1020: 0.
-__device__ __forceinline__ double ver_exp2(double t) {
-  constexpr double L = 0.693147180559945309417;
-  constexpr double C2 = L * L / 2, C3 = C2 * L / 3, C4 = C3 * L / 4, C5 = C4 * L / 5, C6 = C5 * L / 6, C7 = C6 * L / 7, C8 = C7 * L / 8, C9 = C8 * L / 9,
-                   C10 = C9 * L / 10;
+// exp((z - top) / T) in 64 bits, as 2^(n / 16) 2^(f / 16): n whole, its sixteenths from a table in shared memory (16 entries: two banks
+// each, no conflicts) and the rest into the exponent; |f| <= 1/2, by the series of exp(f ln 2 / 16) up to its fifth power (off by
+// (ln 2 / 32)^6 / 6! = 1.4e-13).  64-bit operations are what the kernels below are bound by: twelve here, one of them the conversion.
+struct VerExp {
+  const double* table;   // 2^(i / 16)
+  double scale, shift;   // 16 log2(e) / T, and -top times that
+  float top, below;      // entries below this are 0: (z - top) / T < -700
+};
+__device__ __forceinline__ VerExp ver_exp_of(const double* table, float top, float T) {
+  VerExp x;
+  x.table = table;
+  x.scale = 16.0 * 1.44269504088896340736 / (double)T;
+  x.shift = -(double)top * x.scale;
+  x.top = top;
+  x.below = fmaxf(top - 700.f * T, -3e38f);   // (above -inf)
+  return x;
+}
+__device__ __forceinline__ double ver_exp(const VerExp& x, float z) {
+  constexpr double L = 0.693147180559945309417 / 16, C2 = L * L / 2, C3 = C2 * L / 3, C4 = C3 * L / 4, C5 = C4 * L / 5;
   constexpr double SHIFT = 6755399441055744.0;   // 1.5 * 2^52: adding it leaves the nearest whole number in the low bits
-  const double s = t + SHIFT, f = t - (s - SHIFT), f2 = f * f;
+  const double t = fma((double)z, x.scale, x.shift), s = t + SHIFT, f = t - (s - SHIFT);
   const int n = __double2loint(s);
-  const double a = fma(f2, fma(f2, fma(f2, fma(f2, C10, C8), C6), C4), C2), b = fma(f2, fma(f2, fma(f2, fma(f2, C9, C7), C5), C3), L);
-  const double p = fma(f, b, fma(f2, a, 1.0));   // even and odd powers side by side
-  return t > -1020.0 ? __hiloint2double(__double2hiint(p) + (n << 20), __double2loint(p)) : 0.0;
+  const double p = fma(f, fma(f, fma(f, fma(f, fma(f, C5, C4), C3), C2), L), 1.0) * x.table[n & 15];
+  return z >= x.below ? __hiloint2double(__double2hiint(p) + ((n >> 4) << 20), __double2loint(p)) : 0.0;   // (no number: 0 too)
+}
+__device__ __forceinline__ void ver_table(double* table, const VerifyArgs& a) {   // before a barrier
+  if (threadIdx.x < 16) table[threadIdx.x] = a.sixteenths[threadIdx.x];
 }
 
 // The request's rows, first and behind the last.
@@ -197,6 +211,7 @@ __device__ __forceinline__ int2 ver_rows(const VerifyArgs& a, int req) {
 
 __global__ void __launch_bounds__(VER_THREADS) blink_verify_choose_kernel(const VerifyArgs a) {
   __shared__ int s_first;
+  __shared__ double s_table[16];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int req = (int)blockIdx.x;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -204,8 +219,8 @@ __global__ void __launch_bounds__(VER_THREADS) blink_verify_choose_kernel(const 
   const int2 rows = ver_rows(a, req);
   const int start = rows.x, k = rows.y - rows.x - 1;
   const float T = a.temperature[req];
-  const double to_exp2 = 1.44269504088896340736 / (double)T;
   if (tid == 0) s_first = max(k, 0);
+  ver_table(s_table, a);
   __syncthreads();
   // A row from its pieces: largest value, its index, sum.
   auto row_of = [&](int row, float& m, int& idx, double& sum, bool with_sum) {
@@ -223,8 +238,9 @@ __global__ void __launch_bounds__(VER_THREADS) blink_verify_choose_kernel(const 
     const bool one = ver_one(T, m);
     sum = 0.0;
     if (!one && with_sum) {
+      const VerExp x = ver_exp_of(s_table, m, T);
 #pragma unroll 4
-      for (int j = lane; j < a.chunks; j += 32) sum += c[j].max > -INFINITY ? c[j].sum * ver_exp2(((double)c[j].max - (double)m) * to_exp2) : 0.0;
+      for (int j = lane; j < a.chunks; j += 32) sum += c[j].sum * ver_exp(x, c[j].max);
 #pragma unroll
       for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
     }
@@ -242,7 +258,7 @@ __global__ void __launch_bounds__(VER_THREADS) blink_verify_choose_kernel(const 
     if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
     waited = true;
     const bool one = row_of(row, m, idx, sum, true);
-    const bool ok = one ? x == idx : in && (double)u * (double)q * sum < ver_exp2(((double)z - (double)m) * to_exp2);
+    const bool ok = one ? x == idx : in && (double)u * (double)q * sum < ver_exp(ver_exp_of(s_table, m, T), z);
     if (lane == 0 && !ok) atomicMin(&s_first, i);
   }
   if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -271,21 +287,23 @@ __global__ void __launch_bounds__(VER_THREADS) blink_verify_choose_kernel(const 
 }
 
 __global__ void __launch_bounds__(VER_THREADS) blink_verify_sums_kernel(const VerifyArgs a) {
-  __shared__ double s_part[VER_WARPS];
+  __shared__ double s_part[VER_WARPS], s_table[16];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int req = (int)(blockIdx.x / (unsigned)a.parts), part = (int)(blockIdx.x - (unsigned)req * a.parts);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const double to_exp2 = 1.44269504088896340736 / (double)a.temperature[req];
+  const float T = a.temperature[req];
+  ver_table(s_table, a);
+  __syncthreads();
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const VerChoice c = a.choice[req];
   if (c.row < 0) return;
   const int at = part * VER_PART + warp * VER_RUN;   // this warp's run of the row
   float z[VER_FEW];
   ver_load(z, a.logits + c.row * a.logits_stride + at, a.vocab - at, a.vec, -INFINITY);
+  const VerExp x = ver_exp_of(s_table, c.max, T);
   double s = 0.0;
 #pragma unroll
-  for (int i = 0; i < VER_FEW; i += 2)
-    s += ver_exp2(((double)ver_entry(z[i]) - (double)c.max) * to_exp2) + ver_exp2(((double)ver_entry(z[i + 1]) - (double)c.max) * to_exp2);
+  for (int i = 0; i < VER_FEW; i += 2) s += ver_exp(x, z[i]) + ver_exp(x, z[i + 1]);
 #pragma unroll
   for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
   if (lane == 0) s_part[warp] = s;
@@ -302,24 +320,31 @@ __global__ void __launch_bounds__(VER_THREADS) blink_verify_sums_kernel(const Ve
 struct VerWeights {
   const float *z, *q;   // the row, and that of q (null: none)
   int x;                // the entry that a certain draft takes out (-1: none)
-  double top, to_exp2, inv_sum;
+  VerExp exp;
+  double inv_sum;
 };
+// The row's sum of exponentials, by a whole warp.
+__device__ __forceinline__ double ver_sum(const VerifyArgs& a, int req) {
+  double s = 0.0;
+#pragma unroll 4
+  for (int j = threadIdx.x & 31; j < a.parts; j += 32) s += a.sums[(size_t)req * a.parts + j];
+#pragma unroll
+  for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+  return s;
+}
 // Entries at + 4 lane + 128 g + j of a run, in 64 bits, and the sum of p over the lane's.
-__device__ __forceinline__ void ver_weights(const VerifyArgs& a, const VerWeights& w, int at, double (&e)[VER_FEW], double& all) {
+__device__ __forceinline__ void ver_weights(const VerWeights& w, int at, const float (&z)[VER_FEW], const float (&q)[VER_FEW], double (&e)[VER_FEW], double& all) {
   const int lane = threadIdx.x & 31;
-  float z[VER_FEW], q[VER_FEW];
-  ver_load(z, w.z + at, a.vocab - at, a.vec, -INFINITY);
-  if (w.q) ver_load(q, w.q + at, a.vocab - at, a.probs_vec, 0.f);
 #pragma unroll
   for (int i = 0; i < VER_FEW; ++i) {
-    const double p = ver_exp2(((double)ver_entry(z[i]) - w.top) * w.to_exp2) * w.inv_sum;
+    const double p = ver_exp(w.exp, z[i]) * w.inv_sum;
     all += p;
     if (w.q) e[i] = q[i] > 0.f ? fmax(p - (double)q[i], 0.0) : p;
     else e[i] = at + lane * 4 + (i >> 2) * 128 + (i & 3) == w.x ? 0.0 : p;
   }
 }
 
-// The first of the CTA's values (`count` of them, in order) at which the running sum exceeds target, else the last with anything in it; `base`
+// The first of `count` values, in order, at which the running sum exceeds target, else the last with anything in it; `base`
 // grows by what stands before it.  By one warp.
 template <typename F>
 __device__ __forceinline__ int ver_find(F value, int count, double target, double& base) {
@@ -352,29 +377,43 @@ __device__ __forceinline__ int ver_find(F value, int count, double target, doubl
   return last;
 }
 
-__global__ void __launch_bounds__(VER_THREADS) blink_verify_draw_kernel(const VerifyArgs a) {
-  __shared__ bool s_last;
-  __shared__ VerRun s_run[VER_WARPS];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int req = (int)(blockIdx.x / (unsigned)a.parts), part = (int)(blockIdx.x - (unsigned)req * a.parts);
-  const float T = a.temperature[req], u = a.u_pick[req];
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+// Of the request's chosen row, all but its sum; false: nothing is drawn.
+__device__ __forceinline__ bool ver_choice(const VerifyArgs& a, int req, const double* table, float T, VerWeights& w, int& row) {
   const VerChoice c = a.choice[req];
-  if (c.row < 0) return;
-  VerWeights w;
+  row = c.row;
+  if (c.row < 0) return false;
   w.z = a.logits + c.row * a.logits_stride;
   w.q = c.refused && a.probs ? a.probs + c.row * a.probs_stride : nullptr;
   w.x = c.refused && !a.probs ? a.draft[c.row] : -1;
-  w.top = (double)c.max;
-  w.to_exp2 = 1.44269504088896340736 / (double)T;
-  double s = 0.0;
-#pragma unroll 4
-  for (int j = lane; j < a.parts; j += 32) s += a.sums[(size_t)req * a.parts + j];
-#pragma unroll
-  for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-  w.inv_sum = 1.0 / s;
+  w.exp = ver_exp_of(table, c.max, T);
+  return true;
+}
+
+__global__ void __launch_bounds__(VER_THREADS) blink_verify_weights_kernel(const VerifyArgs a) {
+  __shared__ VerRun s_run[VER_WARPS];
+  __shared__ double s_inv, s_table[16];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int req = (int)(blockIdx.x / (unsigned)a.parts), part = (int)(blockIdx.x - (unsigned)req * a.parts);
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  VerWeights w;
+  const float T = a.temperature[req];
+  ver_table(s_table, a);
+  __syncthreads();
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  int row;
+  if (!ver_choice(a, req, s_table, T, w, row)) return;
+  const int at = part * VER_PART + warp * VER_RUN;
+  float z[VER_FEW], q[VER_FEW];
+  ver_load(z, w.z + at, a.vocab - at, a.vec, -INFINITY);
+  if (w.q) ver_load(q, w.q + at, a.vocab - at, a.probs_vec, 0.f);
+  if (warp == 0) {
+    const double s = ver_sum(a, req);
+    if (lane == 0) s_inv = 1.0 / s;
+  }
+  __syncthreads();
+  w.inv_sum = s_inv;
   double rest = 0.0, all = 0.0, e[VER_FEW];
-  ver_weights(a, w, part * VER_PART + warp * VER_RUN, e, all);
+  ver_weights(w, at, z, q, e, all);
 #pragma unroll
   for (int i = 0; i < VER_FEW; i += 2) rest += e[i] + e[i + 1];
 #pragma unroll
@@ -384,7 +423,7 @@ __global__ void __launch_bounds__(VER_THREADS) blink_verify_draw_kernel(const Ve
   }
   if (lane == 0) s_run[warp] = a.runs[((size_t)req * a.parts + part) * VER_WARPS + warp] = VerRun{rest, all};
   __syncthreads();
-  if (tid == 0) {
+  if (threadIdx.x == 0) {
     VerRun r = {0.0, 0.0};
 #pragma unroll
     for (int i = 0; i < VER_WARPS; ++i) {
@@ -392,19 +431,26 @@ __global__ void __launch_bounds__(VER_THREADS) blink_verify_draw_kernel(const Ve
       r.all += s_run[i].all;
     }
     a.part_runs[(size_t)req * a.parts + part] = r;
-    __threadfence();   // (the CTA's, which the barrier put before this)
-    s_last = atomicAdd(&a.arrived[req], 1u) == (unsigned)a.parts - 1u;
   }
-  __syncthreads();
-  if (!s_last || warp != 0) return;
-  __threadfence();
-  // the request's last CTA: its first warp draws
+}
+
+__global__ void __launch_bounds__(32) blink_verify_draw_kernel(const VerifyArgs a) {
+  __shared__ double s_table[16];
+  const int lane = threadIdx.x, req = (int)blockIdx.x;
+  const float T = a.temperature[req], u = a.u_pick[req];
+  VerWeights w;
+  ver_table(s_table, a);
+  __syncwarp();
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  int row;
+  if (!ver_choice(a, req, s_table, T, w, row)) return;
+  w.inv_sum = 1.0 / ver_sum(a, req);
   const VerRun* r = a.part_runs + (size_t)req * a.parts;
   double total = 0.0, total_all = 0.0;
 #pragma unroll 4
   for (int j = lane; j < a.parts; j += 32) {
-    total += __ldcg(&r[j].rest);
-    total_all += __ldcg(&r[j].all);
+    total += r[j].rest;
+    total_all += r[j].all;
   }
 #pragma unroll
   for (int d = 16; d; d >>= 1) {
@@ -419,52 +465,54 @@ __global__ void __launch_bounds__(VER_THREADS) blink_verify_draw_kernel(const Ve
   }
   const double target = (double)u * total;
   double base = 0.0;
-  const int in = ver_find([&](int j) { return __ldcg(none ? &r[j].all : &r[j].rest); }, a.parts, target, base);
+  const int in = ver_find([&](int j) { return none ? r[j].all : r[j].rest; }, a.parts, target, base);
   r = a.runs + ((size_t)req * a.parts + in) * VER_WARPS;
-  const int run = ver_find([&](int j) { return __ldcg(none ? &r[j].all : &r[j].rest); }, VER_WARPS, target, base);
+  const int run = ver_find([&](int j) { return none ? r[j].all : r[j].rest; }, VER_WARPS, target, base);
   int token = -1, last = 0;
-  {
-    const int from = in * VER_PART + run * VER_RUN;
-    ver_weights(a, w, from, e, all);
-    double sum[VER_FEW / 4];   // running sums over the lanes, of each group of 128
+  const int from = in * VER_PART + run * VER_RUN;
+  float z[VER_FEW], q[VER_FEW];
+  double e[VER_FEW], all = 0.0;
+  ver_load(z, w.z + from, a.vocab - from, a.vec, -INFINITY);
+  if (w.q) ver_load(q, w.q + from, a.vocab - from, a.probs_vec, 0.f);
+  ver_weights(w, from, z, q, e, all);
+  double sum[VER_FEW / 4];   // running sums over the lanes, of each group of 128
 #pragma unroll
-    for (int g = 0; g < VER_FEW / 4; ++g) sum[g] = (e[4 * g] + e[4 * g + 1]) + (e[4 * g + 2] + e[4 * g + 3]);
+  for (int g = 0; g < VER_FEW / 4; ++g) sum[g] = (e[4 * g] + e[4 * g + 1]) + (e[4 * g + 2] + e[4 * g + 3]);
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-#pragma unroll
-      for (int g = 0; g < VER_FEW / 4; ++g) {
-        const double x = __shfl_up_sync(0xffffffffu, sum[g], d);
-        if (lane >= d) sum[g] += x;
-      }
-    }
+  for (int d = 1; d < 32; d <<= 1) {
 #pragma unroll
     for (int g = 0; g < VER_FEW / 4; ++g) {
-      const double up = __shfl_up_sync(0xffffffffu, sum[g], 1);
-      double running = lane ? base + up : base;
-      int hit = 4, some = -1;   // of the lane's four
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        running += e[4 * g + j];
-        if (e[4 * g + j] > 0.0) {
-          some = j;
-          if (hit == 4 && running > target) hit = j;
-        }
-      }
-      const unsigned hits = __ballot_sync(0xffffffffu, hit < 4), any = __ballot_sync(0xffffffffu, some >= 0);
-      const int l = hits ? __ffs(hits) - 1 : any ? 31 - __clz(any) : 0;
-      const int h = __shfl_sync(0xffffffffu, hit, l), o = __shfl_sync(0xffffffffu, some, l);
-      if (token < 0) {
-        if (hits) token = from + g * 128 + l * 4 + h;
-        else if (any) last = from + g * 128 + l * 4 + o;
-      }
-      base += __shfl_sync(0xffffffffu, sum[g], 31);
+      const double x = __shfl_up_sync(0xffffffffu, sum[g], d);
+      if (lane >= d) sum[g] += x;
     }
   }
-  if (lane == 0) a.tokens[c.row] = token >= 0 ? token : last;
+#pragma unroll
+  for (int g = 0; g < VER_FEW / 4; ++g) {
+    const double up = __shfl_up_sync(0xffffffffu, sum[g], 1);
+    double running = lane ? base + up : base;
+    int hit = 4, some = -1;   // of the lane's four
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      running += e[4 * g + j];
+      if (e[4 * g + j] > 0.0) {
+        some = j;
+        if (hit == 4 && running > target) hit = j;
+      }
+    }
+    const unsigned hits = __ballot_sync(0xffffffffu, hit < 4), any = __ballot_sync(0xffffffffu, some >= 0);
+    const int l = hits ? __ffs(hits) - 1 : any ? 31 - __clz(any) : 0;
+    const int h = __shfl_sync(0xffffffffu, hit, l), o = __shfl_sync(0xffffffffu, some, l);
+    if (token < 0) {
+      if (hits) token = from + g * 128 + l * 4 + h;
+      else if (any) last = from + g * 128 + l * 4 + o;
+    }
+    base += __shfl_sync(0xffffffffu, sum[g], 31);
+  }
+  if (lane == 0) a.tokens[row] = token >= 0 ? token : last;
 }
 
 struct VerifySpace {
-  uint64_t chunks, sums, runs, part_runs, choice, arrived, end;
+  uint64_t chunks, sums, runs, part_runs, choice, end;
   int64_t n_chunks, n_parts;
 };
 static VerifySpace verify_space(int64_t rows, int64_t n, int64_t vocab) {
@@ -476,8 +524,7 @@ static VerifySpace verify_space(int64_t rows, int64_t n, int64_t vocab) {
   s.runs = (s.sums + (uint64_t)(n * s.n_parts) * 8 + 15) / 16 * 16;
   s.part_runs = s.runs + (uint64_t)(n * s.n_parts * VER_WARPS) * sizeof(VerRun);
   s.choice = s.part_runs + (uint64_t)(n * s.n_parts) * sizeof(VerRun);
-  s.arrived = s.choice + (uint64_t)n * sizeof(VerChoice);
-  s.end = s.arrived + (uint64_t)n * 4;
+  s.end = s.choice + (uint64_t)n * sizeof(VerChoice);
   return s;
 }
 
@@ -521,19 +568,20 @@ int blink_verify_drafts(const float* logits, int64_t logits_stride, int rows, in
   a.runs = reinterpret_cast<VerRun*>(ws + space.runs);
   a.part_runs = reinterpret_cast<VerRun*>(ws + space.part_runs);
   a.choice = reinterpret_cast<VerChoice*>(ws + space.choice);
-  a.arrived = reinterpret_cast<unsigned*>(ws + space.arrived);
   a.n = n_requests;
   a.rows = rows;
   a.vocab = vocab;
   a.chunks = (int)space.n_chunks;
   a.groups = (int)((space.n_chunks + VER_WARPS - 1) / VER_WARPS);
   a.parts = (int)space.n_parts;
+  for (int i = 0; i < 16; ++i) a.sixteenths[i] = std::exp2(i / 16.0);
   a.vec = logits_stride % 4 == 0 && ops_aligned(logits, 16);
   a.probs_vec = draft_probs && probs_stride % 4 == 0 && ops_aligned(draft_probs, 16);
   int rc = ops_launch(blink_verify_rows_kernel, (int64_t)rows * a.groups, VER_THREADS, 0, stream, 0, false, a);
   if (rc == BLINK_OK) rc = ops_launch(blink_verify_choose_kernel, n_requests, VER_THREADS, 0, stream, 0, true, a);
   if (rc == BLINK_OK) rc = ops_launch(blink_verify_sums_kernel, (int64_t)n_requests * a.parts, VER_THREADS, 0, stream, 0, true, a);
-  if (rc == BLINK_OK) rc = ops_launch(blink_verify_draw_kernel, (int64_t)n_requests * a.parts, VER_THREADS, 0, stream, 0, true, a);
+  if (rc == BLINK_OK) rc = ops_launch(blink_verify_weights_kernel, (int64_t)n_requests * a.parts, VER_THREADS, 0, stream, 0, true, a);
+  if (rc == BLINK_OK) rc = ops_launch(blink_verify_draw_kernel, n_requests, 32, 0, stream, 0, true, a);
   return rc;
 }
 
