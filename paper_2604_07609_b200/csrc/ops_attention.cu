@@ -368,7 +368,8 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) blink_attn_few_kernel(const
   __shared__ long long s_warp[FEW_WARPS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (blockIdx.x == 0 && tid == 0) {
-    *reinterpret_cast<int*>(a.ws) = 0;
+    reinterpret_cast<int*>(a.ws)[0] = 0;
+    reinterpret_cast<int*>(a.ws)[1] = 0;   // units that the tiles' CTAs have taken from the counter
     __threadfence();
   }
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (the join waits for the whole of this kernel itself)
@@ -621,6 +622,7 @@ int blink_window_attention(const blink_model_cfg* model, const blink_kv_pool* kv
   a.sinks = sinks;
   a.few = 0x7fffffff;
   a.qscale = (float)(1.4426950408889634 / std::sqrt((double)a.pool.hd));
+  a.out_32 = ops_aligned(out, 32) && out_stride % 16 == 0;
   a.ws = static_cast<char*>(workspace);
   if (model->dtype == BLINK_DTYPE_FP32)
     return a.pool.hd == 128 ? few_run<float, 128, FewFp32<128>, 2>(a, sms, stream) : few_run<float, 64, FewFp32<64>, 2>(a, sms, stream);

@@ -16,6 +16,7 @@ struct AttnArgs {
   int window, sinks;                // window 0: no window
   int few;                          // requests of up to so many rows go to attn_few, longer ones to the tiles
   float qscale;                     // 1 / sqrt(hd) * log2(e)
+  bool out_32;                      // rows of out begin on 32-byte boundaries
   char* ws;
 };
 

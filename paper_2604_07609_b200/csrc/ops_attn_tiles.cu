@@ -4,17 +4,20 @@
 // narrow window wastes little (4 heads: 64 query rows read the keys of their window once).  Keys come in tiles of 128: the visible
 // blocks of the unit, sinks first, eight to a tile, whatever lies between them.
 //
-//   warps 0-3 | 4-7   softmax of stream 0 | 1, a thread per row: scores from TMEM, probabilities back to TMEM over the scores
-//   warp 8            issues the MMAs: scores = Q K^T (operands in shared memory), output += P V (P in TMEM, V as it lies in the cache)
-//   warps 9, 10 | 11  copies of the keys' halves | of the values: a copy takes its thread some 100 cycles, a tile has 24
+//   warps 0-7 | 8-15  softmax of stream 0 | 1, two threads per row (64 keys of a tile each): scores from TMEM, probabilities back to TMEM
+//                     over the scores
+//   warp 16           issues the MMAs: scores = Q K^T (operands in shared memory), output += P V (P in TMEM, V as it lies in the cache)
+//   warps 17, 18 | 19 copies of the keys' halves | of the values: a copy takes its thread some 100 cycles, a tile has 24.  Warp 17 also
+//                     hands out the units, heaviest of a request first, from a counter
 //
 // While one stream is in its softmax the tensor core works for the other; the next scores of a stream are issued behind its output MMAs, so a
-// stream's scores being complete also says that its accumulator is.  The maximum in use follows the largest score only when that has grown
-// by more than 2^8 (the sum takes up smaller growth); then the scores, still in TMEM, are gone over once more and the accumulator is rescaled by
-// the thread that owns the row.  CTAs are persistent; keys of the next unit are on their way while the last tile of one is worked on.
+// stream's scores being complete also says that its accumulator is.  The maximum in use, the same for both threads of a row, follows the
+// largest score only when that has grown by more than 2^8 (the sum takes up smaller growth); then the scores, still in TMEM, are gone over once
+// more and the accumulator is rescaled.  CTAs are persistent; keys of the next unit are on their way while the last tile of one is worked on.
 //
-// What bounds it: the softmax's exponentials: 128 rows x 128 keys are 1024 cycles of the unit that computes them, two streams 2048 a
-// tile, against 1024 of the tensor core.
+// What bounds it: the chain of a stream, softmax -> output -> next scores, of which two overlap.  With one thread per row (eight warps) the
+// softmax alone took 1900 cycles a tile, at four cycles an instruction with one warp of a stream on a scheduler.  Exponentials on the
+// multiply-adds (a quarter to a half of them, degree 3) made it longer, not shorter: they are not what it waits for.
 #include <cuda.h>
 
 #include <cmath>
@@ -24,7 +27,7 @@
 namespace blink {
 
 constexpr int TIL_KEYS = 128, TIL_BLOCKS = TIL_KEYS / OPS_BLOCK;
-constexpr int TIL_WARPS = 12, TIL_THREADS = TIL_WARPS * 32;
+constexpr int TIL_SOFT = 16, TIL_WARPS = TIL_SOFT + 4, TIL_THREADS = TIL_WARPS * 32;   // softmax; all
 constexpr long long TIL_WAIT_CYCLES = 1ll << 32;   // some two seconds
 
 template <int HD>
@@ -37,7 +40,8 @@ struct TilShape {
 
 struct TilShared {
   uint64_t q_full[2], s_full[2], p_full[2], o_full[2];
-  uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], v_land;
+  uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], v_land, unit_full[8];
+  float row[2][2][128];   // of a stream's rows, from either of their threads: maxima, or sums
   uint32_t tmem;
   int dead;
   int warp_sum[TIL_WARPS];
@@ -118,27 +122,37 @@ __device__ __forceinline__ uint32_t til_idesc(int n) {   // bf16 operands, fp32 
   return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
 
-// 32 lanes x 32 columns, without the wait: nothing may touch the registers before til_wait_ld() has named them.
-__device__ __forceinline__ void til_ld32(uint32_t taddr, uint32_t (&r)[32]) {
+// 32 lanes x 16 columns, without the wait: nothing may touch the registers before tmem_wait_ld_til() has named them.
+__device__ __forceinline__ void til_ld16(uint32_t taddr, uint32_t (&r)[16]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
-      "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
-        "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
-        "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(taddr)
       : "memory");
 }
 #define BLINK_RW8(r, i) "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7])
-__device__ __forceinline__ void tmem_wait_ld_til(uint32_t (&a)[32], uint32_t (&b)[32]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : BLINK_RW8(a, 0), BLINK_RW8(a, 8), BLINK_RW8(a, 16), BLINK_RW8(a, 24), BLINK_RW8(b, 0), BLINK_RW8(b, 8), BLINK_RW8(b, 16),
-                 BLINK_RW8(b, 24)
-               :
-               : "memory");
+__device__ __forceinline__ void tmem_wait_ld_til(uint32_t (&a)[16], uint32_t (&b)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : BLINK_RW8(a, 0), BLINK_RW8(a, 8), BLINK_RW8(b, 0), BLINK_RW8(b, 8) : : "memory");
 }
 #undef BLINK_RW8
+__device__ __forceinline__ void til_st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+// The two warps of 32 rows: a barrier, and whether any of their threads says so.
+__device__ __forceinline__ void til_pair_sync(int id) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ bool til_pair_any(int id, bool mine) {
+  uint32_t any;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\tbarrier.cta.red.or.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+               : "=r"(any)
+               : "r"(id), "r"((uint32_t)mine)
+               : "memory");
+  return any != 0;
+}
 __device__ __forceinline__ void til_st32(uint32_t taddr, const uint32_t* r) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, "
@@ -168,76 +182,71 @@ __device__ __forceinline__ float2 til_add2(float2 a, float2 b) {
 struct TilMask {
   int pos, window, sinks, first_block, n_sinks, from;   // of the row; of the tile's first block in the unit's list; of the list
 };
-// Bits of the keys of a quarter of the tile (two blocks) that the row sees.
-__device__ __forceinline__ uint32_t til_seen(const TilMask& k, int quarter) {
-  uint32_t bits = 0u;
+__device__ __forceinline__ void til_mask(uint32_t (&r)[16], const TilMask& k, int block) {   // block: of the tile
+  const int i = k.first_block + block;
+  const int at = (i < k.n_sinks ? i : k.from + i - k.n_sinks) * OPS_BLOCK;
+  const int hi = min(max(k.pos - at + 1, 0), OPS_BLOCK);                                  // keys up to its own
+  const int lo = k.window > 0 ? min(max(k.pos - k.window - at + 1, 0), OPS_BLOCK) : 0;    // keys before its window
+  const int sink = min(max(k.sinks - at, 0), OPS_BLOCK);
+  const uint32_t bits = ((1u << hi) - 1u) & (~((1u << lo) - 1u) | ((1u << sink) - 1u));
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    const int i = k.first_block + quarter * 2 + b;
-    const int at = (i < k.n_sinks ? i : k.from + i - k.n_sinks) * OPS_BLOCK;
-    const int hi = min(max(k.pos - at + 1, 0), OPS_BLOCK);                                  // keys up to its own
-    const int lo = k.window > 0 ? min(max(k.pos - k.window - at + 1, 0), OPS_BLOCK) : 0;    // keys before its window
-    const int sink = min(max(k.sinks - at, 0), OPS_BLOCK);
-    const uint32_t up_to = (1u << hi) - 1u, before = (1u << lo) - 1u, first = (1u << sink) - 1u;
-    bits |= (up_to & (~before | first)) << (b * OPS_BLOCK);
-  }
-  return bits;
-}
-__device__ __forceinline__ void til_mask(uint32_t (&r)[32], const TilMask& k, int quarter) {
-  const uint32_t bits = til_seen(k, quarter);
-#pragma unroll
-  for (int x = 0; x < 32; ++x)
+  for (int x = 0; x < 16; ++x)
     if (!(bits & (1u << x))) r[x] = 0xff800000u;
 }
 
-// One row of a score tile -> 64 words of probabilities (bf16 pairs), their sum, and the largest score.
+// Half a row of a score tile (blocks block0 .. block0 + 3) -> 32 words of probabilities (bf16 pairs), their sum, and the largest score.
 template <bool MASKED>
-__device__ __forceinline__ void til_probs(uint32_t t_s, float qscale, float neg, const TilMask& mask, uint32_t (&p)[64], float& mx, float& sum) {
+__device__ __forceinline__ void til_probs(uint32_t t_s, float qscale, float neg, const TilMask& mask, int block0, uint32_t (&p)[32], float& mx, float& sum) {
   const float2 scale2 = make_float2(qscale, qscale), neg2 = make_float2(neg, neg);
   float mx0 = -INFINITY, mx1 = -INFINITY;
   float2 s0 = make_float2(0.f, 0.f), s1 = s0;
-  auto quarter = [&](uint32_t (&r)[32], int k) {
-    if constexpr (MASKED) til_mask(r, mask, k);
+  auto part = [&](uint32_t (&r)[16], int k) {
+    if constexpr (MASKED) til_mask(r, mask, block0 + k);
 #pragma unroll
-    for (int x = 0; x < 32; x += 4) {
+    for (int x = 0; x < 16; x += 4) {
       mx0 = fmaxf(fmaxf(mx0, __uint_as_float(r[x])), __uint_as_float(r[x + 1]));
       mx1 = fmaxf(fmaxf(mx1, __uint_as_float(r[x + 2])), __uint_as_float(r[x + 3]));
     }
 #pragma unroll
-    for (int x = 0; x < 32; x += 2) {
+    for (int x = 0; x < 16; x += 2) {
       float2 e = til_fma2(make_float2(__uint_as_float(r[x]), __uint_as_float(r[x + 1])), scale2, neg2);
       e.x = attn_ex2(e.x);
       e.y = attn_ex2(e.y);
       if (x & 2) s1 = til_add2(s1, e); else s0 = til_add2(s0, e);
       const __nv_bfloat162 b2 = __floats2bfloat162_rn(e.x, e.y);
-      p[k * 16 + x / 2] = *reinterpret_cast<const uint32_t*>(&b2);
+      p[k * 8 + x / 2] = *reinterpret_cast<const uint32_t*>(&b2);
     }
   };
-  uint32_t va[32], vb[32], vc[32], vd[32];
-  til_ld32(t_s, va);
-  til_ld32(t_s + 32u, vb);
-  tmem_wait_ld_til(va, vb);
-  til_ld32(t_s + 64u, vc);
-  til_ld32(t_s + 96u, vd);
-  quarter(va, 0);
-  quarter(vb, 1);
-  tmem_wait_ld_til(vc, vd);
-  quarter(vc, 2);
-  quarter(vd, 3);
+  {
+    uint32_t va[16], vb[16];
+    til_ld16(t_s, va);
+    til_ld16(t_s + 16u, vb);
+    tmem_wait_ld_til(va, vb);
+    part(va, 0);
+    part(vb, 1);
+  }
+  {
+    uint32_t va[16], vb[16];
+    til_ld16(t_s + 32u, va);
+    til_ld16(t_s + 48u, vb);
+    tmem_wait_ld_til(va, vb);
+    part(va, 2);
+    part(vb, 3);
+  }
   mx = fmaxf(mx0, mx1);
   const float2 s = til_add2(s0, s1);
   sum = s.x + s.y;
 }
-// A first maximum: the largest score of a quarter of the row's first tile.
-__device__ __forceinline__ float til_max(uint32_t t_s, int quarter, bool masked, const TilMask& mask) {
-  uint32_t va[32], vb[32];
-  til_ld32(t_s + 32u * (uint32_t)quarter, va);
-  til_ld32(t_s + 32u * (uint32_t)quarter, vb);   // (the wait names two)
+// A first maximum: the largest score of one block of the row's first tile.
+__device__ __forceinline__ float til_max(uint32_t t_s, int block, bool masked, const TilMask& mask) {
+  uint32_t va[16], vb[16];
+  til_ld16(t_s + 16u * (uint32_t)block, va);
+  til_ld16(t_s + 16u * (uint32_t)block, vb);   // (the wait names two)
   tmem_wait_ld_til(va, vb);
-  if (masked) til_mask(va, mask, quarter);
+  if (masked) til_mask(va, mask, block);
   float m0 = -INFINITY, m1 = -INFINITY;
 #pragma unroll
-  for (int x = 0; x < 32; x += 4) {
+  for (int x = 0; x < 16; x += 4) {
     m0 = fmaxf(fmaxf(m0, __uint_as_float(va[x])), __uint_as_float(va[x + 1]));
     m1 = fmaxf(fmaxf(m1, __uint_as_float(va[x + 2])), __uint_as_float(va[x + 3]));
   }
@@ -253,7 +262,7 @@ struct alignas(16) TilUnit {
   int last;                // position of the last row
   int begin[2], end[2];    // tiles of each stream
 };
-constexpr int TIL_UNITS = 192;   // of a CTA, worked out by all threads before the first one
+constexpr int TIL_UNITS = 8;   // records of a CTA's units, used in turn: nobody is more than a few behind the warp that writes them
 
 template <int HD>
 __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap key_map,
@@ -266,13 +275,13 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
   __shared__ __align__(16) TilShared sh;
   const int w = (int)til_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   int* status = reinterpret_cast<int*>(a.ws);
-  const int P = 128 / a.pool.rep;                       // query rows of a stream
+  const int lr = 31 - __clz(a.pool.rep), P = 128 >> lr;   // query rows of a stream (1, 2, 4 or 8 heads each)
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < 2; ++s) {
-      til_init(&sh.q_full[s], 4);
+      til_init(&sh.q_full[s], TIL_SOFT / 2);
       til_init(&sh.s_full[s], 1);
-      til_init(&sh.p_full[s], 4);
+      til_init(&sh.p_full[s], TIL_SOFT / 2);
       til_init(&sh.o_full[s], 1);
     }
     for (int i = 0; i < 4; ++i) {
@@ -282,10 +291,11 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
       til_init(&sh.v_empty[i], 1);
     }
     til_init(&sh.v_land, 1);
+    for (int i = 0; i < TIL_UNITS; ++i) til_init(&sh.unit_full[i], 1);
     sh.dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (w == 8) {
+  if (w == TIL_SOFT) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(til_smem(&sh.tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -352,29 +362,42 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
     }
     return t;
   };
-  for (int i = threadIdx.x; i < TIL_UNITS && (long long)blockIdx.x + (long long)i * gridDim.x < n_units; i += TIL_THREADS) s_unit[i] = make_unit((int)(blockIdx.x + i * gridDim.x));
-  __syncthreads();
-  auto unit_of = [&](int u) {
-    const int i = (u - (int)blockIdx.x) / (int)gridDim.x;
-    return i < TIL_UNITS ? s_unit[i] : make_unit(u);
+  // the CTA's i-th unit, live[0] == 0: there is none
+  auto unit_of = [&](int i) {
+    const int slot = i % TIL_UNITS;
+    wait(&sh.unit_full[slot], (uint32_t)(i / TIL_UNITS) & 1u);
+    TilUnit t = s_unit[slot];
+    if (!ok) t.live[0] = 0;
+    return t;
+  };
+  // by one warp
+  auto hand_out = [&](int i, int u) {
+    TilUnit t;
+    if (u < n_units) t = make_unit(u);
+    else t.live[0] = 0;
+    if (lane == 0) {
+      s_unit[i % TIL_UNITS] = t;
+      til_arrive(&sh.unit_full[i % TIL_UNITS]);
+    }
+    __syncwarp();
   };
   auto tiles_of = [&](const TilUnit& t) { return max(t.end[0], t.end[1]); };   // (the first tile is one of stream 0, which always has rows)
 
-  if (w < 8) {
+  if (w < TIL_SOFT) {
     // ---- softmax ----
-    const int s = w >> 2, q = w & 3, m = q * 32 + lane, rep = a.pool.rep;
+    const int s = w >> 3, half = (w >> 2) & 1, q = w & 3, m = q * 32 + lane, rep = 1 << lr, pair = 1 + s * 4 + q;
     const uint32_t t_row = (uint32_t)(q * 32) << 16;
-    const uint32_t t_s = tmem + (uint32_t)s * 128u + t_row, t_o = tmem + 256u + (uint32_t)(s * HD) + t_row;
+    const uint32_t t_s = tmem + (uint32_t)(s * 128) + t_row, t_o = tmem + 256u + (uint32_t)(s * HD + half * (HD / 2)) + t_row;
     const uint32_t b_q = til_smem(base) + S::Q + s * S::TILE;
     uint32_t n_s = 0, n_o = 0;
     auto load_q = [&](const TilUnit& t) {
       constexpr int CH = HD / 8;   // 16-byte pieces of a row
 #pragma unroll 4
-      for (int k = 0; k < CH; ++k) {
-        const int i = k * 128 + (int)(threadIdx.x & 127), row = i / CH, ck = i % CH;
-        const int r = row / rep;
+      for (int k = 0; k < CH / 2; ++k) {
+        const int i = k * 256 + (int)(threadIdx.x & 255), row = i / CH, ck = i % CH;
+        const int r = row >> lr;
         const bool live = r < t.live[s];
-        const char* src = static_cast<const char*>(a.q) + ((long long)(t.row + (live ? s * P + r : 0)) * a.q_stride + (t.h * rep + row % rep) * HD + ck * 8) * 2;
+        const char* src = static_cast<const char*>(a.q) + ((long long)(t.row + (live ? s * P + r : 0)) * a.q_stride + ((t.h << lr) + (row & (rep - 1))) * HD + ck * 8) * 2;
         const uint32_t dst = b_q + (ck >> 3) * 16384 + row * 128 + (((ck & 7) ^ (row & 7)) << 4);
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16u : 0u) : "memory");
       }
@@ -383,121 +406,149 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
     auto q_there = [&]() {
       asm volatile("cp.async.wait_group 0;" ::: "memory");
       til_proxy_fence();
-      til_fence_before();   // (what was read of the accumulator comes before its next use)
       __syncwarp();
       if (lane == 0) til_arrive(&sh.q_full[s]);
     };
-    int u = blockIdx.x;
-    TilUnit t, next;
-    if (u < n_units) {
-      t = unit_of(u);
-      if (t.live[s]) {
-        load_q(t);
-        q_there();
+    // (the two warps of a pair go on together or not at all: a barrier of theirs has no limit)
+    auto together = [&](TilUnit& t) {
+      if (til_pair_any(pair, !ok)) {
+        ok = false;
+        t.live[0] = 0;
       }
+    };
+    TilUnit t = unit_of(0);
+    together(t);
+    if (t.live[0] && t.live[s]) {
+      load_q(t);
+      q_there();
     }
-    while (u < n_units) {
-      const int un = u + (int)gridDim.x;
-      if (un < n_units) next = unit_of(un);
-      const bool more = un < n_units && next.live[s] > 0;
+#pragma unroll 1
+    for (int u = 0; t.live[0]; ++u) {
+      bool more = false;   // a next unit, in which the stream has rows
       if (t.live[s]) {
-        const int r = m / rep;
+        const int r = m >> lr;
         TilMask mask;
         mask.pos = r < t.live[s] ? t.pos + s * P + r : -1;
         mask.window = a.window;
         mask.sinks = a.sinks;
         mask.n_sinks = t.span.sinks;
         mask.from = t.span.from;
-        const int p_lo = t.pos + s * P + (q * 32) / rep, p_hi = t.pos + s * P + (q * 32 + 31) / rep;
+        const int p_lo = t.pos + s * P + ((q * 32) >> lr), p_hi = t.pos + s * P + ((q * 32 + 31) >> lr);
+        const int begin = t.begin[s], end = t.end[s];
+        const int t_row0 = t.row + s * P, t_head = (t.h << lr) + (m & (rep - 1));
+        const bool mine = r < t.live[s];
         float mx_used = -INFINITY, l = 0.f;
-        for (int j = t.begin[s]; j < t.end[s]; ++j) {
+#pragma unroll 1
+        for (int j = begin; j < end; ++j) {
           mask.first_block = j * TIL_BLOCKS;
           const int i0 = mask.first_block, i1 = i0 + TIL_BLOCKS - 1;
           const int lowest = i1 < mask.n_sinks ? a.window + p_hi : (mask.from + max(0, i0 - mask.n_sinks)) * OPS_BLOCK;   // of its blocks behind the sinks
           const int highest = (mask.from + i1 - mask.n_sinks) * OPS_BLOCK + OPS_BLOCK - 1;
-          const bool masked = highest > p_lo || (a.window > 0 && lowest <= p_hi - a.window) || (i0 < mask.n_sinks && (a.sinks & (OPS_BLOCK - 1)));
+          const bool cut = a.window > 0 && lowest <= p_hi - a.window;
+          const bool masked = highest > p_lo || cut || (i0 < mask.n_sinks && (a.sinks & (OPS_BLOCK - 1)));
           wait(&sh.s_full[s], n_s & 1u);
           ++n_s;
           til_fence_after();
-          // a row's first maximum: from the keys next to its window's end where its first tile is cut by the window, else from the first ones
-          if (j == t.begin[s]) mx_used = til_max(t_s, a.window > 0 && lowest <= p_hi - a.window ? 3 : 0, masked, mask) * a.qscale;
-          if (j + 1 == t.end[s] && more) load_q(next);   // (its last scores are complete: the queries have been read)
-          uint32_t p[64];
+          if (j == begin) {   // a first maximum: from keys next to the window's end where the tile is cut by the window, else from the first ones
+            const float x = til_max(t_s, (cut ? 6 : 0) + half, masked, mask) * a.qscale;
+            sh.row[s][half][m] = x;
+            til_pair_sync(pair);
+            mx_used = fmaxf(x, sh.row[s][half ^ 1][m]);
+          }
+          if (j + 1 == end) {   // the last scores are complete: the queries have been read
+            t = unit_of(u + 1);
+            more = t.live[0] > 0 && t.live[s] > 0;
+            if (more) load_q(t);
+          }
+          uint32_t p[32];
           float sum;
 #pragma unroll 1
           while (true) {
             float mx;
             const float neg = mx_used == -INFINITY ? 0.f : -mx_used;
-            if (masked) til_probs<true>(t_s, a.qscale, neg, mask, p, mx, sum);
-            else til_probs<false>(t_s, a.qscale, neg, mask, p, mx, sum);
+            if (masked) til_probs<true>(t_s + (uint32_t)half * 64u, a.qscale, neg, mask, half * 4, p, mx, sum);
+            else til_probs<false>(t_s + (uint32_t)half * 64u, a.qscale, neg, mask, half * 4, p, mx, sum);
             mx *= a.qscale;
-            if (!__any_sync(0xffffffffu, mx > mx_used + 8.f)) break;
-            const float top = fmaxf(mx_used, mx);
+            if (!til_pair_any(pair, mx > mx_used + 8.f)) break;   // (and neither's probabilities go over scores that the other has yet to read)
+            sh.row[s][half][m] = mx;
+            til_pair_sync(pair);
+            const float top = fmaxf(mx_used, fmaxf(mx, sh.row[s][half ^ 1][m]));
             const float f = top == -INFINITY ? 1.f : attn_ex2(mx_used - top);
             mx_used = top;
             l *= f;
-            if (j > t.begin[s]) {   // the stream's accumulator is complete: its MMAs came before these scores'
+            if (j > begin) {   // the stream's accumulator is complete: its MMAs came before these scores'
 #pragma unroll 1
-              for (int k = 0; k < HD; k += 64) {
-                uint32_t x[32], y[32];
-                til_ld32(t_o + (uint32_t)k, x);
-                til_ld32(t_o + (uint32_t)k + 32u, y);
+              for (int k = 0; k < HD / 2; k += 32) {
+                uint32_t x[16], y[16];
+                til_ld16(t_o + (uint32_t)k, x);
+                til_ld16(t_o + (uint32_t)k + 16u, y);
                 tmem_wait_ld_til(x, y);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
+                for (int i = 0; i < 16; ++i) {
                   x[i] = __float_as_uint(__uint_as_float(x[i]) * f);
                   y[i] = __float_as_uint(__uint_as_float(y[i]) * f);
                 }
-                til_st32(t_o + (uint32_t)k, x);
-                til_st32(t_o + (uint32_t)k + 32u, y);
+                til_st16(t_o + (uint32_t)k, x);
+                til_st16(t_o + (uint32_t)k + 16u, y);
               }
               til_wait_st();
             }
+            til_pair_sync(pair);   // (both have read the other's)
           }
           l += sum;
-          til_st32(t_s, p);
-          til_st32(t_s + 32u, p + 32);
+          til_st32(t_s + (uint32_t)half * 32u, p);
           til_wait_st();
           til_fence_before();
           __syncwarp();
           if (lane == 0) til_arrive(&sh.p_full[s]);
         }
         if (more) q_there();
+        sh.row[s][half][m] = l;
+        til_pair_sync(pair);
+        l += sh.row[s][half ^ 1][m];
+        const float inv = l > 0.f ? __fdividef(1.0f, l) : 0.f;
         wait(&sh.o_full[s], n_o & 1u);
         ++n_o;
         til_fence_after();
-        const float inv = l > 0.f ? __fdividef(1.0f, l) : 0.f;
-        const bool store = r < t.live[s] && ok;
-        char* dst = static_cast<char*>(a.out) + ((long long)(t.row + s * P + (store ? r : 0)) * a.out_stride + (t.h * rep + m % rep) * HD) * 2;
+        const bool store = mine && ok;
+        char* dst = static_cast<char*>(a.out) + ((long long)(t_row0 + (store ? r : 0)) * a.out_stride + t_head * HD + half * (HD / 2)) * 2;
 #pragma unroll 1
-        for (int k = 0; k < HD; k += 64) {
-          uint32_t x[32], y[32];
-          til_ld32(t_o + (uint32_t)k, x);
-          til_ld32(t_o + (uint32_t)k + 32u, y);
+        for (int k = 0; k < HD / 2; k += 32) {
+          uint32_t x[16], y[16];
+          til_ld16(t_o + (uint32_t)k, x);
+          til_ld16(t_o + (uint32_t)k + 16u, y);
           tmem_wait_ld_til(x, y);
-          auto put = [&](const uint32_t(&v)[32], int at) {
+          auto put = [&](const uint32_t(&v)[16], int at) {   // a lane's row lies alone: 32 bytes at a time, where they may
+            uint32_t o[8];
 #pragma unroll
-            for (int i = 0; i < 32; i += 8) {
-              uint32_t o[4];
-#pragma unroll
-              for (int c = 0; c < 4; ++c) {
-                const __nv_bfloat162 b2 = __floats2bfloat162_rn(__uint_as_float(v[i + 2 * c]) * inv, __uint_as_float(v[i + 2 * c + 1]) * inv);
-                o[c] = *reinterpret_cast<const uint32_t*>(&b2);
-              }
-              if (store) *reinterpret_cast<uint4*>(dst + (at + i) * 2) = make_uint4(o[0], o[1], o[2], o[3]);
+            for (int c = 0; c < 8; ++c) {
+              const __nv_bfloat162 b2 = __floats2bfloat162_rn(__uint_as_float(v[2 * c]) * inv, __uint_as_float(v[2 * c + 1]) * inv);
+              o[c] = *reinterpret_cast<const uint32_t*>(&b2);
+            }
+            if (store && a.out_32) {
+              asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + at * 2), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]), "r"(o[4]),
+                           "r"(o[5]), "r"(o[6]), "r"(o[7])
+                           : "memory");
+            } else if (store) {
+              *reinterpret_cast<uint4*>(dst + at * 2) = make_uint4(o[0], o[1], o[2], o[3]);
+              *reinterpret_cast<uint4*>(dst + at * 2 + 16) = make_uint4(o[4], o[5], o[6], o[7]);
             }
           };
           put(x, k);
-          put(y, k + 32);
+          put(y, k + 16);
         }
-      } else if (more) {
-        load_q(next);
-        q_there();
+        til_fence_before();      // (before the accumulator's next use: the next probabilities' arrival)
+        together(t);             // (and both have read the other's sum)
+      } else {
+        t = unit_of(u + 1);
+        together(t);
+        if (t.live[0] && t.live[s]) {
+          load_q(t);
+          q_there();
+        }
       }
-      t = next;
-      u = un;
     }
-  } else if (w == 8) {
+  } else if (w == TIL_SOFT) {
     // ---- MMAs ----
     // (what they are issued with comes from uniform registers, and their loops turn on uniform values: otherwise an MMA's operands are moved first
     // and its warp is taken for a diverged one, some 100 cycles each, more than the tensor core takes for it)
@@ -505,8 +556,9 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
     const uint32_t b0 = til_uniform(til_smem(base));
     uint32_t n_tile = 0, n_q0 = 0, n_q1 = 0, n_p0 = 0, n_p1 = 0;
 #pragma unroll 1
-    for (int u = blockIdx.x; u < n_units && ok; u += (int)gridDim.x) {
+    for (int u = 0; ok; ++u) {
       const TilUnit t = unit_of(u);
+      if (til_uniform((uint32_t)t.live[0]) == 0u) break;
       const int begin1 = (int)til_uniform((uint32_t)t.begin[1]), end0 = (int)til_uniform((uint32_t)t.end[0]), end1 = (int)til_uniform((uint32_t)t.end[1]);
       const int tiles = max(end0, end1);   // (stream 0 takes tiles 0 .. end0 - 1, stream 1 begin1 .. end1 - 1, which is none where it has no rows)
       auto scores = [&](int s, int j) {
@@ -561,8 +613,8 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
     }
   } else {
     // ---- copies ----
-    const int part = w - 9;   // 0, 1: halves of the keys; 2: values
-    if (part == 2 || part < S::SLABS) {
+    const int part = w - TIL_SOFT - 1;   // 0, 1: halves of the keys; 2: values
+    if (part == 2 || part < S::SLABS) {   // (head_dim 64: the second has nothing to do)
       uint64_t policy;
       asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
       const CUtensorMap* map = part == 2 ? &value_map : &key_map;
@@ -572,15 +624,12 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
         const int i = min(j * TIL_BLOCKS + (lane & 7), t.span.n - 1);
         return t.last >= 0 ? a.table[(long long)t.req * a.stride + (i < t.span.sinks ? i : t.span.from + i - t.span.sinks)] : -1;
       };
-      TilUnit t, next;
-      int id = 0, next_id = 0;
-      if ((int)blockIdx.x < n_units) {
-        next = unit_of((int)blockIdx.x);
-        next_id = block_id(next, 0);
-      }
-      for (int u = blockIdx.x; u < n_units && ok; u += (int)gridDim.x) {
-        t = next;
-        id = next_id;
+      if (part == 0) hand_out(0, (int)blockIdx.x);
+#pragma unroll 1
+      for (int u = 0; ok; ++u) {
+        const TilUnit t = unit_of(u);
+        if (!t.live[0]) break;
+        int id = block_id(t, 0);
         const int tiles = tiles_of(t);
 #pragma unroll 1
         for (int j = 0; j < tiles; ++j) {
@@ -590,6 +639,12 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
           uint64_t* empty = part == 2 ? &sh.v_empty[slot] : &sh.k_empty[slot];
           if (use > 0) wait(empty, (use - 1u) & 1u);
           if (!ok) break;
+          if (part == 0 && j == max(0, tiles - 2)) {   // the next unit, late, so that the CTAs end together; the counter was zeroed by a kernel before this one
+            if (u == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
+            int next = 0;
+            if (lane == 0) next = (int)gridDim.x + atomicAdd(status + 1, 1);
+            hand_out(u + 1, __shfl_sync(0xffffffffu, next, 0));
+          }
           const uint32_t dst = til_smem(base) + (part == 2 ? S::V : S::K + part * 16384) + slot * S::TILE;
           bool clean = true;   // some row sees every key of the tile, so that its values are numbers
           if (part == 2) {
@@ -623,10 +678,6 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
             __syncwarp();
             if (lane == 0) til_arrive(&sh.v_full[slot]);
           }
-          if (j == 0 && u + (int)gridDim.x < n_units) {   // (the copies are on their way)
-            next = unit_of(u + (int)gridDim.x);
-            next_id = block_id(next, 0);
-          }
         }
         n_tile += (uint32_t)tiles;
       }
@@ -640,7 +691,7 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
   asm volatile("cp.async.wait_all;" ::: "memory");
   til_fence_before();
   __syncthreads();
-  if (w == 8) {
+  if (w == TIL_SOFT) {
     til_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
