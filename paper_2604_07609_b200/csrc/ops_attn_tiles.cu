@@ -5,10 +5,11 @@
 // blocks of the unit, sinks first, eight to a tile, whatever lies between them.
 //
 //   warps 0-7 | 8-15  softmax of stream 0 | 1, two threads per row (64 keys of a tile each): scores from TMEM, probabilities back to TMEM
-//                     over the scores
-//   warp 16           issues the MMAs: scores = Q K^T (operands in shared memory), output += P V (P in TMEM, V as it lies in the cache)
-//   warps 17, 18 | 19 copies of the keys' halves | of the values: a copy takes its thread some 100 cycles, a tile has 24.  Warp 17 also
-//                     hands out the units, heaviest of a request first, from a counter
+//                     over the same scores
+//   warps 16 | 17     issue the MMAs of stream 0 | 1: scores = Q K^T (operands in shared memory), output += P V (P in TMEM, V as it lies in the
+//                     cache)
+//   warps 18 | 19     copies of the keys | of the values, eight a tile (with 24, four of a KB or two a block, these warps were the slowest: 4096
+//                     rows 170 us).  Warp 18 also hands out the units, heaviest of a request first, from a counter
 //
 // While one stream is in its softmax the tensor core works for the other; the next scores of a stream are issued behind its output MMAs, so a
 // stream's scores being complete also says that its accumulator is.  The maximum in use, the same for both threads of a row, follows the
@@ -27,12 +28,12 @@
 namespace blink {
 
 constexpr int TIL_KEYS = 128, TIL_BLOCKS = TIL_KEYS / OPS_BLOCK;
-constexpr int TIL_SOFT = 16, TIL_WARPS = TIL_SOFT + 4, TIL_THREADS = TIL_WARPS * 32;   // softmax; all
+constexpr int TIL_SOFT = 16, TIL_COPY = TIL_SOFT + 1, TIL_K = 1, TIL_WARPS = TIL_COPY + TIL_K + 1, TIL_THREADS = TIL_WARPS * 32;   // softmax; first of the copies, of them for keys; all
 constexpr long long TIL_WAIT_CYCLES = 1ll << 32;   // some two seconds
 
 template <int HD>
 struct TilShape {
-  static constexpr int SLABS = HD / 64;                 // of 64 dims (128-byte rows)
+  static constexpr int SLABS = HD / 64, GROUP = SLABS * 1024;   // slabs of 64 dims (128-byte rows); bytes of eight keys
   static constexpr int TILE = TIL_KEYS * HD * 2;        // bytes of 128 rows
   static constexpr int RING = 131072 / (2 * TILE);      // tiles of keys, and of values, in shared memory
   static constexpr int Q = 0, K = 2 * TILE, V = K + RING * TILE, END = V + RING * TILE;
@@ -92,10 +93,11 @@ __device__ __forceinline__ void til_fence_before() { asm volatile("tcgen05.fence
 __device__ __forceinline__ void til_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void til_proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// 16 keys of the pool: 64 dims from x on, or (values) all dims as slabs of 64 one behind the other
-__device__ __forceinline__ void til_copy(uint32_t dst, const CUtensorMap* map, int row, int slab, int plane, uint64_t* bar, uint64_t policy) {
-  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4, %5}], [%6], %7;" ::"r"(dst),
-               "l"(map), "r"(0), "r"(row), "r"(slab), "r"(plane), "r"(til_smem(bar)), "l"(policy)
+// A block of the cache (16 keys, all dims): two groups of eight keys, each as slabs of 64 dims, 1024 bytes a slab.  So one copy, and
+// groups are the same distance apart in a block and between blocks, which is what an operand of 128 keys needs.
+__device__ __forceinline__ void til_copy(uint32_t dst, const CUtensorMap* map, int group, int plane, uint64_t* bar, uint64_t policy) {
+  asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %2, %2, %3, %4}], [%5], %6;" ::"r"(dst),
+               "l"(map), "r"(0), "r"(group), "r"(plane), "r"(til_smem(bar)), "l"(policy)
                : "memory");
 }
 // D (+)= A B^T, both in shared memory
@@ -113,10 +115,10 @@ __device__ __forceinline__ void til_mma_tmem(uint32_t d, uint32_t a, uint64_t b,
 __device__ __forceinline__ void til_commit(uint64_t* bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(til_smem(bar)) : "memory");
 }
-// Shared-memory operands with 128-byte swizzle.  K-major (128-byte rows of 64 bf16 along K): groups of eight rows 1024 bytes apart.
-// MN-major (128-byte rows of 64 along N): groups of eight K-rows 1024 bytes apart, the next 64 along N `slab` bytes on.
-__device__ __forceinline__ uint64_t til_desc(uint32_t saddr, uint32_t slab) {
-  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)(slab >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+// Shared-memory operands with 128-byte swizzle.  K-major (128-byte rows of 64 bf16 along K): groups of eight rows `group` bytes apart.
+// MN-major (128-byte rows of 64 along N): groups of eight K-rows `group` bytes apart, the next 64 along N `slab` bytes on.
+__device__ __forceinline__ uint64_t til_desc(uint32_t saddr, uint32_t slab, uint32_t group) {
+  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)(slab >> 4) << 16 | (uint64_t)(group >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
 __device__ __forceinline__ uint32_t til_idesc(int n) {   // bf16 operands, fp32 accumulator, M = 128
   return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
@@ -217,22 +219,18 @@ __device__ __forceinline__ void til_probs(uint32_t t_s, float qscale, float neg,
       p[k * 8 + x / 2] = *reinterpret_cast<const uint32_t*>(&b2);
     }
   };
-  {
-    uint32_t va[16], vb[16];
-    til_ld16(t_s, va);
-    til_ld16(t_s + 16u, vb);
-    tmem_wait_ld_til(va, vb);
-    part(va, 0);
-    part(vb, 1);
-  }
-  {
-    uint32_t va[16], vb[16];
-    til_ld16(t_s + 32u, va);
-    til_ld16(t_s + 48u, vb);
-    tmem_wait_ld_til(va, vb);
-    part(va, 2);
-    part(vb, 3);
-  }
+  // (a wait for TMEM takes some 400 cycles: what comes second is on its way while the first is worked on)
+  uint32_t va[16], vb[16], vc[16], vd[16];
+  til_ld16(t_s, va);
+  til_ld16(t_s + 16u, vb);
+  tmem_wait_ld_til(va, vb);
+  til_ld16(t_s + 32u, vc);
+  part(va, 0);
+  til_ld16(t_s + 48u, vd);
+  part(vb, 1);
+  tmem_wait_ld_til(vc, vd);
+  part(vc, 2);
+  part(vd, 3);
   mx = fmaxf(mx0, mx1);
   const float2 s = til_add2(s0, s1);
   sum = s.x + s.y;
@@ -265,8 +263,7 @@ struct alignas(16) TilUnit {
 constexpr int TIL_UNITS = 8;   // records of a CTA's units, used in turn: nobody is more than a few behind the warp that writes them
 
 template <int HD>
-__global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap key_map,
-                                                                          const __grid_constant__ CUtensorMap value_map) {
+__global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap map) {
   using S = TilShape<HD>;
   extern __shared__ char s_raw[];
   char* base = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(s_raw) + 1023) & ~(uintptr_t)1023);
@@ -285,7 +282,7 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
       til_init(&sh.o_full[s], 1);
     }
     for (int i = 0; i < 4; ++i) {
-      til_init(&sh.k_full[i], S::SLABS);
+      til_init(&sh.k_full[i], TIL_K);
       til_init(&sh.k_empty[i], 1);
       til_init(&sh.v_full[i], 1);
       til_init(&sh.v_empty[i], 1);
@@ -469,7 +466,7 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
             if (masked) til_probs<true>(t_s + (uint32_t)half * 64u, a.qscale, neg, mask, half * 4, p, mx, sum);
             else til_probs<false>(t_s + (uint32_t)half * 64u, a.qscale, neg, mask, half * 4, p, mx, sum);
             mx *= a.qscale;
-            if (!til_pair_any(pair, mx > mx_used + 8.f)) break;   // (and neither's probabilities go over scores that the other has yet to read)
+            if (!til_pair_any(pair, mx > mx_used + 8.f)) break;
             sh.row[s][half][m] = mx;
             til_pair_sync(pair);
             const float top = fmaxf(mx_used, fmaxf(mx, sh.row[s][half ^ 1][m]));
@@ -496,7 +493,7 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
             til_pair_sync(pair);   // (both have read the other's)
           }
           l += sum;
-          til_st32(t_s + (uint32_t)half * 32u, p);
+          til_st32(t_s + (uint32_t)half * 64u, p);
           til_wait_st();
           til_fence_before();
           __syncwarp();
@@ -548,7 +545,7 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
         }
       }
     }
-  } else if (w == TIL_SOFT) {
+  } else if (w < TIL_COPY) {
     // ---- MMAs ----
     // (what they are issued with comes from uniform registers, and their loops turn on uniform values: otherwise an MMA's operands are moved first
     // and its warp is taken for a diverged one, some 100 cycles each, more than the tensor core takes for it)
@@ -566,12 +563,12 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
         wait(&sh.k_full[slot], (n / S::RING) & 1u);
         if (!ok) return;
         til_fence_after();
-        const uint64_t dq = til_desc(b0 + S::Q + s * S::TILE, 16), dk = til_desc(b0 + S::K + slot * S::TILE, 16);
+        const uint64_t dq = til_desc(b0 + S::Q + s * S::TILE, 16, 1024), dk = til_desc(b0 + S::K + slot * S::TILE, 16, S::GROUP);
         const bool last = s == 1 || j < begin1 || j >= end1;
         if (til_elect()) {
 #pragma unroll
           for (int i = 0; i < HD / 16; ++i)
-            til_mma(tmem + (uint32_t)s * 128u, dq + (uint64_t)((i >> 2) * 1024 + (i & 3) * 2), dk + (uint64_t)((i >> 2) * 1024 + (i & 3) * 2), idesc_s, i ? 1u : 0u);
+            til_mma(tmem + (uint32_t)s * 128u, dq + (uint64_t)((i >> 2) * 1024 + (i & 3) * 2), dk + (uint64_t)((i >> 2) * 64 + (i & 3) * 2), idesc_s, i ? 1u : 0u);
           til_commit(&sh.s_full[s]);
           if (last) til_commit(&sh.k_empty[slot]);
         }
@@ -583,14 +580,14 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
         wait(&sh.v_full[slot], (n / S::RING) & 1u);
         if (!ok) return;
         til_fence_after();
-        const uint64_t dv = til_desc(b0 + S::V + slot * S::TILE, 2048);
+        const uint64_t dv = til_desc(b0 + S::V + slot * S::TILE, 1024, S::GROUP);
         const uint32_t keep = j > (s ? begin1 : 0) ? 1u : 0u;
         const bool end = j + 1 == (s ? end1 : end0), last = s == 1 || j < begin1 || j >= end1;
         if (til_elect()) {
 #pragma unroll
           for (int i = 0; i < TIL_BLOCKS; ++i)   // 16 keys each, a block of the cache
-            til_mma_tmem(tmem + 256u + (uint32_t)(s * HD), tmem + (uint32_t)s * 128u + (uint32_t)(i * 8), dv + (uint64_t)(i * (S::TILE / TIL_BLOCKS / 16)), idesc_o,
-                         i ? 1u : keep);
+            til_mma_tmem(tmem + 256u + (uint32_t)(s * HD), tmem + (uint32_t)s * 128u + (uint32_t)((i >> 2) * 64 + (i & 3) * 8),
+                         dv + (uint64_t)(i * (S::TILE / TIL_BLOCKS / 16)), idesc_o, i ? 1u : keep);
           if (end) til_commit(&sh.o_full[s]);
           if (last) til_commit(&sh.v_empty[slot]);
         }
@@ -613,12 +610,12 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
     }
   } else {
     // ---- copies ----
-    const int part = w - TIL_SOFT - 1;   // 0, 1: halves of the keys; 2: values
-    if (part == 2 || part < S::SLABS) {   // (head_dim 64: the second has nothing to do)
+    const int part = w - TIL_COPY;   // 0 .. TIL_K - 1: keys
+    const bool values = part == TIL_K;
+    {
       uint64_t policy;
       asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
-      const CUtensorMap* map = part == 2 ? &value_map : &key_map;
-      const int rows_block = a.pool.Hkv * OPS_BLOCK, none = (int)a.pool.n_blocks * rows_block;   // (a row behind the pool: zeros)
+      const int none = (int)a.pool.n_blocks * a.pool.Hkv * 2;   // (a group behind the pool: zeros)
       uint32_t n_tile = 0, n_land = 0;
       auto block_id = [&](const TilUnit& t, int j) {   // lane: block of the tile; behind the list the last one again (nobody sees it there)
         const int i = min(j * TIL_BLOCKS + (lane & 7), t.span.n - 1);
@@ -633,10 +630,10 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
         const int tiles = tiles_of(t);
 #pragma unroll 1
         for (int j = 0; j < tiles; ++j) {
-          const int mine = (unsigned)id < (unsigned)a.pool.n_blocks ? id * rows_block + t.h * OPS_BLOCK : none;
+          const int mine = (unsigned)id < (unsigned)a.pool.n_blocks ? (id * a.pool.Hkv + t.h) * 2 : none;
           if (j + 1 < tiles) id = block_id(t, j + 1);
           const uint32_t n = n_tile + (uint32_t)j, slot = n % S::RING, use = n / S::RING;
-          uint64_t* empty = part == 2 ? &sh.v_empty[slot] : &sh.k_empty[slot];
+          uint64_t* empty = values ? &sh.v_empty[slot] : &sh.k_empty[slot];
           if (use > 0) wait(empty, (use - 1u) & 1u);
           if (!ok) break;
           if (part == 0 && j == max(0, tiles - 2)) {   // the next unit, late, so that the CTAs end together; the counter was zeroed by a kernel before this one
@@ -645,23 +642,25 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
             if (lane == 0) next = (int)gridDim.x + atomicAdd(status + 1, 1);
             hand_out(u + 1, __shfl_sync(0xffffffffu, next, 0));
           }
-          const uint32_t dst = til_smem(base) + (part == 2 ? S::V : S::K + part * 16384) + slot * S::TILE;
+          const uint32_t dst = til_smem(base) + (values ? S::V : S::K) + slot * S::TILE;
           bool clean = true;   // some row sees every key of the tile, so that its values are numbers
-          if (part == 2) {
+          if (values) {
             const int i0 = j * TIL_BLOCKS, i1 = i0 + TIL_BLOCKS - 1;
             clean = t.last >= (t.span.from + i1 - t.span.sinks) * OPS_BLOCK + OPS_BLOCK - 1 && !(i0 < t.span.sinks && (a.sinks & (OPS_BLOCK - 1))) &&
                     !(a.window > 0 && i1 >= t.span.sinks && (t.span.from + max(0, i0 - t.span.sinks)) * OPS_BLOCK <= t.pos - a.window);
           }
-          uint64_t* full = part < 2 ? &sh.k_full[slot] : clean ? &sh.v_full[slot] : &sh.v_land;
-          if (til_elect()) til_expect(full, part < 2 ? 16384u : (uint32_t)S::TILE);
+          uint64_t* full = !values ? &sh.k_full[slot] : clean ? &sh.v_full[slot] : &sh.v_land;
+          if (til_elect()) til_expect(full, (uint32_t)(values ? S::TILE : S::TILE / TIL_K));
           __syncwarp();
 #pragma unroll
-          for (int i = 0; i < TIL_BLOCKS; ++i) {
-            const int row = (int)til_uniform((uint32_t)__shfl_sync(0xffffffffu, mine, i));
-            if (til_elect()) til_copy(dst + i * (part < 2 ? 2048 : S::TILE / TIL_BLOCKS), map, row, part < 2 ? part : 0, part == 2, full, policy);
+          for (int k = 0; k < TIL_BLOCKS; ++k) {
+            if (!values && k >= TIL_BLOCKS / TIL_K) break;
+            const int i = values ? k : part * (TIL_BLOCKS / TIL_K) + k;
+            const int group = (int)til_uniform((uint32_t)__shfl_sync(0xffffffffu, mine, i));
+            if (til_elect()) til_copy(dst + i * (S::TILE / TIL_BLOCKS), &map, group, values, full, policy);
             __syncwarp();
           }
-          if (part == 2 && !clean) {   // what no row sees may be anything, and 0 x NaN is not 0
+          if (values && !clean) {   // what no row sees may be anything, and 0 x NaN is not 0
             wait(&sh.v_land, n_land & 1u);
             ++n_land;
             char* v = base + S::V + slot * S::TILE;
@@ -670,9 +669,9 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
               const int i = j * TIL_BLOCKS + x / OPS_BLOCK;
               const int at = (i < t.span.sinks ? i : t.span.from + i - t.span.sinks) * OPS_BLOCK + x % OPS_BLOCK;
               if (at <= t.last && (a.window == 0 || at > t.pos - a.window || at < a.sinks)) continue;
-              char* to = v + (x / OPS_BLOCK) * (S::TILE / TIL_BLOCKS) + (x % OPS_BLOCK) * 128;
+              char* to = v + (x / 8) * S::GROUP + (x % 8) * 128;
 #pragma unroll
-              for (int c = 0; c < HD / 8; ++c) *reinterpret_cast<uint4*>(to + (c >> 3) * 2048 + ((c + lane) & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+              for (int c = 0; c < HD / 8; ++c) *reinterpret_cast<uint4*>(to + (c >> 3) * 1024 + ((c + lane) & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
             }
             til_proxy_fence();
             __syncwarp();
@@ -716,18 +715,17 @@ static int tiles_run(const AttnArgs& a, int sms, int64_t most_units, void* strea
   using S = TilShape<HD>;
   const TilEncode encode = til_encode();
   if (!encode) return BLINK_ECUDA;
-  // the layer's keys and values as {64 dims, rows of a head's block, halves, keys | values}; a copy brings 16 keys, of one half (keys) or both (values)
-  const cuuint64_t rows = (cuuint64_t)a.pool.n_blocks * a.pool.Hkv * OPS_BLOCK;
-  const cuuint64_t dims[4] = {64, rows, HD / 64, 2}, strides[3] = {HD * 2, 128, rows * HD * 2};
-  const cuuint32_t key_box[4] = {64, OPS_BLOCK, 1, 1}, value_box[4] = {64, OPS_BLOCK, HD / 64, 1}, one[4] = {1, 1, 1, 1};
-  CUtensorMap maps[2];
-  for (int i = 0; i < 2; ++i)
-    if (encode(&maps[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, a.pool.k, dims, strides, i ? value_box : key_box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-      return BLINK_ECUDA;
+  // the layer's keys and values as {64 dims, 8 keys, slabs of dims, groups of 8 keys, keys | values}; a copy brings two groups
+  const cuuint64_t groups = (cuuint64_t)a.pool.n_blocks * a.pool.Hkv * 2;
+  const cuuint64_t dims[5] = {64, 8, HD / 64, groups, 2}, strides[4] = {HD * 2, 128, 8 * HD * 2, groups * 8 * HD * 2};
+  const cuuint32_t box[5] = {64, 8, HD / 64, 2, 1}, one[5] = {1, 1, 1, 1, 1};
+  CUtensorMap map;
+  if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, a.pool.k, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return BLINK_ECUDA;
   const size_t smem = (size_t)S::END + 1024 + TIL_UNITS * sizeof(TilUnit) + (size_t)(a.n + 1) * 4;
   const int64_t grid = most_units < sms ? most_units : sms;
-  return ops_launch(blink_attn_tiles_kernel<HD>, grid, TIL_THREADS, smem, stream, 0, true, a, maps[0], maps[1]);
+  return ops_launch(blink_attn_tiles_kernel<HD>, grid, TIL_THREADS, smem, stream, 0, true, a, map);
 }
 
 int attn_tiles(const AttnArgs& a, int sms, void* stream) {
