@@ -48,10 +48,11 @@ inline int ops_launched(cudaError_t e) {
   return e == cudaSuccess ? BLINK_OK : BLINK_ECUDA;
 }
 
-// cluster > 0: CTAs of a cluster.  after: the kernel may be set up while the one before it in the stream still runs; it waits for that
-// kernel's results itself (griddepcontrol.wait).
+// cluster > 0: CTAs of a cluster.  Kernels are set up while the one before them in the stream still runs (1 to 2 us less a launch) and wait for
+// it themselves: the first kernel of a call in all of its threads before anything else (ops_begin), the later ones before they read what it
+// wrote, or at their end at the latest, so that a kernel that is done says that all before it are.
 template <typename... P, typename... A>
-inline int ops_launch(void (*kernel)(P...), int64_t grid, int threads, size_t smem, void* stream, int cluster, bool after, A... args) {
+inline int ops_launch(void (*kernel)(P...), int64_t grid, int threads, size_t smem, void* stream, int cluster, A... args) {
   if (grid < 1) return BLINK_OK;
   if (grid > 0x7fffffffll) return BLINK_ETOOBIG;
   if (smem > 48 * 1024) {
@@ -75,14 +76,23 @@ inline int ops_launch(void (*kernel)(P...), int64_t grid, int threads, size_t sm
     at[n].val.clusterDim.y = at[n].val.clusterDim.z = 1;
     ++n;
   }
-  if (after) {
-    at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[n].val.programmaticStreamSerializationAllowed = 1;
-    ++n;
-  }
+  at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[n].val.programmaticStreamSerializationAllowed = 1;
+  ++n;
   cfg.attrs = at;
   cfg.numAttrs = (unsigned)n;
   return ops_launched(cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...));
 }
+
+#ifdef __CUDACC__
+__device__ __forceinline__ void ops_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// What came before is done, and what comes next may be set up.  (In this order: a kernel that does not wait for what came before its call's first
+// kernel must not begin earlier.)
+__device__ __forceinline__ void ops_begin() {
+  ops_wait();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+__device__ __forceinline__ void ops_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+#endif
 
 }  // namespace blink

@@ -17,6 +17,9 @@
 //   output: probabilities become an operand with one movmatrix per 8 keys; values are read as rows and paired by key with byte permutes
 // Probabilities are rounded to bf16 for the product with the values (as large an error as that of the output's own rounding);
 // scores, maxima, sums and outputs are in 32 bits.  The maximum in use follows the largest score only when that has grown by more than 2^8.
+#include <cooperative_groups.h>
+
+#include <algorithm>
 #include <cmath>
 
 #include "ops_attention.cuh"
@@ -28,6 +31,7 @@ constexpr int FEW_MAX_CTAS = 640;    // of a launch; the records are laid out fo
 constexpr int FEW_MIN_TILES = 4;     // of a CTA's run, while there are any
 constexpr int FEW_UNIT_TILES = 4;    // what a unit costs beside its tiles, in tiles
 constexpr int JOIN_THREADS = 256;
+constexpr int NEAR_CTAS = 16, NEAR_KEYS = 4096;   // a cluster per unit: its CTAs, keys that a row sees at most
 
 // What the join needs of a unit that was cut, written by the CTA in whose run it begins.
 struct FewCut {
@@ -367,12 +371,13 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) blink_attn_few_kernel(const
   int2* s_len = reinterpret_cast<int2*>(s_pre + a.n + 1);                                // [n] first row, kv_len
   __shared__ long long s_warp[FEW_WARPS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (a.first) ops_wait();
   if (blockIdx.x == 0 && tid == 0) {
     reinterpret_cast<int*>(a.ws)[0] = 0;
     reinterpret_cast<int*>(a.ws)[1] = 0;   // units that the tiles' CTAs have taken from the counter
     __threadfence();
   }
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (the join waits for the whole of this kernel itself)
+  ops_next();
 
   // the sequence of tiles: a run of requests per thread
   const int each = (a.n + FEW_THREADS - 1) / FEW_THREADS;
@@ -486,6 +491,7 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) blink_attn_few_kernel(const
     at += t1 - t0;
   }
   if (tid == 0) reinterpret_cast<FewCut*>(a.ws + ATTN_STATUS_BYTES)[blockIdx.x] = cut;
+  ops_wait();   // (a kernel before it in the call may still run)
 }
 
 // The parts of the unit that begins, but does not end, in the run of CTA blockIdx.x.  A row's parts are shared out over warps, and these joined
@@ -495,7 +501,8 @@ __global__ void __launch_bounds__(JOIN_THREADS) blink_attn_join_kernel(const __g
   constexpr int WARPS = JOIN_THREADS / 32, V = HD / 32;   // values of a row per lane
   __shared__ float s_acc[WARPS][HD];
   __shared__ float2 s_ml[WARPS];
-  asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
+  ops_next();
+  ops_wait();
   const FewCut cut = reinterpret_cast<const FewCut*>(a.ws + ATTN_STATUS_BYTES)[blockIdx.x];
   if (cut.parts == 0) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -557,13 +564,117 @@ __global__ void __launch_bounds__(JOIN_THREADS) blink_attn_join_kernel(const __g
   }
 }
 
+// The same for few units and short contexts, where latency is all there is: a cluster of CTAs per unit, which share its tiles and join their records
+// through distributed shared memory.  One kernel instead of two, no sequence to be added up first: a row of 1024 keys of the 8B shape
+// NEAR_US us, 12.3 with the kernels above.  a.few as there; `groups` clusters per (request, kv head), a group of rows each, or every
+// groups-th where there are more.
+template <typename T, int HD, typename W>
+__global__ void __launch_bounds__(FEW_THREADS) blink_attn_near_kernel(const __grid_constant__ AttnArgs a, const int groups) {
+  namespace cg = cooperative_groups;
+  constexpr int MR = W::MR, PITCH = W::PITCH;
+  extern __shared__ __align__(16) char s_dyn[];
+  float* s_acc = reinterpret_cast<float*>(s_dyn);                             // [FEW_WARPS][MR][PITCH], then this CTA's record in the first of them
+  float2* s_ml = reinterpret_cast<float2*>(s_acc + FEW_WARPS * MR * PITCH);   // [FEW_WARPS][MR]
+  float2* s_rec = s_ml + FEW_WARPS * MR;                                      // [MR] maxima and sums of the record
+  cg::cluster_group cluster = cg::this_cluster();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
+  if (a.first) ops_wait();
+  if (blockIdx.x == 0 && tid == 0) {
+    reinterpret_cast<int*>(a.ws)[0] = 0;
+    reinterpret_cast<int*>(a.ws)[1] = 0;   // units that the tiles' CTAs have taken from the counter
+    __threadfence();
+  }
+  ops_next();
+  const int unit = (int)blockIdx.x / ctas, h = unit % a.pool.Hkv, r = unit / a.pool.Hkv / groups, g0 = unit / a.pool.Hkv % groups;
+  const AttnReq req = attn_req(a, a.row_start[r], a.row_start[r + 1], a.kv_len[r]);
+  if (req.rows == 0 || req.rows > a.few) {   // (the whole cluster)
+    ops_wait();
+    return;
+  }
+  const int32_t* table = a.table + (long long)r * a.stride;
+  W w;
+  for (int m0 = g0 * MR; m0 < req.rows * a.pool.rep; m0 += groups * MR) {
+    const int m1 = min(req.rows * a.pool.rep, m0 + MR);
+    const int first = req.ctx + m0 / a.pool.rep, last = req.ctx + (m1 - 1) / a.pool.rep;
+    const AttnSpan span = attn_span(a, first, last);
+    auto block_of = [&](int t) { return t < span.sinks ? t : span.from + t - span.sinks; };
+    const int t0 = rank * FEW_WARPS + warp, step = ctas * FEW_WARPS;   // the warp's tiles
+    int id = -1;   // of its tile number `lane`, of 32 at a time
+    if (t0 + step * lane < span.n && last >= 0) id = table[block_of(t0 + step * lane)];
+    w.begin(a, req, h, m0, m1);
+    int i = 0;
+    for (int t = t0; t < span.n; t += step, ++i) {
+      if (i == 32) {
+        i = 0;
+        id = t + step * lane < span.n && last >= 0 ? table[block_of(t + step * lane)] : -1;
+      }
+      const int b = block_of(t), block = __shfl_sync(0xffffffffu, id, i);
+      const bool there = (unsigned)block < (unsigned)a.pool.n_blocks;
+      const long long tile = ((long long)block * a.pool.Hkv + h) * (OPS_BLOCK * HD * (int)sizeof(T));
+      const int k0 = b * OPS_BLOCK, k1 = k0 + OPS_BLOCK - 1;
+      const bool edge = k1 > first || (a.window > 0 && k0 <= last - a.window && k1 >= a.sinks);
+      w.tile(a, b, there ? a.pool.k + tile : nullptr, there ? a.pool.v + tile : nullptr, edge, first, last);
+    }
+    w.leave(s_acc + warp * MR * PITCH, s_ml + warp * MR);
+    __syncthreads();
+    // the warps' parts -> the CTA's record, in the place of the first (each thread reads what it writes)
+    const int items = (m1 - m0) * (HD / 4);
+    for (int k = tid; k < items; k += FEW_THREADS) {
+      const int row = k / (HD / 4), d = (k - row * (HD / 4)) * 4;
+      float M = -INFINITY, L = 0.f;
+#pragma unroll
+      for (int y = 0; y < FEW_WARPS; ++y) M = fmaxf(M, s_ml[y * MR + row].x);
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int y = 0; y < FEW_WARPS; ++y) {
+        const float2 ml = s_ml[y * MR + row];
+        const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
+        const float4 z = *reinterpret_cast<const float4*>(s_acc + (y * MR + row) * PITCH + d);
+        L = fmaf(ml.y, f, L);
+        o.x = fmaf(z.x, f, o.x); o.y = fmaf(z.y, f, o.y); o.z = fmaf(z.z, f, o.z); o.w = fmaf(z.w, f, o.w);
+      }
+      *reinterpret_cast<float4*>(s_acc + row * PITCH + d) = o;
+      if (d == 0) s_rec[row] = make_float2(M, L);
+    }
+    cluster.sync();
+    // the CTAs' records -> the output, a share of it by each CTA
+    for (int k = rank * FEW_THREADS + tid; k < items; k += ctas * FEW_THREADS) {
+      const int row = k / (HD / 4), d = (k - row * (HD / 4)) * 4;
+      float M = -INFINITY, L = 0.f;
+#pragma unroll 4
+      for (int c = 0; c < ctas; ++c) M = fmaxf(M, cluster.map_shared_rank(s_rec, c)[row].x);
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+      for (int c = 0; c < ctas; ++c) {
+        const float2 ml = cluster.map_shared_rank(s_rec, c)[row];
+        const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
+        const float4 z = *reinterpret_cast<const float4*>(cluster.map_shared_rank(s_acc, c) + row * PITCH + d);
+        L = fmaf(ml.y, f, L);
+        o.x = fmaf(z.x, f, o.x); o.y = fmaf(z.y, f, o.y); o.z = fmaf(z.z, f, o.z); o.w = fmaf(z.w, f, o.w);
+      }
+      const float inv = L > 0.f ? 1.f / L : 0.f;
+      const int mr = m0 + row;
+      few_store(static_cast<T*>(a.out) + (req.start + mr / a.pool.rep) * a.out_stride + (h * a.pool.rep + mr % a.pool.rep) * HD + d,
+                make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+    }
+    cluster.sync();   // (the records have been read)
+  }
+  ops_wait();   // (a kernel before it in the call may still run)
+}
+
 template <typename T, int HD, typename W, int CTAS>
 static int few_run(const AttnArgs& a, int sms, void* stream) {
+  if (a.near_ctas > 0) {
+    const int64_t ctas = (int64_t)a.n * a.pool.Hkv * a.near_groups * a.near_ctas;
+    const size_t need = (size_t)FEW_WARPS * W::MR * (W::PITCH * 4 + 8) + W::MR * 8;
+    return ops_launch(blink_attn_near_kernel<T, HD, W>, ctas, FEW_THREADS, need, stream, a.near_ctas, a, a.near_groups);
+  }
   const size_t smem = (size_t)FEW_WARPS * W::MR * (W::PITCH * 4 + 8) + (size_t)(a.n + 1) * 16;
   const int grid = sms * CTAS < FEW_MAX_CTAS ? sms * CTAS : FEW_MAX_CTAS;
-  const int rc = ops_launch(blink_attn_few_kernel<T, HD, W, CTAS>, grid, FEW_THREADS, smem, stream, 0, false, a);
+  const int rc = ops_launch(blink_attn_few_kernel<T, HD, W, CTAS>, grid, FEW_THREADS, smem, stream, 0, a);
   if (rc != BLINK_OK) return rc;
-  return ops_launch(blink_attn_join_kernel<T, HD, W::MR>, grid, JOIN_THREADS, 0, stream, 0, true, a);
+  return ops_launch(blink_attn_join_kernel<T, HD, W::MR>, grid, JOIN_THREADS, 0, stream, 0, a);
 }
 
 template <int HD>
@@ -624,13 +735,28 @@ int blink_window_attention(const blink_model_cfg* model, const blink_kv_pool* kv
   a.qscale = (float)(1.4426950408889634 / std::sqrt((double)a.pool.hd));
   a.out_32 = ops_aligned(out, 32) && out_stride % 16 == 0;
   a.ws = static_cast<char*>(workspace);
-  if (model->dtype == BLINK_DTYPE_FP32)
-    return a.pool.hd == 128 ? few_run<float, 128, FewFp32<128>, 2>(a, sms, stream) : few_run<float, 64, FewFp32<64>, 2>(a, sms, stream);
   const int nt = few_nt((int64_t)max_new * a.pool.rep);
-  const bool tiles = (int64_t)max_new * a.pool.rep > 32;
-  if (tiles) a.few = 8 * nt / a.pool.rep;
+  const bool bf16 = model->dtype == BLINK_DTYPE_BF16;
+  const bool tiles = (int64_t)max_new * a.pool.rep > (bf16 ? 32 : 8);   // there may be requests of more than a few rows
+  if (tiles) a.few = (bf16 ? 8 * nt : 8) / a.pool.rep;
+  // So few units that each can have a cluster of 16 CTAs, and rows that see no more than NEAR_KEYS keys.  (8B shape, rows x keys, us, the sequence | clusters
+  // of 16, 8, 4: 1 x 1000 12.5 | 8.9, 4 x 1000 14.6 | 17.7, 8 x 1000 16.7 | 16.9, 16 x 1000 20.8 | 22.9.)
+  const int64_t keys = std::min<int64_t>((int64_t)table_stride * OPS_BLOCK, window > 0 ? (int64_t)window + sinks + max_new : INT64_MAX);
+  const int64_t mr = few_rows_of(model, max_new), rows_few = std::min<int64_t>(max_new, a.few);
+  const int64_t groups = (rows_few * a.pool.rep + mr - 1) / mr, units = (int64_t)n_requests * a.pool.Hkv * groups;
+  a.near_ctas = 0;
+  a.first = bf16 || !tiles;
+  if (keys <= NEAR_KEYS && units * NEAR_CTAS <= sms) {
+    a.near_groups = (int)groups;
+    a.near_ctas = NEAR_CTAS;
+  }
+  if (!bf16) {   // the many rows first: the few find room beside them
+    const int done = tiles ? attn_blocks(a, sms, stream) : BLINK_OK;
+    if (done != BLINK_OK) return done;
+    return a.pool.hd == 128 ? few_run<float, 128, FewFp32<128>, 2>(a, sms, stream) : few_run<float, 64, FewFp32<64>, 2>(a, sms, stream);
+  }
   const int done = a.pool.hd == 128 ? few_bf16<128>(a, nt, sms, stream) : few_bf16<64>(a, nt, sms, stream);
-  return done != BLINK_OK || !tiles ? done : attn_tiles(a, sms, stream);
+  return done != BLINK_OK || !tiles ? done : attn_tiles(a, sms, stream);   // (whose counter the first kernel zeroes)
 }
 
 }  // extern "C"

@@ -16,6 +16,8 @@ struct AttnArgs {
   int window, sinks;                // window 0: no window
   int few;                          // requests of up to so many rows go to attn_few, longer ones to the tiles
   float qscale;                     // 1 / sqrt(hd) * log2(e)
+  int near_ctas, near_groups;       // > 0: a cluster of so many CTAs per unit; clusters per (request, kv head)
+  bool first;                       // attn_few is the call's first kernel
   bool out_32;                      // rows of out begin on 32-byte boundaries
   char* ws;
 };
@@ -52,6 +54,8 @@ __device__ __forceinline__ bool attn_sees(const AttnArgs& a, int key, int pos) {
 constexpr size_t ATTN_STATUS_BYTES = 256;
 // Requests of more than a.few rows on tcgen05 (ops_attn_tiles.cu); the others are in the stream before it.
 int attn_tiles(const AttnArgs& a, int sms, void* stream);
+// The same in 32 bits (ops_attn_block.cu).
+int attn_blocks(const AttnArgs& a, int sms, void* stream);
 
 __device__ __forceinline__ float attn_ex2(float x) {
   float y;

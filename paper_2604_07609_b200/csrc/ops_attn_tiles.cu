@@ -270,6 +270,7 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
   TilUnit* s_unit = reinterpret_cast<TilUnit*>(base + S::END);         // [TIL_UNITS]
   int* s_pre = reinterpret_cast<int*>(base + S::END) + TIL_UNITS * (sizeof(TilUnit) / 4);   // [n + 1] units before a request
   __shared__ __align__(16) TilShared sh;
+  ops_next();
   const int w = (int)til_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   int* status = reinterpret_cast<int*>(a.ws);
   const int lr = 31 - __clz(a.pool.rep), P = 128 >> lr;   // query rows of a stream (1, 2, 4 or 8 heads each)
@@ -637,7 +638,7 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
           if (use > 0) wait(empty, (use - 1u) & 1u);
           if (!ok) break;
           if (part == 0 && j == max(0, tiles - 2)) {   // the next unit, late, so that the CTAs end together; the counter was zeroed by a kernel before this one
-            if (u == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
+            if (u == 0) ops_wait();
             int next = 0;
             if (lane == 0) next = (int)gridDim.x + atomicAdd(status + 1, 1);
             hand_out(u + 1, __shfl_sync(0xffffffffu, next, 0));
@@ -694,7 +695,7 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
     til_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
-  asm volatile("griddepcontrol.wait;" ::: "memory");   // the kernels before it in the call may still run; this one is not done before they are
+  ops_wait();   // the kernels before it in the call may still run; this one is not done before they are
 }
 
 typedef CUresult (*TilEncode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
@@ -725,7 +726,7 @@ static int tiles_run(const AttnArgs& a, int sms, int64_t most_units, void* strea
     return BLINK_ECUDA;
   const size_t smem = (size_t)S::END + 1024 + TIL_UNITS * sizeof(TilUnit) + (size_t)(a.n + 1) * 4;
   const int64_t grid = most_units < sms ? most_units : sms;
-  return ops_launch(blink_attn_tiles_kernel<HD>, grid, TIL_THREADS, smem, stream, 0, true, a, map);
+  return ops_launch(blink_attn_tiles_kernel<HD>, grid, TIL_THREADS, smem, stream, 0, a, map);
 }
 
 int attn_tiles(const AttnArgs& a, int sms, void* stream) {

@@ -32,21 +32,34 @@ struct NormRopeArgs {
   double turns[64];                 // theta^(-2 i / hd) / (2 pi)
 };
 
-__device__ __forceinline__ void nr_load(const __nv_bfloat16* p, float (&x)[8]) {
-  uint32_t r[4];
-  asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "l"(p));
+// Eight elements as they come (so that those on their way take no more registers than that), and as numbers.
+template <typename T>
+struct NrEight {
+  uint4 raw[sizeof(T) * 8 / 16];
+  __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(r[i] << 16);
-    x[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
+    for (int i = 0; i < (int)(sizeof(T) * 8 / 16); ++i)
+      asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(raw[i].x), "=r"(raw[i].y), "=r"(raw[i].z), "=r"(raw[i].w) : "l"(p + i * (16 / (int)sizeof(T))));
   }
-}
-__device__ __forceinline__ void nr_load(const float* p, float (&x)[8]) {
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+    if constexpr (sizeof(T) == 2) {
+      const uint32_t r[4] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w};
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-    asm volatile("ld.global.L1::no_allocate.v4.f32 {%0, %1, %2, %3}, [%4];"
-                 : "=f"(x[4 * i]), "=f"(x[4 * i + 1]), "=f"(x[4 * i + 2]), "=f"(x[4 * i + 3]) : "l"(p + 4 * i));
-}
+      for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(r[i] << 16);
+        x[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        x[4 * i] = __uint_as_float(raw[i].x);
+        x[4 * i + 1] = __uint_as_float(raw[i].y);
+        x[4 * i + 2] = __uint_as_float(raw[i].z);
+        x[4 * i + 3] = __uint_as_float(raw[i].w);
+      }
+    }
+  }
+};
 __device__ __forceinline__ void nr_store(__nv_bfloat16* p, const float (&x)[8]) {
   uint32_t r[4];
 #pragma unroll
@@ -65,6 +78,7 @@ template <typename TI, typename TO, int HD, int U>
 __global__ void __launch_bounds__(NR_WARPS * 32) blink_norm_rope_kernel(const __grid_constant__ NormRopeArgs a) {
   constexpr int HALF = HD / 2, LANES = HALF / 8, GROUP = 32 / LANES;   // lanes of a head, heads of a warp at a time
   __shared__ float2 s_turn[NR_WARPS][HALF];
+  ops_begin();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int heads = a.pool.Hq + 2 * a.pool.Hkv, tasks_row = (heads + GROUP * U - 1) / (GROUP * U);
   const long long task = (long long)blockIdx.x * NR_WARPS + warp;
@@ -72,12 +86,12 @@ __global__ void __launch_bounds__(NR_WARPS * 32) blink_norm_rope_kernel(const __
   const int row = (int)(task / tasks_row), h0 = (int)(task - (long long)row * tasks_row) * GROUP * U + lane / LANES;
   const int i0 = (lane % LANES) * 8;
   const TI* src = static_cast<const TI*>(a.qkv) + row * a.qkv_stride + i0;
-  float x1[U][8], x2[U][8];
+  NrEight<TI> in1[U], in2[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int h = min(h0 + u * GROUP, heads - 1);   // behind the end: the last head once more, not stored
-    nr_load(src + h * HD, x1[u]);
-    nr_load(src + h * HD + HALF, x2[u]);
+    in1[u].load(src + h * HD);
+    in2[u].load(src + h * HD + HALF);
   }
   const int pos = a.positions[row], slot = a.slot_map[row];
   if (pos < 0) return;
@@ -85,10 +99,10 @@ __global__ void __launch_bounds__(NR_WARPS * 32) blink_norm_rope_kernel(const __
   for (int j = 0; j < (HALF + 31) / 32; ++j) {
     const int i = lane + 32 * j;
     const double t = (double)pos * a.turns[i];
-    const double r = (t - rint(t)) * 6.283185307179586;
-    const float hi = (float)r, lo = (float)(r - (double)hi);   // (to first order in what 32 bits leave of the angle)
+    const double r = (t - rint(t)) * 2.0;   // in half turns, -1 .. 1
+    const float hi = (float)r, lo = (float)(r - (double)hi) * 3.14159265f;   // (to first order in what 32 bits leave of the angle)
     float s, c;
-    sincosf(hi, &s, &c);
+    sincospif(hi, &s, &c);
     s_turn[warp][i] = make_float2(fmaf(-s, lo, c), fmaf(c, lo, s));
   }
   __syncwarp();
@@ -106,55 +120,57 @@ __global__ void __launch_bounds__(NR_WARPS * 32) blink_norm_rope_kernel(const __
     const int h = h0 + u * GROUP;
     const bool is_q = h < a.pool.Hq, turn = h < a.pool.Hq + a.pool.Hkv;
     const float* gain = is_q ? a.q_gain : a.k_gain;
+    float x1[8], x2[8];
+    in1[u].get(x1);
+    in2[u].get(x2);
     float ss = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) ss = fmaf(x1[u][i], x1[u][i], fmaf(x2[u][i], x2[u][i], ss));
+    for (int i = 0; i < 8; ++i) ss = fmaf(x1[i], x1[i], fmaf(x2[i], x2[i], ss));
 #pragma unroll
     for (int d = 1; d < LANES; d <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
     if (h >= heads) continue;
-    float y1[8], y2[8];
     if (turn) {
       if (gain) {
         const float f = rsqrtf(ss * (1.0f / HD) + a.eps);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          x1[u][i] *= f * gain[i0 + i];
-          x2[u][i] *= f * gain[HALF + i0 + i];
+          x1[i] *= f * gain[i0 + i];
+          x2[i] *= f * gain[HALF + i0 + i];
         }
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        y1[i] = fmaf(x1[u][i], c[i], -x2[u][i] * s[i]);
-        y2[i] = fmaf(x2[u][i], c[i], x1[u][i] * s[i]);
+        const float y = fmaf(x1[i], c[i], -x2[i] * s[i]);
+        x2[i] = fmaf(x2[i], c[i], x1[i] * s[i]);
+        x1[i] = y;
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) { y1[i] = x1[u][i]; y2[i] = x2[u][i]; }
     }
     TO* dst;
     if (is_q) dst = static_cast<TO*>(a.q_out) + row * a.q_stride + h * HD + i0;
     else if (!cached) continue;
     else dst = reinterpret_cast<TO*>(turn ? a.pool.k : a.pool.v) + tile + (long long)(h - a.pool.Hq - (turn ? 0 : a.pool.Hkv)) * OPS_BLOCK * HD;
-    nr_store(dst, y1);
-    nr_store(dst + HALF, y2);
+    nr_store(dst, x1);
+    nr_store(dst + HALF, x2);
   }
 }
 
 template <typename TI, typename TO>
 int norm_rope_launch(const NormRopeArgs& a, void* stream) {
   const int heads = a.pool.Hq + 2 * a.pool.Hkv;
-  // Few rows: a warp per group of heads, so that a row is spread over as many SMs as it can be; many rows: four groups a warp, which
-  // share the row's angles.
+  // Few rows: a warp per group of heads, so that a row is spread over as many SMs as it can be.  Many: several groups a warp, which share the
+  // row's angles and have more on its way: 1.5 KB a lane's worth in 32 bits or of heads of 64, 3 KB of wide heads in 16 bits.  (16000 rows of the 8B
+  // shape, us, with 2 | 3 | 4 | 6 groups: fp32 in 113 | 105 | 105 | 109, bf16 in 92 | 80 | 77 | 72; 4099 rows of the 1B shape in bf16 14.4 | 12.7 | 14.5 | 14.4.)
   const int group = a.pool.hd == 128 ? 4 : 8;
   const bool few = (long long)a.rows * ((heads + group - 1) / group) <= 4 * 148 * 16;
-  const int u = few ? 1 : 4;
+  constexpr int WIDE = sizeof(TI) == 2 ? 6 : 3;
+  const int u = few ? 1 : a.pool.hd == 128 ? WIDE : 3;
   const long long tasks = (long long)a.rows * ((heads + group * u - 1) / (group * u));
   const long long grid = (tasks + NR_WARPS - 1) / NR_WARPS;
   if (a.pool.hd == 128)
-    return few ? ops_launch(blink_norm_rope_kernel<TI, TO, 128, 1>, grid, NR_WARPS * 32, 0, stream, 0, false, a)
-               : ops_launch(blink_norm_rope_kernel<TI, TO, 128, 4>, grid, NR_WARPS * 32, 0, stream, 0, false, a);
-  return few ? ops_launch(blink_norm_rope_kernel<TI, TO, 64, 1>, grid, NR_WARPS * 32, 0, stream, 0, false, a)
-             : ops_launch(blink_norm_rope_kernel<TI, TO, 64, 4>, grid, NR_WARPS * 32, 0, stream, 0, false, a);
+    return few ? ops_launch(blink_norm_rope_kernel<TI, TO, 128, 1>, grid, NR_WARPS * 32, 0, stream, 0, a)
+               : ops_launch(blink_norm_rope_kernel<TI, TO, 128, WIDE>, grid, NR_WARPS * 32, 0, stream, 0, a);
+  return few ? ops_launch(blink_norm_rope_kernel<TI, TO, 64, 1>, grid, NR_WARPS * 32, 0, stream, 0, a)
+             : ops_launch(blink_norm_rope_kernel<TI, TO, 64, 3>, grid, NR_WARPS * 32, 0, stream, 0, a);
 }
 
 }  // namespace blink

@@ -36,6 +36,7 @@ __global__ void __launch_bounds__(TAB_THREADS) blink_tables_kernel(const TablesA
   __shared__ int s_err;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
+  ops_begin();
   if (tid == 0) s_err = 0;
   __syncthreads();
 
@@ -177,5 +178,5 @@ extern "C" int blink_build_tables(const int32_t* ctx_len, const int32_t* new_len
                         block_table, blocks_held_out, free_count_out, row_start, kv_len, positions, slot_map, status};
   const int cluster = max_rows > 4 * TAB_THREADS || n_requests > TAB_THREADS ? 8 : 1;
   const size_t smem = (size_t)(4 * n_requests + 2) * 4;
-  return ops_launch(blink_tables_kernel, cluster, TAB_THREADS, smem, stream, cluster, false, a);
+  return ops_launch(blink_tables_kernel, cluster, TAB_THREADS, smem, stream, cluster, a);
 }

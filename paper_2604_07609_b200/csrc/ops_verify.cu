@@ -4,19 +4,21 @@
 //   first refused i: a token from max(0, p_i - q_i), none refused: from p of the last row; by the inverse of its running sum in the order of
 //   the indexes: the first j with sum_{<= j} > v * sum
 //
-// Five kernels, each waiting for the one before it only where it needs its results.
+// Three kernels, each waiting for the one before it only where it needs its results.
 //   rows    largest value and sum of exponentials of pieces of 1024 entries of every row, a warp each: one pass over the logits, which is what
 //           bounds the whole (HBM: 4 bytes an entry).  A lane has its 32 entries on their way at once and sums against its own largest
 //           value, so that nothing waits for another warp.  Exponentials in 32 bits, sums of a lane's entries in 32, everything above in
 //           64: the acceptance test is off by some 1e-8.
 //   choose  a CTA per request: the first refused draft, from the pieces
-//   sums    the exponentials of that row, 512 entries a warp
-//   weights the same entries once more: max(0, p - q), and their sum per warp
-//   draw    a warp per request: the run of 512 in which the running sum passes its target, and the entry of that run
-// (the last two as one kernel, the last CTA of a request to come drawing, were slower: a fence and a counter in every CTA's way)
+//   draw    a cluster of 16 CTAs per request: the exponentials of that row, which stay in registers (up to 16 a thread), their sum, then the weights
+//           max(0, p - q), their sum, and the entry at which the running sum passes its target.  Sums go from CTA to CTA through
+//           distributed shared memory.
 // The chosen row's sums decide between neighbours that are as close as 1e-6, so its exponentials, sums and running sum are in 64 bits.  Sums are
-// taken in an order that sizes alone fix, whoever comes last: the same call gives the same token.
+// taken in an order that sizes alone fix: the same call gives the same token.
+#include <cooperative_groups.h>
+
 #include <cmath>
+#include <utility>
 
 #include "ops.h"
 
@@ -24,7 +26,7 @@ namespace blink {
 
 constexpr int VER_WARPS = 8, VER_THREADS = VER_WARPS * 32;
 constexpr int VER_EACH = 32, VER_CHUNK = 32 * VER_EACH;   // rows: entries of a lane, a warp
-constexpr int VER_FEW = 16, VER_RUN = 32 * VER_FEW, VER_PART = VER_WARPS * VER_RUN;            // sums, weights
+constexpr int PICK_THREADS = 512, PICK_WARPS = 16, PICK_CTAS = 16;   // draw
 
 struct VerChunk {
   double sum;   // of exp((z - max) / T)
@@ -37,10 +39,6 @@ struct VerChoice {
   float max;
   int unused;
 };
-struct VerRun {
-  double rest, all;   // sums over a warp's run: of the weights, and of p
-};
-
 struct VerifyArgs {
   const float* logits;
   const float* probs;
@@ -49,11 +47,8 @@ struct VerifyArgs {
   const float *temperature, *u_accept, *u_pick;
   int32_t *tokens, *accepted;
   VerChunk* chunks_of;   // [rows][chunks]
-  double* sums;          // [n][parts]
-  VerRun* runs;          // [n][parts * VER_WARPS], and behind them the same for whole parts, [n][parts]
-  VerRun* part_runs;
   VerChoice* choice;     // [n]
-  int n, rows, vocab, chunks, groups, parts;
+  int n, rows, vocab, chunks, groups;
   bool vec, probs_vec;   // rows on 16-byte boundaries
   double sixteenths[16]; // 2^(i / 16)
 };
@@ -112,7 +107,7 @@ __global__ void __launch_bounds__(VER_THREADS) blink_verify_rows_kernel(const Ve
   __shared__ float s_T;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int row = (int)(blockIdx.x / (unsigned)a.groups), chunk = (int)(blockIdx.x - (unsigned)row * a.groups) * VER_WARPS + warp;
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (the second kernel waits for the whole of this one itself)
+  ops_begin();
   float v[VER_EACH];
   if (chunk < a.chunks)
     ver_load(v, a.logits + row * a.logits_stride + (long long)chunk * VER_CHUNK, min(VER_CHUNK, a.vocab - chunk * VER_CHUNK), a.vec, -INFINITY);
@@ -214,7 +209,7 @@ __global__ void __launch_bounds__(VER_THREADS) blink_verify_choose_kernel(const 
   __shared__ double s_table[16];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int req = (int)blockIdx.x;
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  ops_next();
   // (all but the pieces is there before the first kernel is done)
   const int2 rows = ver_rows(a, req);
   const int start = rows.x, k = rows.y - rows.x - 1;
@@ -255,13 +250,13 @@ __global__ void __launch_bounds__(VER_THREADS) blink_verify_choose_kernel(const 
     const bool in = x >= 0 && x < a.vocab;
     const float z = in ? ver_entry(__ldcg(a.logits + row * a.logits_stride + x)) : -INFINITY, q = in && a.probs ? a.probs[row * a.probs_stride + x] : 1.f;
     const float u = a.u_accept[row];
-    if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (!waited) ops_wait();
     waited = true;
     const bool one = row_of(row, m, idx, sum, true);
     const bool ok = one ? x == idx : in && (double)u * (double)q * sum < ver_exp(ver_exp_of(s_table, m, T), z);
     if (lane == 0 && !ok) atomicMin(&s_first, i);
   }
-  if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (!waited) ops_wait();
   __syncthreads();
   const int acc = s_first, row = start + acc;
   if (k < 0) {   // a request without rows
@@ -286,244 +281,220 @@ __global__ void __launch_bounds__(VER_THREADS) blink_verify_choose_kernel(const 
     if (i != acc) a.tokens[start + i] = i < acc ? a.draft[start + i] : -1;
 }
 
-__global__ void __launch_bounds__(VER_THREADS) blink_verify_sums_kernel(const VerifyArgs a) {
-  __shared__ double s_part[VER_WARPS], s_table[16];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int req = (int)(blockIdx.x / (unsigned)a.parts), part = (int)(blockIdx.x - (unsigned)req * a.parts);
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const float T = a.temperature[req];
-  ver_table(s_table, a);
-  __syncthreads();
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  const VerChoice c = a.choice[req];
-  if (c.row < 0) return;
-  const int at = part * VER_PART + warp * VER_RUN;   // this warp's run of the row
-  float z[VER_FEW];
-  ver_load(z, a.logits + c.row * a.logits_stride + at, a.vocab - at, a.vec, -INFINITY);
-  const VerExp x = ver_exp_of(s_table, c.max, T);
-  double s = 0.0;
-#pragma unroll
-  for (int i = 0; i < VER_FEW; i += 2) s += ver_exp(x, z[i]) + ver_exp(x, z[i + 1]);
-#pragma unroll
-  for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-  if (lane == 0) s_part[warp] = s;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    s = 0.0;
-#pragma unroll
-    for (int w = 0; w < VER_WARPS; ++w) s += s_part[w];
-    a.sums[(size_t)req * a.parts + part] = s;
-  }
-}
-
-// What a token is drawn from: p - q where a draft was refused (what is no number or negative in q counts as 0), p otherwise.
-struct VerWeights {
-  const float *z, *q;   // the row, and that of q (null: none)
-  int x;                // the entry that a certain draft takes out (-1: none)
-  VerExp exp;
-  double inv_sum;
-};
-// The row's sum of exponentials, by a whole warp.
-__device__ __forceinline__ double ver_sum(const VerifyArgs& a, int req) {
-  double s = 0.0;
-#pragma unroll 4
-  for (int j = threadIdx.x & 31; j < a.parts; j += 32) s += a.sums[(size_t)req * a.parts + j];
-#pragma unroll
-  for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-  return s;
-}
-// Entries at + 4 lane + 128 g + j of a run, in 64 bits, and the sum of p over the lane's.
-__device__ __forceinline__ void ver_weights(const VerWeights& w, int at, const float (&z)[VER_FEW], const float (&q)[VER_FEW], double (&e)[VER_FEW], double& all) {
+// The first of 16 parts (a lane each, lanes 16 .. 31 have 0) whose running sum exceeds target, else the last with anything in it; `base` grows by
+// what stands before it.
+__device__ __forceinline__ int ver_part(double part, double target, double& base) {
   const int lane = threadIdx.x & 31;
+  double c = part;
 #pragma unroll
-  for (int i = 0; i < VER_FEW; ++i) {
-    const double p = ver_exp(w.exp, z[i]) * w.inv_sum;
-    all += p;
-    if (w.q) e[i] = q[i] > 0.f ? fmax(p - (double)q[i], 0.0) : p;
-    else e[i] = at + lane * 4 + (i >> 2) * 128 + (i & 3) == w.x ? 0.0 : p;
+  for (int d = 1; d < 16; d <<= 1) {
+    const double u = __shfl_up_sync(0xffffffffu, c, d);
+    if (lane >= d) c += u;
   }
+  const unsigned hit = __ballot_sync(0xffffffffu, part > 0.0 && base + c > target), any = __ballot_sync(0xffffffffu, part > 0.0);
+  const int at = hit ? __ffs(hit) - 1 : any ? 31 - __clz(any) : 0;
+  const double before = __shfl_sync(0xffffffffu, c, max(at - 1, 0));
+  if (at > 0) base += before;
+  return at;
 }
 
-// The first of `count` values, in order, at which the running sum exceeds target, else the last with anything in it; `base`
-// grows by what stands before it.  By one warp.
-template <typename F>
-__device__ __forceinline__ int ver_find(F value, int count, double target, double& base) {
-  const int lane = threadIdx.x & 31;
-  int last = 0;
-  double last_base = base;
-  for (int j0 = 0; j0 < count; j0 += 32) {
-    const double v = j0 + lane < count ? value(j0 + lane) : 0.0;
-    double c = v;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const double u = __shfl_up_sync(0xffffffffu, c, d);
-      if (lane >= d) c += u;
-    }
-    const double up = __shfl_up_sync(0xffffffffu, c, 1), before = base + (lane ? up : 0.0);
-    const unsigned hit = __ballot_sync(0xffffffffu, v > 0.0 && base + c > target), any = __ballot_sync(0xffffffffu, v > 0.0);
-    const int l = hit ? __ffs(hit) - 1 : any ? 31 - __clz(any) : 0;
-    const double at = __shfl_sync(0xffffffffu, before, l);
-    if (hit) {
-      base = at;
-      return j0 + l;
-    }
-    if (any) {
-      last = j0 + l;
-      last_base = at;
-    }
-    base += __shfl_sync(0xffffffffu, c, 31);
-  }
-  base = last_base;
-  return last;
-}
-
-// Of the request's chosen row, all but its sum; false: nothing is drawn.
-__device__ __forceinline__ bool ver_choice(const VerifyArgs& a, int req, const double* table, float T, VerWeights& w, int& row) {
-  const VerChoice c = a.choice[req];
-  row = c.row;
-  if (c.row < 0) return false;
-  w.z = a.logits + c.row * a.logits_stride;
-  w.q = c.refused && a.probs ? a.probs + c.row * a.probs_stride : nullptr;
-  w.x = c.refused && !a.probs ? a.draft[c.row] : -1;
-  w.exp = ver_exp_of(table, c.max, T);
-  return true;
-}
-
-__global__ void __launch_bounds__(VER_THREADS) blink_verify_weights_kernel(const VerifyArgs a) {
-  __shared__ VerRun s_run[VER_WARPS];
-  __shared__ double s_inv, s_table[16];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int req = (int)(blockIdx.x / (unsigned)a.parts), part = (int)(blockIdx.x - (unsigned)req * a.parts);
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  VerWeights w;
-  const float T = a.temperature[req];
-  ver_table(s_table, a);
-  __syncthreads();
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  int row;
-  if (!ver_choice(a, req, s_table, T, w, row)) return;
-  const int at = part * VER_PART + warp * VER_RUN;
-  float z[VER_FEW], q[VER_FEW];
-  ver_load(z, w.z + at, a.vocab - at, a.vec, -INFINITY);
-  if (w.q) ver_load(q, w.q + at, a.vocab - at, a.probs_vec, 0.f);
-  if (warp == 0) {
-    const double s = ver_sum(a, req);
-    if (lane == 0) s_inv = 1.0 / s;
-  }
-  __syncthreads();
-  w.inv_sum = s_inv;
-  double rest = 0.0, all = 0.0, e[VER_FEW];
-  ver_weights(w, at, z, q, e, all);
-#pragma unroll
-  for (int i = 0; i < VER_FEW; i += 2) rest += e[i] + e[i + 1];
-#pragma unroll
-  for (int d = 16; d; d >>= 1) {
-    rest += __shfl_xor_sync(0xffffffffu, rest, d);
-    all += __shfl_xor_sync(0xffffffffu, all, d);
-  }
-  if (lane == 0) s_run[warp] = a.runs[((size_t)req * a.parts + part) * VER_WARPS + warp] = VerRun{rest, all};
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    VerRun r = {0.0, 0.0};
-#pragma unroll
-    for (int i = 0; i < VER_WARPS; ++i) {
-      r.rest += s_run[i].rest;
-      r.all += s_run[i].all;
-    }
-    a.part_runs[(size_t)req * a.parts + part] = r;
-  }
-}
-
-__global__ void __launch_bounds__(32) blink_verify_draw_kernel(const VerifyArgs a) {
+// EACH: entries of a lane at a time.
+template <int EACH>
+__global__ void __launch_bounds__(PICK_THREADS, 2) blink_verify_draw_kernel(const VerifyArgs a) {
+  namespace cg = cooperative_groups;
+  constexpr int TILE = 32 * EACH;
+  cg::cluster_group cluster = cg::this_cluster();
+  __shared__ __align__(16) float s_q[PICK_WARPS][TILE];   // a tile of q per warp, each lane's own entries
+  __shared__ double s_part[PICK_WARPS];                   // a sum per warp
+  __shared__ double s_all[2][PICK_CTAS];                  // a sum per CTA, the same in all of them
   __shared__ double s_table[16];
-  const int lane = threadIdx.x, req = (int)blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int rank = (int)cluster.block_rank(), req = (int)(blockIdx.x / PICK_CTAS);
+  const int V = a.vocab;
   const float T = a.temperature[req], u = a.u_pick[req];
-  VerWeights w;
   ver_table(s_table, a);
-  __syncwarp();
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  int row;
-  if (!ver_choice(a, req, s_table, T, w, row)) return;
-  w.inv_sum = 1.0 / ver_sum(a, req);
-  const VerRun* r = a.part_runs + (size_t)req * a.parts;
-  double total = 0.0, total_all = 0.0;
-#pragma unroll 4
-  for (int j = lane; j < a.parts; j += 32) {
-    total += r[j].rest;
-    total_all += r[j].all;
-  }
+  __syncthreads();
+  ops_wait();
+  ops_next();
+  const VerChoice choice = a.choice[req];
+  const int row = choice.row;
+  if (row < 0) return;   // (the whole cluster)
+  cg::cluster_group::arrival_token there = cluster.barrier_arrive();   // all CTAs have to be there before they are written to
+  // the row's entries: a run of tiles per warp, in the order of CTAs, warps and tiles
+  const int tiles = (V + PICK_CTAS * PICK_WARPS * TILE - 1) / (PICK_CTAS * PICK_WARPS * TILE);
+  const int w0 = (rank * PICK_WARPS + warp) * tiles * TILE;
+  const float* z = a.logits + row * a.logits_stride;
+  const float* q = choice.refused && a.probs ? a.probs + row * a.probs_stride : nullptr;
+  float zv[EACH];   // of the warp's first tile
+  ver_load(zv, z + w0, V - w0, a.vec, -INFINITY);
+  auto fetch_q = [&](int at) {
 #pragma unroll
-  for (int d = 16; d; d >>= 1) {
-    total += __shfl_xor_sync(0xffffffffu, total, d);
-    total_all += __shfl_xor_sync(0xffffffffu, total_all, d);
-  }
-  const bool none = !(total > 0.0);   // q covers p everywhere: from p itself
-  if (none) {
-    w.q = nullptr;
-    w.x = -1;
-    total = total_all;
-  }
-  const double target = (double)u * total;
-  double base = 0.0;
-  const int in = ver_find([&](int j) { return none ? r[j].all : r[j].rest; }, a.parts, target, base);
-  r = a.runs + ((size_t)req * a.parts + in) * VER_WARPS;
-  const int run = ver_find([&](int j) { return none ? r[j].all : r[j].rest; }, VER_WARPS, target, base);
-  int token = -1, last = 0;
-  const int from = in * VER_PART + run * VER_RUN;
-  float z[VER_FEW], q[VER_FEW];
-  double e[VER_FEW], all = 0.0;
-  ver_load(z, w.z + from, a.vocab - from, a.vec, -INFINITY);
-  if (w.q) ver_load(q, w.q + from, a.vocab - from, a.probs_vec, 0.f);
-  ver_weights(w, from, z, q, e, all);
-  double sum[VER_FEW / 4];   // running sums over the lanes, of each group of 128
+    for (int g = 0; g < EACH / 4; ++g) {
+      const int o = g * 128 + lane * 4;
+      const uint32_t dst = (uint32_t)__cvta_generic_to_shared(&s_q[warp][o]);
+      if (a.probs_vec && at + o + 4 <= V) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(q + at + o) : "memory");
+      } else {
 #pragma unroll
-  for (int g = 0; g < VER_FEW / 4; ++g) sum[g] = (e[4 * g] + e[4 * g + 1]) + (e[4 * g + 2] + e[4 * g + 3]);
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-#pragma unroll
-    for (int g = 0; g < VER_FEW / 4; ++g) {
-      const double x = __shfl_up_sync(0xffffffffu, sum[g], d);
-      if (lane >= d) sum[g] += x;
-    }
-  }
-#pragma unroll
-  for (int g = 0; g < VER_FEW / 4; ++g) {
-    const double up = __shfl_up_sync(0xffffffffu, sum[g], 1);
-    double running = lane ? base + up : base;
-    int hit = 4, some = -1;   // of the lane's four
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      running += e[4 * g + j];
-      if (e[4 * g + j] > 0.0) {
-        some = j;
-        if (hit == 4 && running > target) hit = j;
+        for (int j = 0; j < 4; ++j)
+          if (at + o + j < V) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + 4 * j), "l"(q + at + o + j) : "memory");
       }
     }
-    const unsigned hits = __ballot_sync(0xffffffffu, hit < 4), any = __ballot_sync(0xffffffffu, some >= 0);
-    const int l = hits ? __ffs(hits) - 1 : any ? 31 - __clz(any) : 0;
-    const int h = __shfl_sync(0xffffffffu, hit, l), o = __shfl_sync(0xffffffffu, some, l);
-    if (token < 0) {
-      if (hits) token = from + g * 128 + l * 4 + h;
-      else if (any) last = from + g * 128 + l * 4 + o;
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  if (q) fetch_q(w0);
+  const VerExp exp = ver_exp_of(s_table, choice.max, T);
+  double e[EACH];
+  auto exps = [&]() {
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) e[i] = ver_exp(exp, zv[i]);
+  };
+  auto lane_sum = [&]() {
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < EACH; i += 4) s += (e[i] + e[i + 1]) + (e[i + 2] + e[i + 3]);
+    return s;
+  };
+  // sum over the lanes -> over the CTA -> over the cluster; s_part keeps the warps', s_all the CTAs'
+  auto sum_all = [&](double s, int which) {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+    if (lane == 0) s_part[warp] = s;
+    __syncthreads();
+    if (warp == 0) {
+      double t = s_part[lane & 15];
+#pragma unroll
+      for (int d = 8; d; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
+      if (lane < PICK_CTAS) *cluster.map_shared_rank(&s_all[which][rank], lane) = t;
     }
-    base += __shfl_sync(0xffffffffu, sum[g], 31);
+    cluster.sync();
+    double t = s_all[which][lane & 15];
+#pragma unroll
+    for (int d = 8; d; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
+    return t;
+  };
+  auto load_more = [&](int t) {   // tiles behind the first are read again in every pass
+    const int at = w0 + t * TILE;
+    ver_load(zv, z + at, V - at, a.vec, -INFINITY);
+    if (q) fetch_q(at);
+  };
+  double s = 0.0;
+#pragma unroll 1
+  for (int t = tiles - 1; t >= 0; --t) {   // (the first last: it stays)
+    if (tiles > 1) load_more(t);
+    exps();
+    s += lane_sum();
+  }
+  cluster.barrier_wait(std::move(there));
+  const double inv_S = 1.0 / sum_all(s, 0);
+
+  // what is drawn from: p - q where a draft was refused (what is no number or negative in q counts as 0), p otherwise
+  int x = choice.refused && !a.probs ? a.draft[row] : -1;
+  auto rests = [&](int t) {   // of tile t, whose exponentials are in e
+    const int at = w0 + t * TILE + lane * 4;
+    if (q) {
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
+#pragma unroll
+      for (int i = 0; i < EACH; i += 4) {
+        const float4 v = *reinterpret_cast<const float4*>(&s_q[warp][i * 32 + lane * 4]);
+        const float w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const double p = e[i + j] * inv_S;
+          e[i + j] = w[j] > 0.f && at + i * 32 + j < V ? fmax(p - (double)w[j], 0.0) : p;   // (behind the end: nothing was fetched, and p is 0)
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) {
+        const double p = e[i] * inv_S;
+        e[i] = at + (i >> 2) * 128 + (i & 3) == x ? 0.0 : p;
+      }
+    }
+  };
+  bool have = tiles == 1;   // the exponentials of the only tile are in e
+  auto rest_sum = [&]() {
+    double r = 0.0;
+#pragma unroll 1
+    for (int t = tiles - 1; t >= 0; --t) {
+      if (!have) {
+        load_more(t);
+        exps();
+      }
+      rests(t);
+      r += lane_sum();
+    }
+    return sum_all(r, 1);
+  };
+  double total;
+#pragma unroll 1
+  while (true) {
+    total = rest_sum();
+    if (total > 0.0 || (!q && x < 0)) break;
+    q = nullptr;          // q covers p everywhere: from p itself
+    x = -1;
+    have = false;
+    cluster.sync();       // (everybody has read the sums)
+  }
+  const double target = (double)u * total;
+  // the CTA, and the warp in it, whose run takes the sum past the target; else the last with anything in it
+  double base = 0.0;
+  if (ver_part(lane < PICK_CTAS ? s_all[1][lane] : 0.0, target, base) != rank) return;
+  if (ver_part(lane < PICK_WARPS ? s_part[lane] : 0.0, target, base) != warp) return;
+  int token = -1, last = 0;
+#pragma unroll 1
+  for (int t = 0; t < tiles && token < 0; ++t) {
+    if (tiles > 1) {   // (one tile: its are in e)
+      load_more(t);
+      exps();
+      rests(t);
+    }
+    double c[EACH / 4];   // running sums over the lanes, of each group of 128
+#pragma unroll
+    for (int g = 0; g < EACH / 4; ++g) c[g] = (e[4 * g] + e[4 * g + 1]) + (e[4 * g + 2] + e[4 * g + 3]);
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+#pragma unroll
+      for (int g = 0; g < EACH / 4; ++g) {
+        const double u = __shfl_up_sync(0xffffffffu, c[g], d);
+        if (lane >= d) c[g] += u;
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < EACH / 4; ++g) {
+      const double up = __shfl_up_sync(0xffffffffu, c[g], 1);
+      double run = lane ? base + up : base;
+      int hit = 4, some = -1;   // of the lane's four
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        run += e[4 * g + j];
+        if (e[4 * g + j] > 0.0) {
+          some = j;
+          if (hit == 4 && run > target) hit = j;
+        }
+      }
+      const unsigned hits = __ballot_sync(0xffffffffu, hit < 4), any = __ballot_sync(0xffffffffu, some >= 0);
+      const int at = w0 + t * TILE + g * 128;
+      const int l = hits ? __ffs(hits) - 1 : any ? 31 - __clz(any) : 0;
+      const int h = __shfl_sync(0xffffffffu, hit, l), o = __shfl_sync(0xffffffffu, some, l);
+      if (token < 0) {
+        if (hits) token = at + l * 4 + h;
+        else if (any) last = at + l * 4 + o;
+      }
+      base += __shfl_sync(0xffffffffu, c[g], 31);
+    }
   }
   if (lane == 0) a.tokens[row] = token >= 0 ? token : last;
 }
 
 struct VerifySpace {
-  uint64_t chunks, sums, runs, part_runs, choice, end;
-  int64_t n_chunks, n_parts;
+  uint64_t choice, end;   // behind the pieces
+  int64_t n_chunks;
 };
 static VerifySpace verify_space(int64_t rows, int64_t n, int64_t vocab) {
   VerifySpace s;
   s.n_chunks = (vocab + VER_CHUNK - 1) / VER_CHUNK;
-  s.n_parts = (vocab + VER_PART - 1) / VER_PART;
-  s.chunks = 0;
-  s.sums = s.chunks + (uint64_t)(rows * s.n_chunks) * sizeof(VerChunk);
-  s.runs = (s.sums + (uint64_t)(n * s.n_parts) * 8 + 15) / 16 * 16;
-  s.part_runs = s.runs + (uint64_t)(n * s.n_parts * VER_WARPS) * sizeof(VerRun);
-  s.choice = s.part_runs + (uint64_t)(n * s.n_parts) * sizeof(VerRun);
+  s.choice = (uint64_t)(rows * s.n_chunks) * sizeof(VerChunk);
   s.end = s.choice + (uint64_t)n * sizeof(VerChoice);
   return s;
 }
@@ -563,26 +534,24 @@ int blink_verify_drafts(const float* logits, int64_t logits_stride, int rows, in
   a.u_pick = u_pick;
   a.tokens = out_tokens;
   a.accepted = n_accepted;
-  a.chunks_of = reinterpret_cast<VerChunk*>(ws + space.chunks);
-  a.sums = reinterpret_cast<double*>(ws + space.sums);
-  a.runs = reinterpret_cast<VerRun*>(ws + space.runs);
-  a.part_runs = reinterpret_cast<VerRun*>(ws + space.part_runs);
+  a.chunks_of = reinterpret_cast<VerChunk*>(ws);
   a.choice = reinterpret_cast<VerChoice*>(ws + space.choice);
   a.n = n_requests;
   a.rows = rows;
   a.vocab = vocab;
   a.chunks = (int)space.n_chunks;
   a.groups = (int)((space.n_chunks + VER_WARPS - 1) / VER_WARPS);
-  a.parts = (int)space.n_parts;
   for (int i = 0; i < 16; ++i) a.sixteenths[i] = std::exp2(i / 16.0);
   a.vec = logits_stride % 4 == 0 && ops_aligned(logits, 16);
   a.probs_vec = draft_probs && probs_stride % 4 == 0 && ops_aligned(draft_probs, 16);
-  int rc = ops_launch(blink_verify_rows_kernel, (int64_t)rows * a.groups, VER_THREADS, 0, stream, 0, false, a);
-  if (rc == BLINK_OK) rc = ops_launch(blink_verify_choose_kernel, n_requests, VER_THREADS, 0, stream, 0, true, a);
-  if (rc == BLINK_OK) rc = ops_launch(blink_verify_sums_kernel, (int64_t)n_requests * a.parts, VER_THREADS, 0, stream, 0, true, a);
-  if (rc == BLINK_OK) rc = ops_launch(blink_verify_weights_kernel, (int64_t)n_requests * a.parts, VER_THREADS, 0, stream, 0, true, a);
-  if (rc == BLINK_OK) rc = ops_launch(blink_verify_draw_kernel, n_requests, 32, 0, stream, 0, true, a);
-  return rc;
+  int rc = ops_launch(blink_verify_rows_kernel, (int64_t)rows * a.groups, VER_THREADS, 0, stream, 0, a);
+  if (rc == BLINK_OK) rc = ops_launch(blink_verify_choose_kernel, n_requests, VER_THREADS, 0, stream, 0, a);
+  if (rc != BLINK_OK) return rc;
+  // as few entries of a lane as hold the row in one go: 32768 entries in 16 CTAs of 16 warps with four, 131072 with 16 (beyond that, runs of tiles)
+  const int64_t ctas = (int64_t)n_requests * PICK_CTAS;
+  if (vocab <= 32768) return ops_launch(blink_verify_draw_kernel<4>, ctas, PICK_THREADS, 0, stream, PICK_CTAS, a);
+  if (vocab <= 65536) return ops_launch(blink_verify_draw_kernel<8>, ctas, PICK_THREADS, 0, stream, PICK_CTAS, a);
+  return ops_launch(blink_verify_draw_kernel<16>, ctas, PICK_THREADS, 0, stream, PICK_CTAS, a);
 }
 
 }  // extern "C"
