@@ -80,7 +80,7 @@ struct Args {
                           (long long)cols, c10::toString(type));
       else fail(PyExc_ValueError, "%s: [rows][columns] of %s, elements of a row next to one another", what, c10::toString(type));
     } else {
-      *stride = t->size(0) > 1 ? t->stride(0) : std::max<int64_t>(t->size(1), t->stride(0));
+      *stride = t->size(0) > 1 ? t->stride(0) : t->size(1);   // (of a single row it may be anything)
     }
     return t;
   }

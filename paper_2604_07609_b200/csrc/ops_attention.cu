@@ -64,13 +64,20 @@ __device__ __forceinline__ uint32_t few_transposed(uint32_t x) {
 template <int HD, int NT>
 struct FewBf16 {
   static constexpr int MR = 8 * NT, CH = HD / 32, U = HD / 64, PITCH = HD + 4;
-  uint32_t q[NT][CH][4];
+  // 32 rows: the queries stay in shared memory, in fragments (a 16-byte read for two instructions), or registers spill (48 requests of 2500 keys, 8 rows each:
+  // 157 us with them in registers, 131 so; 24 rows 107 and 110)
+  static constexpr bool Q_SHARED = NT >= 4;
+  static constexpr int Q_BYTES = Q_SHARED ? NT * CH * 512 : 0;
+  uint4 q[Q_SHARED ? 1 : NT][Q_SHARED ? 1 : CH];
+  const uint4* q_at;
   float acc[NT][U][4][4], m[NT][2], l[NT][2];
   int pos[NT][2];
   int live;   // instructions' worth of rows in use
 
-  __device__ __forceinline__ void begin(const AttnArgs& a, const AttnReq& r, int h, int m0, int m1) {
+  // (Q_SHARED: between two barriers; the warps take a share of the fragments each)
+  __device__ __forceinline__ void begin(const AttnArgs& a, const AttnReq& r, int h, int m0, int m1, char* s_q) {
     const int g = (threadIdx.x & 31) >> 2, c = threadIdx.x & 3, rep = a.pool.rep;
+    q_at = reinterpret_cast<const uint4*>(s_q) + (threadIdx.x & 31);
     live = (m1 - m0 + 7) / 8;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -79,8 +86,14 @@ struct FewBf16 {
 #pragma unroll
       for (int k = 0; k < CH; ++k) {
         uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (mq < m1) x = *reinterpret_cast<const uint4*>(src + k * 64);
-        q[nt][k][0] = x.x; q[nt][k][1] = x.y; q[nt][k][2] = x.z; q[nt][k][3] = x.w;
+        if constexpr (Q_SHARED) {
+          if (k % FEW_WARPS != (int)(threadIdx.x >> 5)) continue;
+          if (mq < m1) x = *reinterpret_cast<const uint4*>(src + k * 64);
+          reinterpret_cast<uint4*>(s_q)[(nt * CH + k) * 32 + (threadIdx.x & 31)] = x;
+        } else {
+          if (mq < m1) x = *reinterpret_cast<const uint4*>(src + k * 64);
+          q[nt][k] = x;
+        }
       }
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -132,8 +145,11 @@ struct FewBf16 {
       s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
 #pragma unroll
       for (int x = 0; x < CH; ++x) {
-        few_mma(s[nt], kk[0][x].x, kk[1][x].x, kk[0][x].y, kk[1][x].y, q[nt][x][0], q[nt][x][1]);
-        few_mma(s[nt], kk[0][x].z, kk[1][x].z, kk[0][x].w, kk[1][x].w, q[nt][x][2], q[nt][x][3]);
+        uint4 y;
+        if constexpr (Q_SHARED) y = q_at[(nt * CH + x) * 32];
+        else y = q[nt][x];
+        few_mma(s[nt], kk[0][x].x, kk[1][x].x, kk[0][x].y, kk[1][x].y, y.x, y.y);
+        few_mma(s[nt], kk[0][x].z, kk[1][x].z, kk[0][x].w, kk[1][x].w, y.z, y.w);
       }
     }
     const int key = b * OPS_BLOCK + g;
@@ -232,11 +248,13 @@ struct FewBf16 {
 template <int HD>
 struct FewFp32 {
   static constexpr int MR = HD == 128 ? 4 : 8, J = HD / 32, PITCH = HD + 4;
+  static constexpr bool Q_SHARED = false;
+  static constexpr int Q_BYTES = 0;
   float4 q[MR][J], acc[MR][J];
   float m[MR], l[MR];
   int pos[MR];
 
-  __device__ __forceinline__ void begin(const AttnArgs& a, const AttnReq& r, int h, int m0, int m1) {
+  __device__ __forceinline__ void begin(const AttnArgs& a, const AttnReq& r, int h, int m0, int m1, char*) {
     const int s = threadIdx.x & 7, rep = a.pool.rep;
 #pragma unroll
     for (int i = 0; i < MR; ++i) {
@@ -367,7 +385,8 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) blink_attn_few_kernel(const
   extern __shared__ __align__(16) char s_dyn[];
   float* s_acc = reinterpret_cast<float*>(s_dyn);                                        // [FEW_WARPS][MR][PITCH]
   float2* s_ml = reinterpret_cast<float2*>(s_acc + FEW_WARPS * MR * PITCH);              // [FEW_WARPS][MR]
-  long long* s_pre = reinterpret_cast<long long*>(s_ml + FEW_WARPS * MR);                // [n + 1] tiles before a request
+  char* s_q = reinterpret_cast<char*>(s_ml + FEW_WARPS * MR);
+  long long* s_pre = reinterpret_cast<long long*>(s_q + W::Q_BYTES);                     // [n + 1] tiles before a request
   int2* s_len = reinterpret_cast<int2*>(s_pre + a.n + 1);                                // [n] first row, kv_len
   __shared__ long long s_warp[FEW_WARPS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -442,7 +461,8 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) blink_attn_few_kernel(const
     auto block_of = [&](int t) { return t < span.sinks ? t : span.from + t - span.sinks; };
     int id = -1;   // of the warp's tile number `lane`, of 32 at a time
     if (t0 + warp + FEW_WARPS * lane < stop && last >= 0) id = table[block_of(t0 + warp + FEW_WARPS * lane)];
-    w.begin(a, req, h, m0, m1);
+    w.begin(a, req, h, m0, m1, s_q);   // (the barrier before it: that behind the tiles of the segment before)
+    if constexpr (W::Q_SHARED) __syncthreads();
     int i = 0;
     for (int t = t0 + warp; t < stop; t += FEW_WARPS, ++i) {
       if (i == 32) {
@@ -602,7 +622,8 @@ __global__ void __launch_bounds__(FEW_THREADS) blink_attn_near_kernel(const __gr
     const int t0 = rank * FEW_WARPS + warp, step = ctas * FEW_WARPS;   // the warp's tiles
     int id = -1;   // of its tile number `lane`, of 32 at a time
     if (t0 + step * lane < span.n && last >= 0) id = table[block_of(t0 + step * lane)];
-    w.begin(a, req, h, m0, m1);
+    w.begin(a, req, h, m0, m1, reinterpret_cast<char*>(s_rec + MR));
+    if constexpr (W::Q_SHARED) __syncthreads();
     int i = 0;
     for (int t = t0; t < span.n; t += step, ++i) {
       if (i == 32) {
@@ -667,10 +688,10 @@ template <typename T, int HD, typename W, int CTAS>
 static int few_run(const AttnArgs& a, int sms, void* stream) {
   if (a.near_ctas > 0) {
     const int64_t ctas = (int64_t)a.n * a.pool.Hkv * a.near_groups * a.near_ctas;
-    const size_t need = (size_t)FEW_WARPS * W::MR * (W::PITCH * 4 + 8) + W::MR * 8;
+    const size_t need = (size_t)FEW_WARPS * W::MR * (W::PITCH * 4 + 8) + W::MR * 8 + W::Q_BYTES;
     return ops_launch(blink_attn_near_kernel<T, HD, W>, ctas, FEW_THREADS, need, stream, a.near_ctas, a, a.near_groups);
   }
-  const size_t smem = (size_t)FEW_WARPS * W::MR * (W::PITCH * 4 + 8) + (size_t)(a.n + 1) * 16;
+  const size_t smem = (size_t)FEW_WARPS * W::MR * (W::PITCH * 4 + 8) + W::Q_BYTES + (size_t)(a.n + 1) * 16;
   const int grid = sms * CTAS < FEW_MAX_CTAS ? sms * CTAS : FEW_MAX_CTAS;
   const int rc = ops_launch(blink_attn_few_kernel<T, HD, W, CTAS>, grid, FEW_THREADS, smem, stream, 0, a);
   if (rc != BLINK_OK) return rc;
@@ -715,7 +736,7 @@ int blink_window_attention(const blink_model_cfg* model, const blink_kv_pool* kv
     return BLINK_EINVAL;
   if (rows < 1 || n_requests < 1 || table_stride < 1 || window < 0 || sinks < 0 || max_new < 1) return BLINK_EINVAL;
   if (q_stride < q_dim || out_stride < q_dim || q_stride % 8 || out_stride % 8) return BLINK_EINVAL;
-  if (n_requests > OPS_MAX_REQUESTS || rows > 0x3ffffff || table_stride > 0x7ffffff || sinks > 0x3fffffff || window > 0x3fffffff) return BLINK_ETOOBIG;
+  if (n_requests > OPS_MAX_REQUESTS || rows > 0x3ffffff || table_stride > 0x3ffffff || sinks > 0x3fffffff || window > 0x3fffffff) return BLINK_ETOOBIG;
   if (!ops_aligned(workspace, 256) || workspace_bytes < blink_window_attention_workspace(model, max_new)) return BLINK_EINVAL;
   int dev = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return BLINK_ECUDA;
