@@ -56,7 +56,8 @@ def check_tables(ctx, new, held, free, count, table, rows, out=None, cap=None):
 
 
 @pytest.mark.parametrize("n,ctx,new,spare", [(1, 0, 1, 0), (1, 40, 1, 3), (3, 20, 40, 5), (31, 100, 3, 0), (256, 300, 8, 77), (257, 60, 33, 1),
-                                             (1025, 50, 2, 0), (4096, 30, 3, 9), (40, 2000, 700, 100)])
+                                             (1025, 50, 2, 0), (4096, 30, 3, 9), (40, 2000, 700, 100), (200, 50, 600, 9),
+                                             (3, 0, 20000, 70000)])
 def test_tables(n, ctx, new, spare):
     case = list(tables_case(np.random.default_rng(n), n, ctx, new, spare))
     case[6] = max(1, case[6])
@@ -95,7 +96,7 @@ def test_tables_in_place_and_entries_that_are_no_block():
 
 
 # ---- norms, rotation, cache -------------------------------------------------------------------------------------------
-@pytest.mark.parametrize("rows", [1, 3, 64, 300])
+@pytest.mark.parametrize("rows", [1, 3, 64, 300, 3001])   # (the last: several groups of heads a warp)
 @pytest.mark.parametrize("rep,hkv,hd,dtype,qkv", [(4, 2, 128, "bf16", "bf16"), (1, 3, 64, "bf16", "bf16"), (8, 1, 128, "bf16", "fp32"), (2, 2, 64, "fp32", "fp32"),
                                                   (4, 8, 64, "bf16", "fp32"), (1, 1, 128, "fp32", "fp32")])
 @pytest.mark.parametrize("gains", ["both", "q", None])
@@ -280,6 +281,62 @@ def test_attention_large_scores_and_out_over_q():
     assert torch.equal(q, out)
 
 
+def test_attention_tiles_of_long_requests():
+    """More tiles than the rings of shared memory hold, windows that cut tiles anywhere, sinks inside and outside of them."""
+    for rep, hkv, hd in ((4, 1, 128), (1, 1, 128), (8, 1, 64), (2, 1, 64)):
+        for window, sinks in ((0, 0), (200, 5), (511, 0), (64, 150), (700, 16)):
+            c = attention_case(shape(rep, hkv, hd), [900, 0, 77], [50, 130, 1], window, sinks, seed=window + rep)
+            check_attention(c, run_attention(c))
+
+
+def test_attention_many_units_per_cta():
+    """More units than a CTA has records for, in every CTA."""
+    c = attention_case(shape(8, 8, 64), [3] * 45, [140] * 45, 40, 3, seed=7)
+    out = run_attention(c)
+    check_attention(c, out, only=[0, 22, 44])
+    assert torch.equal(out, run_attention(c))          # who takes which unit changes nothing
+
+
+@pytest.mark.parametrize("rep,hkv,hd,dtype", [(4, 1, 128, "bf16"), (4, 1, 64, "bf16"), (2, 1, 64, "fp32")])
+@pytest.mark.parametrize("rising", [True, False])
+def test_attention_scores_that_rise_and_fall(rep, hkv, hd, dtype, rising):
+    """The largest score grows by far more than 2^8 from tile to tile, or is the first key's: every way to rescale."""
+    for new in (1, 5, 90):
+        c = attention_case(shape(rep, hkv, hd, dtype), [600], [new], 0, 0, seed=new)
+        n = 600 + new
+        d = torch.randn(hd, device="cuda")
+        j = torch.arange(n, device="cuda", dtype=torch.float32)
+        size = (j if rising else n - j) * (150.0 / n)
+        k = (size[:, None] * d / d.norm() + 0.1 * torch.randn(n, hd, device="cuda")).to(c["pool"].dtype)
+        block = c["table"][0].long()[torch.arange(n, device="cuda") // BS]
+        c["pool"][1, 0][block, 0, torch.arange(n, device="cuda") % BS] = k
+        c["kv"][0][0, :, 0] = f64(k)
+        c["q"].copy_((d / d.norm() * 30.0).to(c["q"].dtype).repeat(rep)[None, :])
+        check_attention(c, run_attention(c))
+
+
+def test_attention_two_calls_at_once():
+    cases = [attention_case(shape(4, 2, 128), [500, 20, 300], [1, 60, 4], 100, 4, seed=1), attention_case(shape(4, 2, 64), [90, 700], [200, 1], 0, 0, seed=2)]
+    want = [run_attention(c) for c in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    got = [[], []]
+    for _ in range(10):
+        for i, (st, c) in enumerate(zip(streams, cases)):
+            with torch.cuda.stream(st):
+                got[i].append(run_attention(c))
+    torch.cuda.synchronize()
+    for w, g in zip(want, got):
+        assert all(torch.equal(w, x) for x in g)
+
+
+def test_attention_the_workspace_says_that_no_wait_ran_out():
+    c = attention_case(shape(4, 2, 128), [50, 3], [90, 1], 0, 0)
+    ws = torch.full((B.blink_window_attention_workspace(c["m"], 90),), 255, dtype=torch.uint8, device="cuda")
+    check_attention(c, run_attention(c, workspace=ws))
+    assert int(ws[:4].view(torch.int32)) == B.BLINK_OK
+
+
 def test_attention_max_new_is_a_hint():
     c = attention_case(shape(4, 2, 128), [90, 20, 300], [1, 90, 6], 64, 4, seed=5)
     for hint in (1, 2, 5, 90, 10000):
@@ -331,7 +388,7 @@ def check_verify(c, tokens, accepted):
             assert accepted[r] == n and np.array_equal(tokens[a:b], want), (r, n, accepted[r], want, tokens[a:b], near)
 
 
-@pytest.mark.parametrize("V", [2, 31, 257, 1000, 4096, 4097, 32000])
+@pytest.mark.parametrize("V", [2, 31, 257, 1000, 4096, 4097, 32000, 50001])
 @pytest.mark.parametrize("probs", [True, False])
 def test_verify(V, probs):
     rng = np.random.default_rng(V)
@@ -352,6 +409,21 @@ def test_verify_many_draws_of_flat_rows():
     rng = np.random.default_rng(2)
     c = verify_case(rng, [1] * 150, 5000, True, [1.0] * 150, spread=0.05)
     check_verify(c, *run_verify(c))
+
+
+def test_verify_long_drafts():
+    rng = np.random.default_rng(5)
+    c = verify_case(rng, [150, 3], 600, True, [1.0, 0.9])
+    c["ua"] *= 0.01                          # most are accepted
+    check_verify(c, *run_verify(c))
+
+
+def test_verify_the_same_call_gives_the_same_tokens():
+    rng = np.random.default_rng(6)
+    c = verify_case(rng, [3] * 40, 9000, True, [1.0] * 40, spread=0.1)
+    first = run_verify(c)
+    for _ in range(5):
+        assert all(torch.equal(x, y) for x, y in zip(first, run_verify(c)))
 
 
 def test_verify_special_entries():
