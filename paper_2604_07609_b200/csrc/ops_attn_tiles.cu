@@ -260,6 +260,10 @@ struct alignas(16) TilUnit {
   AttnSpan span;
   int last;                // position of the last row
   int begin[2], end[2];    // tiles of each stream
+  // (an array indexed with a register would lie in local memory, all of the record with it)
+  __device__ __forceinline__ int live_of(int s) const { return s ? live[1] : live[0]; }
+  __device__ __forceinline__ int begin_of(int s) const { return s ? begin[1] : begin[0]; }
+  __device__ __forceinline__ int end_of(int s) const { return s ? end[1] : end[0]; }
 };
 constexpr int TIL_UNITS = 8;   // records of a CTA's units, used in turn: nobody is more than a few behind the warp that writes them
 
@@ -352,12 +356,12 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
     t.span = attn_span(a, t.pos, t.last);
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      const int first = t.pos + s * P, last = max(0, first + t.live[s] - 1);
+      const int first = t.pos + s * P, last = max(0, first + t.live_of(s) - 1);
       const int from = a.window > 0 ? max(0, first - a.window + 1) / OPS_BLOCK : 0;
       t.begin[s] = a.sinks > 0 ? 0 :   // (the sinks may lie in the unit's window, and not in the stream's)
                                    min(max(0, from - t.span.from), t.span.n - 1) / TIL_BLOCKS;
       t.end[s] = min(t.span.n - 1, max(0, t.span.sinks + last / OPS_BLOCK - t.span.from)) / TIL_BLOCKS + 1;
-      if (t.live[s] == 0) t.begin[s] = t.end[s] = 0;
+      if (t.live_of(s) == 0) t.begin[s] = t.end[s] = 0;
     }
     return t;
   };
@@ -395,7 +399,7 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
       for (int k = 0; k < CH / 2; ++k) {
         const int i = k * 256 + (int)(threadIdx.x & 255), row = i / CH, ck = i % CH;
         const int r = row >> lr;
-        const bool live = r < t.live[s];
+        const bool live = r < t.live_of(s);
         const char* src = static_cast<const char*>(a.q) + ((long long)(t.row + (live ? s * P + r : 0)) * a.q_stride + ((t.h << lr) + (row & (rep - 1))) * HD + ck * 8) * 2;
         const uint32_t dst = b_q + (ck >> 3) * 16384 + row * 128 + (((ck & 7) ^ (row & 7)) << 4);
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16u : 0u) : "memory");
@@ -417,25 +421,25 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
     };
     TilUnit t = unit_of(0);
     together(t);
-    if (t.live[0] && t.live[s]) {
+    if (t.live[0] && t.live_of(s)) {
       load_q(t);
       q_there();
     }
 #pragma unroll 1
     for (int u = 0; t.live[0]; ++u) {
       bool more = false;   // a next unit, in which the stream has rows
-      if (t.live[s]) {
+      if (t.live_of(s)) {
         const int r = m >> lr;
         TilMask mask;
-        mask.pos = r < t.live[s] ? t.pos + s * P + r : -1;
+        mask.pos = r < t.live_of(s) ? t.pos + s * P + r : -1;
         mask.window = a.window;
         mask.sinks = a.sinks;
         mask.n_sinks = t.span.sinks;
         mask.from = t.span.from;
         const int p_hi = t.pos + s * P + ((q * 32 + 31) >> lr);
-        const int begin = t.begin[s], end = t.end[s];
+        const int begin = t.begin_of(s), end = t.end_of(s);
         const int t_row0 = t.row + s * P, t_head = (t.h << lr) + (m & (rep - 1));
-        const bool mine = r < t.live[s];
+        const bool mine = r < t.live_of(s);
         float mx_used = -INFINITY, l = 0.f;
 #pragma unroll 1
         for (int j = begin; j < end; ++j) {
@@ -454,7 +458,7 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
           }
           if (j + 1 == end) {   // the last scores are complete: the queries have been read
             t = unit_of(u + 1);
-            more = t.live[0] > 0 && t.live[s] > 0;
+            more = t.live[0] > 0 && t.live_of(s) > 0;
             if (more) load_q(t);
           }
           uint32_t p[32];
@@ -538,7 +542,7 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
       } else {
         t = unit_of(u + 1);
         together(t);
-        if (t.live[0] && t.live[s]) {
+        if (t.live[0] && t.live_of(s)) {
           load_q(t);
           q_there();
         }
