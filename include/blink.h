@@ -426,7 +426,7 @@ int blink_build_tables(const int32_t* ctx_len, const int32_t* new_len, const int
  * [hd]; NULL: not normed), then pairs (i, i + hd/2) are turned by position * rope_theta^(-2i/hd) (angles in 64 bits).  q
  * goes to q_out [rows][Hq * hd] (model dtype, q_stride), which may be qkv itself (same dtype and stride) but not overlap it
  * otherwise; k and v to the row's slot.  A row whose slot is not one of the pool's is not cached; a row with a negative
- * position is left alone.  Two rows of one slot: either of them.  Pointers 16-byte aligned, strides multiples of 8. */
+ * position is left alone.  Two rows of one slot: each head of it is of either.  Pointers 16-byte aligned, strides multiples of 8. */
 int blink_qk_norm_rope(const blink_model_cfg* model, const blink_kv_pool* kv, int layer, const void* qkv, int qkv_dtype,
                        int64_t qkv_stride, const float* q_gain, const float* k_gain, const int32_t* positions,
                        const int32_t* slot_map, int rows, void* q_out, int64_t q_stride, void* stream);
@@ -463,7 +463,7 @@ uint64_t blink_verify_workspace(int rows, int n_requests, int vocab);
  * token outside the vocabulary is refused.
  *   out_tokens [rows]          the accepted drafts, the token drawn, then -1
  *   n_accepted [n_requests]    0 .. k (a request without rows: 0)
- * Acceptance compares in 64 bits (the sum of exponentials to about 1e-8), the draw is in 64 bits throughout.  fp32 [rows][vocab] logits
+ * Acceptance compares in 64 bits (the sum of exponentials to about 1e-8, 1e-6 at worst), the draw is in 64 bits throughout.  fp32 [rows][vocab] logits
  * and probabilities with their strides; draft_probs is not read in a request's last row. */
 int blink_verify_drafts(const float* logits, int64_t logits_stride, int rows, int vocab, const int32_t* row_start, int n_requests,
                         const int32_t* draft_tokens, const float* draft_probs, int64_t probs_stride, const float* temperature,

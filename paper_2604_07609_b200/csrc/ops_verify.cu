@@ -8,7 +8,8 @@
 //   rows    largest value and sum of exponentials of pieces of 1024 entries of every row, a warp each: one pass over the logits, which is what
 //           bounds the whole (HBM: 4 bytes an entry).  A lane has its 32 entries on their way at once and sums against its own largest
 //           value, so that nothing waits for another warp.  Exponentials in 32 bits, sums of a lane's entries in 32, everything above in
-//           64: the acceptance test is off by some 1e-8.
+//           64: the acceptance test is off by some 1e-8 where the entries differ, and by 1e-6 at worst (most of the weight on entries that are
+//           all alike, 12 below the largest: an argument's rounding of 2^-24 of itself, and the exponential's own 2^-22).
 //   choose  a CTA per request: the first refused draft, from the pieces
 //   draw    a cluster of 16 CTAs per request: the exponentials of that row, which stay in registers (up to 16 a thread), their sum, then the weights
 //           max(0, p - q), their sum, and the entry at which the running sum passes its target.  Sums go from CTA to CTA through
@@ -183,7 +184,7 @@ __device__ __forceinline__ VerExp ver_exp_of(const double* table, float top, flo
   x.scale = 16.0 * 1.44269504088896340736 / (double)T;
   x.shift = -(double)top * x.scale;
   x.top = top;
-  x.below = fmaxf(top - 700.f * T, -3e38f);   // (above -inf)
+  x.below = fmaxf(__double2float_ru((double)top - 700.0 * (double)T), -3.402823466e38f);   // (rounded up: no less than -700; above -inf)
   return x;
 }
 __device__ __forceinline__ double ver_exp(const VerExp& x, float z) {

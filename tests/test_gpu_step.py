@@ -337,6 +337,53 @@ def test_attention_the_workspace_says_that_no_wait_ran_out():
     assert int(ws[:4].view(torch.int32)) == B.BLINK_OK
 
 
+def test_attention_calls_behind_one_another_share_a_workspace():
+    cases = [attention_case(shape(4, 2, 128), [500, 20, 300], [1, 60, 4], 100, 4, seed=1), attention_case(shape(4, 1, 128), [900], [1], 0, 0, seed=2),
+             attention_case(shape(4, 2, 128, "fp32"), [90, 300], [50, 1], 0, 0, seed=3), attention_case(shape(8, 2, 64), [2000, 5], [2, 2], 0, 0, seed=4)]
+    want = [run_attention(c) for c in cases]
+    ws = torch.empty(max(B.blink_window_attention_workspace(c["m"], 60) for c in cases), dtype=torch.uint8, device="cuda")
+    got = [run_attention(cases[i % 4], workspace=ws) for i in range(80)]
+    assert all(torch.equal(g, want[i % 4]) for i, g in enumerate(got))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_attention_a_query_that_is_no_number_stays_with_its_row(dtype, bad):
+    for new in (1, 5, 90):
+        c = attention_case(shape(4, 2, 64, dtype), [300, 30, 7], [new, new, 1], 50, 4, seed=new)
+        rows = [new - 1, new]                              # the first request's last row, the second's first
+        c["q"][rows] = 0
+        out = run_attention(c)
+        c["q"][rows, 3::64] = bad
+        other = run_attention(c)
+        assert not torch.isfinite(other[rows]).any()
+        c["q"][rows], other[rows] = 0, out[rows]
+        check_attention(c, other)
+
+
+def test_attention_and_rotation_far_into_a_large_pool():
+    """Blocks whose elements are more than 2^31, and their bytes more than 2^32, behind the pool's first."""
+    blocks = 140_000
+    if torch.cuda.mem_get_info()[0] < 12 << 30:
+        pytest.skip("needs 12 GB")
+    for new in (1, 4, 70):
+        c = attention_case(shape(4, 8, 128, layers=1), [200, 30, 0], [new, 1, new], 0, 0, seed=new, layer=0)
+        small = c["pool"].shape[2]
+        pool = torch.empty(1, 2, blocks, 8, BS, 128, dtype=torch.bfloat16, device="cuda")
+        pool[:, :, blocks - small:] = c["pool"]
+        c["table"] = torch.where((c["table"] >= 0) & (c["table"] < small), c["table"] + (blocks - small), c["table"])
+        want = run_attention(c | {"table": torch.where(c["table"] >= blocks - small, c["table"] - (blocks - small), -1)})
+        c["pool"] = pool
+        assert torch.equal(run_attention(c), want)
+    m, n = c["m"], 40
+    x = torch.randn(n, m.qkv_dim, device="cuda").bfloat16()
+    slots = blocks * BS - 1 - torch.randperm(n, device="cuda", dtype=torch.int32)
+    B.blink_qk_norm_rope(m, pool, 0, x, None, None, ints(np.zeros(n)), slots)       # position 0: as they are
+    heads = x[:, m.q_dim:].reshape(n, 2, 8, 128)
+    for i in (0, 1):
+        assert torch.equal(pool[0, i][slots.long() // BS, :, slots.long() % BS], heads[:, i])
+
+
 def test_attention_max_new_is_a_hint():
     c = attention_case(shape(4, 2, 128), [90, 20, 300], [1, 90, 6], 64, 4, seed=5)
     for hint in (1, 2, 5, 90, 10000):
@@ -448,6 +495,21 @@ def test_verify_special_entries():
     c["ua"][s[9]] = np.nan
     z[s[10]:s[11], 100:] = -np.inf           # most of the row without weight
     check_verify(c, *run_verify(c))
+
+
+def test_verify_temperatures_at_the_ends_of_their_range():
+    step = 2.0 ** -19   # between neighbours at 22
+    low = np.zeros(1000, np.float32)
+    low[100:400] = np.float32(22 - 4 * step)   # exp(-790): nothing, and below what a 64-bit exponent holds
+    low[5] = 22.0
+    wide = np.zeros(1000, np.float32)
+    wide[0] = -3.4e38                          # exp(-3.4) of the others' weight
+    c = dict(z=np.stack([low, low, low, wide, wide]), V=1000, start=np.array([0, 1, 3, 4, 5]), draft=np.array([0, 5, 0, 0, 0]), q=None,
+             T=np.array([4 * step / 790, 4 * step / 790, 1e38, 1e38], np.float32), ua=np.full(5, 0.5, np.float32),
+             up=np.array([0.5, 0.999, 1e-5, 1e-4], np.float32))
+    tokens, accepted = run_verify(c)
+    check_verify(c, tokens, accepted)
+    assert tokens.tolist() == [5, 5, 5, 0, 1] and accepted.tolist() == [0, 1, 0, 0]
 
 
 def test_verify_rows_behind_the_last_request_and_requests_without_rows():
