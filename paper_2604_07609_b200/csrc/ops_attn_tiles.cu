@@ -43,6 +43,8 @@ struct TilShared {
   uint64_t q_full[2], s_full[2], p_full[2], o_full[2];
   uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], v_land, unit_full[8];
   float row[2][2][128];   // of a stream's rows, from either of their threads: maxima, or sums
+  uint64_t x_full, x_done;   // a unit that the streams share: stream 1's results are there; have been read
+  float2 other[128];         // maxima and sums of stream 1's rows then
   uint32_t tmem;
   int dead;
   int warp_sum[TIL_WARPS];
@@ -259,7 +261,8 @@ struct alignas(16) TilUnit {
   int pos;                 // position of the first row
   AttnSpan span;
   int last;                // position of the last row
-  int begin[2], end[2];    // tiles of each stream
+  int split;               // 1: rows for one stream only; both have them, stream 0 the even tiles and stream 1 the odd ones
+  int begin[2], end[2];    // tiles of each stream: every one, or every second
   // (an array indexed with a register would lie in local memory, all of the record with it)
   __device__ __forceinline__ int live_of(int s) const { return s ? live[1] : live[0]; }
   __device__ __forceinline__ int begin_of(int s) const { return s ? begin[1] : begin[0]; }
@@ -294,6 +297,8 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
       til_init(&sh.v_empty[i], 1);
     }
     til_init(&sh.v_land, 1);
+    til_init(&sh.x_full, TIL_SOFT / 2);
+    til_init(&sh.x_done, TIL_SOFT / 2);
     for (int i = 0; i < TIL_UNITS; ++i) til_init(&sh.unit_full[i], 1);
     sh.dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -363,6 +368,12 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
       t.end[s] = min(t.span.n - 1, max(0, t.span.sinks + last / OPS_BLOCK - t.span.from)) / TIL_BLOCKS + 1;
       if (t.live_of(s) == 0) t.begin[s] = t.end[s] = 0;
     }
+    t.split = t.live[1] == 0 && t.end[0] > 1;
+    if (t.split) {
+      t.live[1] = t.live[0];
+      t.begin[1] = 1;
+      t.end[1] = t.end[0];
+    }
     return t;
   };
   // the CTA's i-th unit, live[0] == 0: there is none
@@ -392,7 +403,7 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
     const uint32_t t_row = (uint32_t)(q * 32) << 16;
     const uint32_t t_s = tmem + (uint32_t)(s * 128) + t_row, t_o = tmem + 256u + (uint32_t)(s * HD + half * (HD / 2)) + t_row;
     const uint32_t b_q = til_smem(base) + S::Q + s * S::TILE;
-    uint32_t n_s = 0, n_o = 0;
+    uint32_t n_s = 0, n_o = 0, n_x = 0;
     auto load_q = [&](const TilUnit& t) {
       constexpr int CH = HD / 8;   // 16-byte pieces of a row
 #pragma unroll 4
@@ -400,7 +411,7 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
         const int i = k * 256 + (int)(threadIdx.x & 255), row = i / CH, ck = i % CH;
         const int r = row >> lr;
         const bool live = r < t.live_of(s);
-        const char* src = static_cast<const char*>(a.q) + ((long long)(t.row + (live ? s * P + r : 0)) * a.q_stride + ((t.h << lr) + (row & (rep - 1))) * HD + ck * 8) * 2;
+        const char* src = static_cast<const char*>(a.q) + ((long long)(t.row + (live ? (t.split ? 0 : s * P) + r : 0)) * a.q_stride + ((t.h << lr) + (row & (rep - 1))) * HD + ck * 8) * 2;
         const uint32_t dst = b_q + (ck >> 3) * 16384 + row * 128 + (((ck & 7) ^ (row & 7)) << 4);
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16u : 0u) : "memory");
       }
@@ -429,20 +440,20 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
     for (int u = 0; t.live[0]; ++u) {
       bool more = false;   // a next unit, in which the stream has rows
       if (t.live_of(s)) {
-        const int r = m >> lr;
+        const int r = m >> lr, split = t.split, off = split ? 0 : s * P, step = 1 + split;
         TilMask mask;
-        mask.pos = r < t.live_of(s) ? t.pos + s * P + r : -1;
+        mask.pos = r < t.live_of(s) ? t.pos + off + r : -1;
         mask.window = a.window;
         mask.sinks = a.sinks;
         mask.n_sinks = t.span.sinks;
         mask.from = t.span.from;
-        const int p_hi = t.pos + s * P + ((q * 32 + 31) >> lr);
+        const int p_hi = t.pos + off + ((q * 32 + 31) >> lr);
         const int begin = t.begin_of(s), end = t.end_of(s);
-        const int t_row0 = t.row + s * P, t_head = (t.h << lr) + (m & (rep - 1));
+        const int t_row0 = t.row + off, t_head = (t.h << lr) + (m & (rep - 1));
         const bool mine = r < t.live_of(s);
         float mx_used = -INFINITY, l = 0.f;
 #pragma unroll 1
-        for (int j = begin; j < end; ++j) {
+        for (int j = begin; j < end; j += step) {
           mask.first_block = j * TIL_BLOCKS;
           const int i0 = mask.first_block, i1 = i0 + TIL_BLOCKS - 1;
           const int lowest = i1 < mask.n_sinks ? a.window + p_hi : (mask.from + max(0, i0 - mask.n_sinks)) * OPS_BLOCK;   // of its blocks behind the sinks
@@ -456,7 +467,7 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
             til_pair_sync(pair);
             mx_used = fmaxf(x, sh.row[s][half ^ 1][m]);
           }
-          if (j + 1 == end) {   // the last scores are complete: the queries have been read
+          if (j + step >= end) {   // the last scores are complete: the queries have been read
             t = unit_of(u + 1);
             more = t.live[0] > 0 && t.live_of(s) > 0;
             if (more) load_q(t);
@@ -506,10 +517,29 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
         sh.row[s][half][m] = l;
         til_pair_sync(pair);
         l += sh.row[s][half ^ 1][m];
-        const float inv = l > 0.f ? __fdividef(1.0f, l) : 0.f;
         wait(&sh.o_full[s], n_o & 1u);
         ++n_o;
         til_fence_after();
+        float f0 = l > 0.f ? __fdividef(1.0f, l) : 0.f, f1 = 0.f;
+        if (split) {
+          if (s == 1) {
+            if (half == 0) sh.other[m] = make_float2(mx_used, l);
+            til_fence_before();
+            __syncwarp();
+            if (lane == 0) til_arrive(&sh.x_full);
+            wait(&sh.x_done, n_x++ & 1u);   // (before the accumulator's next use)
+            together(t);
+            continue;
+          }
+          wait(&sh.x_full, n_x++ & 1u);
+          til_fence_after();
+          const float2 o = sh.other[m];
+          const float top = fmaxf(mx_used, o.x), g0 = mx_used == -INFINITY ? 0.f : attn_ex2(mx_used - top), g1 = o.x == -INFINITY ? 0.f : attn_ex2(o.x - top);
+          const float sum = l * g0 + o.y * g1;
+          const float inv = sum > 0.f ? __fdividef(1.0f, sum) : 0.f;
+          f0 = g0 * inv;
+          f1 = g1 * inv;
+        }
         const bool store = mine && ok;
         char* dst = static_cast<char*>(a.out) + ((long long)(t_row0 + (store ? r : 0)) * a.out_stride + t_head * HD + half * (HD / 2)) * 2;
 #pragma unroll 1
@@ -518,11 +548,27 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
           til_ld16(t_o + (uint32_t)k, x);
           til_ld16(t_o + (uint32_t)k + 16u, y);
           tmem_wait_ld_til(x, y);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            x[i] = __float_as_uint(__uint_as_float(x[i]) * f0);
+            y[i] = __float_as_uint(__uint_as_float(y[i]) * f0);
+          }
+          if (split) {
+            uint32_t x1[16], y1[16];
+            til_ld16(t_o + (uint32_t)(HD + k), x1);
+            til_ld16(t_o + (uint32_t)(HD + k) + 16u, y1);
+            tmem_wait_ld_til(x1, y1);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              x[i] = __float_as_uint(fmaf(__uint_as_float(x1[i]), f1, __uint_as_float(x[i])));
+              y[i] = __float_as_uint(fmaf(__uint_as_float(y1[i]), f1, __uint_as_float(y[i])));
+            }
+          }
           auto put = [&](const uint32_t(&v)[16], int at) {   // a lane's row lies alone: 32 bytes at a time, where they may
             uint32_t o[8];
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
-              const __nv_bfloat162 b2 = __floats2bfloat162_rn(__uint_as_float(v[2 * c]) * inv, __uint_as_float(v[2 * c + 1]) * inv);
+              const __nv_bfloat162 b2 = __floats2bfloat162_rn(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1]));
               o[c] = *reinterpret_cast<const uint32_t*>(&b2);
             }
             if (store && a.out_32) {
@@ -538,6 +584,10 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
           put(y, k + 16);
         }
         til_fence_before();      // (before the accumulator's next use: the next probabilities' arrival)
+        if (split) {
+          __syncwarp();
+          if (lane == 0) til_arrive(&sh.x_done);
+        }
         together(t);             // (and both have read the other's sum)
       } else {
         t = unit_of(u + 1);
@@ -560,14 +610,15 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
       const TilUnit t = unit_of(u);
       if (til_uniform((uint32_t)t.live[0]) == 0u) break;
       const int begin1 = (int)til_uniform((uint32_t)t.begin[1]), end0 = (int)til_uniform((uint32_t)t.end[0]), end1 = (int)til_uniform((uint32_t)t.end[1]);
-      const int tiles = max(end0, end1);   // (stream 0 takes tiles 0 .. end0 - 1, stream 1 begin1 .. end1 - 1, which is none where it has no rows)
+      const int tiles = max(end0, end1);   // (stream 0 takes tiles 0 .. end0 - 1, stream 1 begin1 .. end1 - 1, which is none where it has no rows; shared: 0, 2 .., and 1, 3 ..)
+      const int split = (int)til_uniform((uint32_t)t.split), step = 1 + split;
       auto scores = [&](int s, int j) {
         const uint32_t n = n_tile + (uint32_t)j, slot = n % S::RING;
         wait(&sh.k_full[slot], (n / S::RING) & 1u);
         if (!ok) return;
         til_fence_after();
         const uint64_t dq = til_desc(b0 + S::Q + s * S::TILE, 16, 1024), dk = til_desc(b0 + S::K + slot * S::TILE, 16, S::GROUP);
-        const bool last = s == 1 || j < begin1 || j >= end1;
+        const bool last = split || s == 1 || j < begin1 || j >= end1;
         if (til_elect()) {
 #pragma unroll
           for (int i = 0; i < HD / 16; ++i)
@@ -585,7 +636,7 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
         til_fence_after();
         const uint64_t dv = til_desc(b0 + S::V + slot * S::TILE, 1024, S::GROUP);
         const uint32_t keep = j > (s ? begin1 : 0) ? 1u : 0u;
-        const bool end = j + 1 == (s ? end1 : end0), last = s == 1 || j < begin1 || j >= end1;
+        const bool end = j + step >= (s ? end1 : end0), last = split || s == 1 || j < begin1 || j >= end1;
         if (til_elect()) {
 #pragma unroll
           for (int i = 0; i < TIL_BLOCKS; ++i)   // 16 keys each, a block of the cache
@@ -600,14 +651,15 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
       scores(0, 0);
       if (end1 > 0) {
         wait(&sh.q_full[1], n_q1++ & 1u);
-        if (begin1 == 0) scores(1, 0);
+        if (begin1 == split) scores(1, split);
       }
 #pragma unroll 1
-      for (int j = 0; j < tiles && ok; ++j) {
+      for (int j = 0; j < tiles && ok; j += step) {
+        const int j1 = j + split;
         if (j < end0) outputs(0, j, n_p0++);
-        if (j + 1 < end0) scores(0, j + 1);
-        if (j >= begin1 && j < end1) outputs(1, j, n_p1++);
-        if (j + 1 >= begin1 && j + 1 < end1) scores(1, j + 1);
+        if (j + step < end0) scores(0, j + step);
+        if (j1 >= begin1 && j1 < end1) outputs(1, j1, n_p1++);
+        if (j1 + step >= begin1 && j1 + step < end1) scores(1, j1 + step);
       }
       n_tile += (uint32_t)tiles;
     }

@@ -289,6 +289,16 @@ def test_attention_tiles_of_long_requests():
             check_attention(c, run_attention(c))
 
 
+@pytest.mark.parametrize("rep,hkv,hd", [(4, 2, 128), (1, 3, 128), (8, 1, 64), (2, 2, 64)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (300, 3), (140, 40)])
+def test_attention_few_rows_behind_many_keys(rep, hkv, hd, window, sinks):
+    """Units that fill one stream of rows only, with any number of tiles, beside full ones."""
+    c = attention_case(shape(rep, hkv, hd), [1500, 40, 250, 700, 3, 130, 120, 500], [17, 140, 33, 40, 260, 9, 33, 64], window, sinks, seed=rep)
+    out = run_attention(c)
+    check_attention(c, out)
+    assert torch.equal(out, run_attention(c))
+
+
 def test_attention_many_units_per_cta():
     """More units than a CTA has records for, in every CTA."""
     c = attention_case(shape(8, 8, 64), [3] * 45, [140] * 45, 40, 3, seed=7)
