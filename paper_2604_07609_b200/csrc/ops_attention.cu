@@ -31,6 +31,7 @@ constexpr int FEW_MAX_CTAS = 640;    // of a launch; the records are laid out fo
 constexpr int FEW_MIN_TILES = 4;     // of a CTA's run, while there are any
 constexpr int FEW_UNIT_TILES = 4;    // what a unit costs beside its tiles, in tiles
 constexpr int JOIN_THREADS = 256;
+constexpr int ALL_ROWS = 8, ALL_SHORT = 1024, ALL_KEYS = 8192;   // calls that take all requests to the tiles: rows (of a kv head) of the longest; keys that a row sees, at most
 constexpr int NEAR_CTAS = 16, NEAR_KEYS = 4096;   // a cluster per unit: its CTAs, keys that a row sees at most
 
 // What the join needs of a unit that was cut, written by the CTA in whose run it begins.
@@ -760,9 +761,19 @@ int blink_window_attention(const blink_model_cfg* model, const blink_kv_pool* kv
   const bool bf16 = model->dtype == BLINK_DTYPE_BF16;
   const bool tiles = (int64_t)max_new * a.pool.rep > (bf16 ? 32 : 8);   // there may be requests of more than a few rows
   if (tiles) a.few = (bf16 ? 8 * nt : 8) / a.pool.rep;
+  const int64_t keys = std::min<int64_t>((int64_t)table_stride * OPS_BLOCK, window > 0 ? (int64_t)window + sinks + max_new : INT64_MAX);
+  // Everything to the tiles, which share nothing out over CTAs, where there are units enough and none can be very long: a tile's rows cost the same
+  // however few they are, but its copies run by themselves.  (8B shape, us, with the kernels for few rows | without: 48 requests of 1 to 6 rows behind
+  // 300 to 5000 keys 116 | 86, of 1 to 3 91 | 86; 28 of them 77 | 60, 19 55 | 55, 10 34 | 46; 40 of 1 to 300 rows with a window of 256 51 | 41.  20 of 5
+  // rows behind 10000 keys 151 | 205.  10 of 1 to 6 rows behind 200 to 900 keys 23 | 17.  Eight rows of a head or less, one instruction of those
+  // kernels: 64 rows behind 5000 keys 197 us, 6.7 TB/s, which the tiles do not reach.)
+  const int64_t least = keys <= ALL_SHORT ? sms / 2 : sms + sms / 2;
+  if (bf16 && (int64_t)max_new * a.pool.rep > ALL_ROWS && (int64_t)n_requests * a.pool.Hkv >= least && keys <= ALL_KEYS) {
+    a.few = 0;
+    return attn_tiles(a, sms, stream);
+  }
   // So few units that each can have a cluster of 16 CTAs, and rows that see no more than NEAR_KEYS keys.  (8B shape, rows x keys, us, the sequence | clusters
   // of 16, 8, 4: 1 x 1000 12.5 | 8.9, 4 x 1000 14.6 | 17.7, 8 x 1000 16.7 | 16.9, 16 x 1000 20.8 | 22.9.)
-  const int64_t keys = std::min<int64_t>((int64_t)table_stride * OPS_BLOCK, window > 0 ? (int64_t)window + sinks + max_new : INT64_MAX);
   const int64_t mr = few_rows_of(model, max_new), rows_few = std::min<int64_t>(max_new, a.few);
   const int64_t groups = (rows_few * a.pool.rep + mr - 1) / mr, units = (int64_t)n_requests * a.pool.Hkv * groups;
   a.near_ctas = 0;

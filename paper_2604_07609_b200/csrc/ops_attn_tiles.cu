@@ -29,6 +29,7 @@ namespace blink {
 
 constexpr int TIL_KEYS = 128, TIL_BLOCKS = TIL_KEYS / OPS_BLOCK;
 constexpr int TIL_SOFT = 16, TIL_COPY = TIL_SOFT + 1, TIL_K = 1, TIL_WARPS = TIL_COPY + TIL_K + 1, TIL_THREADS = TIL_WARPS * 32;   // softmax; first of the copies, of them for keys; all
+constexpr int TIL_SORTED = 256;   // requests of a call that are put in order
 constexpr long long TIL_WAIT_CYCLES = 1ll << 32;   // some two seconds
 
 template <int HD>
@@ -48,6 +49,8 @@ struct TilShared {
   uint32_t tmem;
   int dead;
   int warp_sum[TIL_WARPS];
+  int weight[TIL_SORTED], count[TIL_SORTED];   // of requests: tiles of their last unit; units (by place)
+  uint16_t order[TIL_SORTED];                  // request of a place
 };
 
 __device__ __forceinline__ uint32_t til_smem(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -307,15 +310,43 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(til_smem(&sh.tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  // the sequence of units: a run of requests per thread
+  // The sequence of units: requests of more keys first, so that no CTA is left with a long unit at the end (48 requests of 300 to 5000 keys: in their
+// own order 99 us, so 86); beyond TIL_SORTED requests units are many and their order matters less.  A run of requests (or places) per thread.
+  const bool sorted = a.n <= TIL_SORTED;
+  auto units_of = [&](const AttnReq& q) { return q.rows > a.few ? (q.rows + 2 * P - 1) / (2 * P) * a.pool.Hkv : 0; };
   {
     const int each = (a.n + TIL_THREADS - 1) / TIL_THREADS;
     const int r0 = min(a.n, (int)threadIdx.x * each), r1 = min(a.n, r0 + each);
     int mine = 0;
-    for (int r = r0; r < r1; ++r) {
-      const AttnReq q = attn_req(a, a.row_start[r], a.row_start[r + 1], a.kv_len[r]);
-      s_pre[r] = mine;
-      if (q.rows > a.few) mine += (q.rows + 2 * P - 1) / (2 * P) * a.pool.Hkv;
+    if (sorted) {
+      const int r = threadIdx.x;
+      int weight = 0, count = 0;
+      if (r < a.n) {
+        const AttnReq q = attn_req(a, a.row_start[r], a.row_start[r + 1], a.kv_len[r]);
+        count = units_of(q);
+        if (count > 0) weight = attn_span(a, q.ctx + (q.rows - 1) / (2 * P) * (2 * P), q.ctx + q.rows - 1).n;
+        sh.weight[r] = weight;
+      }
+      __syncthreads();
+      if (r < a.n) {
+        int place = 0;
+        for (int k = 0; k < a.n; ++k) {
+          const int other = sh.weight[k];
+          place += other > weight || (other == weight && k < r);
+        }
+        sh.order[place] = (uint16_t)r;
+        sh.count[place] = count;
+      }
+      __syncthreads();
+      if (r < a.n) {
+        s_pre[r] = 0;
+        mine = sh.count[r];
+      }
+    } else {
+      for (int r = r0; r < r1; ++r) {
+        s_pre[r] = mine;
+        mine += units_of(attn_req(a, a.row_start[r], a.row_start[r + 1], a.kv_len[r]));
+      }
     }
     int x = mine;
 #pragma unroll
@@ -342,15 +373,16 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
   };
   auto make_unit = [&](int u) {
     TilUnit t;
-    int lo = 0, hi = a.n;   // the last request that begins at or before it
+    int lo = 0, hi = a.n;   // the last place that begins at or before it
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (s_pre[mid] <= u) lo = mid; else hi = mid;
     }
-    const AttnReq q = attn_req(a, a.row_start[lo], a.row_start[lo + 1], a.kv_len[lo]);
+    const int r = sorted ? sh.order[lo] : lo;
+    const AttnReq q = attn_req(a, a.row_start[r], a.row_start[r + 1], a.kv_len[r]);
     const int blocks = (q.rows + 2 * P - 1) / (2 * P);
-    const int i = u - s_pre[lo], b = blocks - 1 - i / a.pool.Hkv;   // later rows, which see more, first
-    t.req = lo;
+    const int i = u - s_pre[lo], b = max(0, blocks - 1 - i / a.pool.Hkv);   // later rows, which see more, first
+    t.req = r;
     t.h = i % a.pool.Hkv;
     t.row = q.start + b * 2 * P;
     const int rows = min(2 * P, q.rows - b * 2 * P);
@@ -765,6 +797,12 @@ static TilEncode til_encode() {
   return f;
 }
 
+// The kernel before the tiles where there are no requests for the other kernels: a status, and the counter of units.
+__global__ void blink_attn_begin_kernel(int* ws) {
+  ops_begin();
+  if (threadIdx.x < 2) ws[threadIdx.x] = 0;
+}
+
 template <int HD>
 static int tiles_run(const AttnArgs& a, int sms, int64_t most_units, void* stream) {
   using S = TilShape<HD>;
@@ -780,6 +818,10 @@ static int tiles_run(const AttnArgs& a, int sms, int64_t most_units, void* strea
     return BLINK_ECUDA;
   const size_t smem = (size_t)S::END + 1024 + TIL_UNITS * sizeof(TilUnit) + (size_t)(a.n + 1) * 4;
   const int64_t grid = most_units < sms ? most_units : sms;
+  if (a.few == 0) {
+    const int rc = ops_launch(blink_attn_begin_kernel, 1, 32, 0, stream, 0, reinterpret_cast<int*>(a.ws));
+    if (rc != BLINK_OK) return rc;
+  }
   return ops_launch(blink_attn_tiles_kernel<HD>, grid, TIL_THREADS, smem, stream, 0, a, map);
 }
 

@@ -299,6 +299,21 @@ def test_attention_few_rows_behind_many_keys(rep, hkv, hd, window, sinks):
     assert torch.equal(out, run_attention(c))
 
 
+@pytest.mark.parametrize("n,window,top", [(30, 0, 700), (12, 0, 400), (30, 200, 9000), (9, 3000, 5000)])
+def test_attention_batches_of_drafts(n, window, top):
+    """Calls that go to the tiles whole, to the kernels for few rows, or to both, by requests, rows and keys."""
+    rng = np.random.default_rng(n + window)
+    for most, rep in ((2, 4), (3, 4), (6, 4), (9, 4), (2, 8)):
+        new = rng.integers(0, most + 1, n)
+        new[0] = most
+        ctx = np.minimum(np.exp(rng.uniform(0, np.log(top), n)).astype(int), top)
+        ctx[1] = top
+        c = attention_case(shape(rep, 8, 64), ctx, new, window, 3 if window else 0, seed=most)
+        out = run_attention(c)
+        check_attention(c, out)
+        assert torch.equal(out, run_attention(c))
+
+
 def test_attention_many_units_per_cta():
     """More units than a CTA has records for, in every CTA."""
     c = attention_case(shape(8, 8, 64), [3] * 45, [140] * 45, 40, 3, seed=7)
