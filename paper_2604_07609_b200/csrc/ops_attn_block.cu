@@ -29,7 +29,7 @@ __global__ void __launch_bounds__(BLK_THREADS) blink_attn_block_kernel(const __g
   constexpr int BLK_ROWS = S::ROWS;
   extern __shared__ __align__(16) float s_f[];
   __shared__ int s_ids[BLK_IDS];   // of the list's first blocks
-  __shared__ int s_warp[BLK_THREADS / 32], s_unit[4];   // request, first row, rows and position of the unit's first
+  __shared__ int s_warp[BLK_THREADS / 32], s_unit[5];   // of the unit: request; its first row, rows and first position; rows (of a head) before it
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rep = a.pool.rep;
   ops_begin();
   // the unit: the CTA's place in the sequence of all of them, found by the thread whose run of requests holds it
@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(BLK_THREADS) blink_attn_block_kernel(const __g
         s_unit[1] = q.start;
         s_unit[2] = q.rows;
         s_unit[3] = q.ctx;
-        s_warp[0] = (at + g - 1 - place) * BLK_ROWS;   // later rows, which see more, first
+        s_unit[4] = (at + g - 1 - place) * BLK_ROWS;   // later rows, which see more, first
         break;
       }
       at += g;
@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(BLK_THREADS) blink_attn_block_kernel(const __g
   __syncthreads();
   const int r = s_unit[0];
   if (r < 0) return;   // (the grid is as large as it can have to be)
-  const int start = s_unit[1], ctx = s_unit[3], m0 = s_warp[0], m1 = min(s_unit[2] * rep, m0 + BLK_ROWS);
+  const int start = s_unit[1], ctx = s_unit[3], m0 = s_unit[4], m1 = min(s_unit[2] * rep, m0 + BLK_ROWS);
   const int first = ctx + m0 / rep, last = ctx + (m1 - 1) / rep;
   const AttnSpan span = attn_span(a, first, last);
   const int32_t* table = a.table + (long long)r * a.stride;
