@@ -31,7 +31,7 @@ constexpr int FEW_MAX_CTAS = 640;    // of a launch; the records are laid out fo
 constexpr int FEW_MIN_TILES = 4;     // of a CTA's run, while there are any
 constexpr int FEW_UNIT_TILES = 4;    // what a unit costs beside its tiles, in tiles
 constexpr int JOIN_THREADS = 256;
-constexpr int ALL_ROWS = 8, ALL_SHORT = 1024, ALL_KEYS = 8192;   // calls that take all requests to the tiles: rows (of a kv head) of the longest; keys that a row sees, at most
+constexpr int ALL_ROWS = 8, ALL_SHORT = 1024, ALL_KEYS = 8192, ALL_KEYS_32 = 256;   // calls that take all requests to the tiles: rows (of a kv head) of the longest; keys that a row sees, at most
 constexpr int NEAR_CTAS = 16, NEAR_KEYS = 4096;   // a cluster per unit: its CTAs, keys that a row sees at most
 
 // What the join needs of a unit that was cut, written by the CTA in whose run it begins.
@@ -781,6 +781,13 @@ int blink_window_attention(const blink_model_cfg* model, const blink_kv_pool* kv
   if (keys <= NEAR_KEYS && units * NEAR_CTAS <= sms) {
     a.near_groups = (int)groups;
     a.near_ctas = NEAR_CTAS;
+  }
+  // In 32 bits where a row sees so little that the kernels for few rows only add their launches.  (us, with them | without: the small shape, 8 requests of
+  // 40 rows behind 30 keys 17.1 | 13.1, 64 of one row and one of 40 behind 200 keys 46 | 26; the 8B shape, 4 and one 43 | 35, but behind 450 keys 24 | 62
+  // where the 40 rows see none of them.)
+  if (!bf16 && tiles && keys <= ALL_KEYS_32) {
+    a.few = 0;
+    return attn_blocks(a, sms, stream);
   }
   if (!bf16) {   // the many rows first: the few find room beside them
     const int done = tiles ? attn_blocks(a, sms, stream) : BLINK_OK;

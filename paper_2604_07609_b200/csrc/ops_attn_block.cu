@@ -32,6 +32,7 @@ __global__ void __launch_bounds__(BLK_THREADS) blink_attn_block_kernel(const __g
   __shared__ int s_warp[BLK_THREADS / 32], s_unit[5];   // of the unit: request; its first row, rows and first position; rows (of a head) before it
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rep = a.pool.rep;
   ops_begin();
+  if (a.few == 0 && blockIdx.x == 0 && tid == 0) *reinterpret_cast<int*>(a.ws) = 0;   // (else the kernels behind this one do)
   // the unit: the CTA's place in the sequence of all of them, found by the thread whose run of requests holds it
   const int h = (int)blockIdx.x % a.pool.Hkv, place = (int)blockIdx.x / a.pool.Hkv;
   const int each = (a.n + BLK_THREADS - 1) / BLK_THREADS, r0 = min(a.n, tid * each), r1 = min(a.n, r0 + each);
