@@ -461,7 +461,7 @@ uint64_t blink_verify_workspace(int rows, int n_requests, int vocab);
  * above 0, or not finite: greedy, a draft is accepted when it is the row's largest (the first of equals), which is also the token drawn; a row
  * whose largest entry is infinite, or that holds no number, is taken so too (token 0 in the latter).  A logit of NaN counts as -inf; a
  * token outside the vocabulary is refused.
- *   out_tokens [rows]          the accepted drafts, the token drawn, then -1
+ *   out_tokens [rows]          the accepted drafts, the token drawn, then -1; may be draft_tokens
  *   n_accepted [n_requests]    0 .. k (a request without rows: 0)
  * Acceptance compares in 64 bits (the sum of exponentials to about 1e-8, 1e-6 at worst), the draw is in 64 bits throughout.  fp32 [rows][vocab] logits
  * and probabilities with their strides; draft_probs is not read in a request's last row. */

@@ -4,13 +4,13 @@
 //   first refused i: a token from max(0, p_i - q_i), none refused: from p of the last row; by the inverse of its running sum in the order of
 //   the indexes: the first j with sum_{<= j} > v * sum
 //
-// Three kernels, each waiting for the one before it only where it needs its results.
+// Three kernels (or two), each waiting for the one before it only where it needs its results.
 //   rows    largest value and sum of exponentials of pieces of 1024 entries of every row, a warp each: one pass over the logits, which is what
 //           bounds the whole (HBM: 4 bytes an entry).  A lane has its 32 entries on their way at once and sums against its own largest
 //           value, so that nothing waits for another warp.  Exponentials in 32 bits, sums of a lane's entries in 32, everything above in
 //           64: the acceptance test is off by some 1e-8 where the entries differ, and by 1e-6 at worst (most of the weight on entries that are
 //           all alike, 12 below the largest: an argument's rounding of 2^-24 of itself, and the exponential's own 2^-22).
-//   choose  a CTA per request: the first refused draft, from the pieces
+//   choose  a CTA per request: the first refused draft, from the pieces (with few requests every CTA of the draw does so for itself)
 //   draw    a cluster of 16 CTAs per request: the exponentials of that row, which stay in registers (up to 16 a thread), their sum, then the weights
 //           max(0, p - q), their sum, and the entry at which the running sum passes its target.  Sums go from CTA to CTA through
 //           distributed shared memory.
@@ -28,6 +28,7 @@ namespace blink {
 constexpr int VER_WARPS = 8, VER_THREADS = VER_WARPS * 32;
 constexpr int VER_EACH = 32, VER_CHUNK = 32 * VER_EACH;   // rows: entries of a lane, a warp
 constexpr int PICK_THREADS = 512, PICK_WARPS = 16, PICK_CTAS = 16;   // draw
+constexpr int PICK_CHOOSE = 12;   // requests up to which each draw chooses for itself
 
 struct VerChunk {
   double sum;   // of exp((z - max) / T)
@@ -205,18 +206,20 @@ __device__ __forceinline__ int2 ver_rows(const VerifyArgs& a, int req) {
   return make_int2(start, min(max(a.row_start[req + 1], start), a.rows));
 }
 
-__global__ void __launch_bounds__(VER_THREADS) blink_verify_choose_kernel(const VerifyArgs a) {
-  __shared__ int s_first;
-  __shared__ double s_table[16];
+// What is chosen for a request: its rows, the accepted drafts, what the draw needs, and the token of a row that stands for its largest entry alone.
+struct VerPicked {
+  int start, k, accepted, index;   // k: drafts, -1 for a request without rows; index: -1 where a token is drawn
+  VerChoice choice;
+};
+// By a CTA of WARPS warps, which all get it; s_table is there.  Waits for the first kernel.
+template <int WARPS>
+__device__ __forceinline__ VerPicked ver_choose(const VerifyArgs& a, int req, const double* s_table, VerPicked* s_out) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int req = (int)blockIdx.x;
-  ops_next();
   // (all but the pieces is there before the first kernel is done)
   const int2 rows = ver_rows(a, req);
   const int start = rows.x, k = rows.y - rows.x - 1;
   const float T = a.temperature[req];
-  if (tid == 0) s_first = max(k, 0);
-  ver_table(s_table, a);
+  if (tid == 0) s_out->accepted = max(k, 0);
   __syncthreads();
   // A row from its pieces: largest value, its index, sum.
   auto row_of = [&](int row, float& m, int& idx, double& sum, bool with_sum) {
@@ -243,7 +246,7 @@ __global__ void __launch_bounds__(VER_THREADS) blink_verify_choose_kernel(const 
     return one;
   };
   bool waited = false;
-  for (int i = warp; i < k; i += VER_WARPS) {
+  for (int i = warp; i < k; i += WARPS) {
     float m;
     int idx;
     double sum;
@@ -255,31 +258,42 @@ __global__ void __launch_bounds__(VER_THREADS) blink_verify_choose_kernel(const 
     waited = true;
     const bool one = row_of(row, m, idx, sum, true);
     const bool ok = one ? x == idx : in && (double)u * (double)q * sum < ver_exp(ver_exp_of(s_table, m, T), z);
-    if (lane == 0 && !ok) atomicMin(&s_first, i);
+    if (lane == 0 && !ok) atomicMin(&s_out->accepted, i);
   }
   if (!waited) ops_wait();
   __syncthreads();
-  const int acc = s_first, row = start + acc;
-  if (k < 0) {   // a request without rows
-    if (tid == 0) {
-      a.accepted[req] = 0;
-      a.choice[req].row = -1;
-    }
-    return;
-  }
   if (warp == 0) {
-    float top;
-    int index;
+    const int acc = s_out->accepted, row = start + acc;
+    float top = 0.f;
+    int index = -1;
     double unused;
-    const bool one = row_of(row, top, index, unused, false);
+    const bool one = k < 0 || row_of(row, top, index, unused, false);
     if (lane == 0) {
-      a.accepted[req] = acc;
-      a.choice[req] = VerChoice{one ? -1 : row, acc < k, top, 0};
-      if (one) a.tokens[row] = index;
+      s_out->start = start;
+      s_out->k = k;
+      s_out->index = one ? index : -1;
+      s_out->choice = VerChoice{one ? -1 : row, acc < k, top, 0};
     }
   }
-  for (int i = tid; i <= k; i += VER_THREADS)
-    if (i != acc) a.tokens[start + i] = i < acc ? a.draft[start + i] : -1;
+  __syncthreads();
+  return *s_out;
+}
+// The outputs that stand fixed then, by a CTA.
+__device__ __forceinline__ void ver_write(const VerifyArgs& a, int req, const VerPicked& p) {
+  if (threadIdx.x == 0) a.accepted[req] = p.accepted;
+  for (int i = threadIdx.x; i <= p.k; i += blockDim.x)
+    if (i != p.accepted || p.index >= 0) a.tokens[p.start + i] = i < p.accepted ? a.draft[p.start + i] : i == p.accepted ? p.index : -1;
+}
+
+__global__ void __launch_bounds__(VER_THREADS) blink_verify_choose_kernel(const VerifyArgs a) {
+  __shared__ VerPicked s_out;
+  __shared__ double s_table[16];
+  const int req = (int)blockIdx.x;
+  ops_next();
+  ver_table(s_table, a);
+  const VerPicked p = ver_choose<VER_WARPS>(a, req, s_table, &s_out);
+  if (threadIdx.x == 0) a.choice[req] = p.choice;
+  ver_write(a, req, p);
 }
 
 // The first of 16 parts (a lane each, lanes 16 .. 31 have 0) whose running sum exceeds target, else the last with anything in it; `base` grows by
@@ -299,8 +313,10 @@ __device__ __forceinline__ int ver_part(double part, double target, double& base
   return at;
 }
 
-// EACH: entries of a lane at a time.
-template <int EACH>
+// EACH: entries of a lane at a time.  CHOOSE: every CTA chooses for itself, and the kernel before this one is left out.  With as many requests
+// as there is room for clusters at a time that is a launch less, with more each wave of them would choose first.  (Five rows of 32000 a request, us, with
+// the kernel before it | without: 1 request 9.5 | 9.0, 8 11.6 | 10.4, 12 13.1 | 12.0, 16 15.7 | 17.6, 64 34 | 43.)
+template <int EACH, bool CHOOSE>
 __global__ void __launch_bounds__(PICK_THREADS, 2) blink_verify_draw_kernel(const VerifyArgs a) {
   namespace cg = cooperative_groups;
   constexpr int TILE = 32 * EACH;
@@ -314,13 +330,29 @@ __global__ void __launch_bounds__(PICK_THREADS, 2) blink_verify_draw_kernel(cons
   const int V = a.vocab;
   const float T = a.temperature[req], u = a.u_pick[req];
   ver_table(s_table, a);
-  __syncthreads();
-  ops_wait();
-  ops_next();
-  const VerChoice choice = a.choice[req];
+  __shared__ VerPicked s_out;
+  VerPicked picked;
+  VerChoice choice;
+  if constexpr (CHOOSE) {
+    ops_next();
+    picked = ver_choose<PICK_WARPS>(a, req, s_table, &s_out);
+    choice = picked.choice;
+  } else {
+    __syncthreads();
+    ops_wait();
+    ops_next();
+    choice = a.choice[req];
+  }
   const int row = choice.row;
-  if (row < 0) return;   // (the whole cluster)
+  if (!CHOOSE && row < 0) return;   // (the whole cluster)
   cg::cluster_group::arrival_token there = cluster.barrier_arrive();   // all CTAs have to be there before they are written to
+  if constexpr (CHOOSE) {
+    if (row < 0) {
+      cluster.barrier_wait(std::move(there));
+      if (rank == 0) ver_write(a, req, picked);
+      return;
+    }
+  }
   // the row's entries: a run of tiles per warp, in the order of CTAs, warps and tiles
   const int tiles = (V + PICK_CTAS * PICK_WARPS * TILE - 1) / (PICK_CTAS * PICK_WARPS * TILE);
   const int w0 = (rank * PICK_WARPS + warp) * tiles * TILE;
@@ -387,6 +419,8 @@ __global__ void __launch_bounds__(PICK_THREADS, 2) blink_verify_draw_kernel(cons
     s += lane_sum();
   }
   cluster.barrier_wait(std::move(there));
+  if constexpr (CHOOSE)
+    if (rank == 0) ver_write(a, req, picked);   // (all CTAs have read the drafts, which may lie there)
   const double inv_S = 1.0 / sum_all(s, 0);
 
   // what is drawn from: p - q where a draft was refused (what is no number or negative in q counts as 0), p otherwise
@@ -488,6 +522,11 @@ __global__ void __launch_bounds__(PICK_THREADS, 2) blink_verify_draw_kernel(cons
   if (lane == 0) a.tokens[row] = token >= 0 ? token : last;
 }
 
+template <int EACH, bool CHOOSE>
+static int verify_draw(const VerifyArgs& a, void* stream) {
+  return ops_launch(blink_verify_draw_kernel<EACH, CHOOSE>, (int64_t)a.n * PICK_CTAS, PICK_THREADS, 0, stream, PICK_CTAS, a);
+}
+
 struct VerifySpace {
   uint64_t choice, end;   // behind the pieces
   int64_t n_chunks;
@@ -546,13 +585,13 @@ int blink_verify_drafts(const float* logits, int64_t logits_stride, int rows, in
   a.vec = logits_stride % 4 == 0 && ops_aligned(logits, 16);
   a.probs_vec = draft_probs && probs_stride % 4 == 0 && ops_aligned(draft_probs, 16);
   int rc = ops_launch(blink_verify_rows_kernel, (int64_t)rows * a.groups, VER_THREADS, 0, stream, 0, a);
-  if (rc == BLINK_OK) rc = ops_launch(blink_verify_choose_kernel, n_requests, VER_THREADS, 0, stream, 0, a);
+  const bool choose = n_requests > PICK_CHOOSE;
+  if (rc == BLINK_OK && choose) rc = ops_launch(blink_verify_choose_kernel, n_requests, VER_THREADS, 0, stream, 0, a);
   if (rc != BLINK_OK) return rc;
   // as few entries of a lane as hold the row in one go: 32768 entries in 16 CTAs of 16 warps with four, 131072 with 16 (beyond that, runs of tiles)
-  const int64_t ctas = (int64_t)n_requests * PICK_CTAS;
-  if (vocab <= 32768) return ops_launch(blink_verify_draw_kernel<4>, ctas, PICK_THREADS, 0, stream, PICK_CTAS, a);
-  if (vocab <= 65536) return ops_launch(blink_verify_draw_kernel<8>, ctas, PICK_THREADS, 0, stream, PICK_CTAS, a);
-  return ops_launch(blink_verify_draw_kernel<16>, ctas, PICK_THREADS, 0, stream, PICK_CTAS, a);
+  if (vocab <= 32768) return choose ? verify_draw<4, false>(a, stream) : verify_draw<4, true>(a, stream);
+  if (vocab <= 65536) return choose ? verify_draw<8, false>(a, stream) : verify_draw<8, true>(a, stream);
+  return choose ? verify_draw<16, false>(a, stream) : verify_draw<16, true>(a, stream);
 }
 
 }  // extern "C"

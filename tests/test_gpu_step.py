@@ -498,6 +498,25 @@ def test_verify_the_same_call_gives_the_same_tokens():
         assert all(torch.equal(x, y) for x, y in zip(first, run_verify(c)))
 
 
+@pytest.mark.parametrize("V,probs", [(700, False), (40000, True), (70000, True), (150000, False)])
+def test_verify_in_one_call_or_several_and_over_the_drafts(V, probs):
+    rng = np.random.default_rng(V)
+    k = [3, 0, 5, 1] * 7
+    c = verify_case(rng, k, V, probs, [1.0, 0.0, 0.8, 1.1] * 7, spread=1.0)
+    tokens, accepted = run_verify(c)
+    check_verify(c, tokens, accepted)
+    for a, b in ((0, 4), (4, 16), (16, 28)):
+        s = slice(c["start"][a], c["start"][b])
+        part = dict(c, z=c["z"][s], start=c["start"][a:b + 1] - c["start"][a], draft=c["draft"][s], q=c["q"][s] if probs else None, T=c["T"][a:b], ua=c["ua"][s], up=c["up"][a:b])
+        some, n = run_verify(part)
+        assert torch.equal(some, tokens[s]) and torch.equal(n, accepted[a:b])
+        z = torch.from_numpy(part["z"]).cuda()
+        f = lambda x: torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32)).cuda()
+        drafts = ints(part["draft"])
+        B.blink_verify_drafts(z, ints(part["start"]), drafts, f(part["q"]) if probs else None, f(part["T"]), f(part["ua"]), f(part["up"]), out_tokens=drafts)
+        assert torch.equal(drafts, some)
+
+
 def test_verify_special_entries():
     rng = np.random.default_rng(3)
     V, n = 300, 12
