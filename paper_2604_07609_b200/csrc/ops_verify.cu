@@ -53,6 +53,7 @@ struct VerifyArgs {
   int n, rows, vocab, chunks, groups;
   bool vec, probs_vec;   // rows on 16-byte boundaries
   double sixteenths[16]; // 2^(i / 16)
+  double series[5];      // (ln 2 / 16)^i / i!, i = 1 .. 5 (as operands from the constant bank: written out they take two moves each at every use)
 };
 
 // No number: as if the entry were not there.
@@ -87,11 +88,19 @@ __device__ __forceinline__ void ver_larger(float& m, int& i, float m2, int i2) {
 template <int EACH>
 __device__ __forceinline__ void ver_load(float (&v)[EACH], const float* z, int n, bool vec, float behind) {
   const int lane = threadIdx.x & 31;
+  if (vec && n >= 32 * EACH) {   // (no question at every piece)
+#pragma unroll
+    for (int k = 0; k < EACH / 4; ++k) {
+      const float4 x = __ldcg(reinterpret_cast<const float4*>(z + k * 128 + lane * 4));   // (the chosen row is read again, from L2)
+      v[4 * k] = x.x; v[4 * k + 1] = x.y; v[4 * k + 2] = x.z; v[4 * k + 3] = x.w;
+    }
+    return;
+  }
 #pragma unroll
   for (int k = 0; k < EACH / 4; ++k) {
     const int at = k * 128 + lane * 4;
     if (vec && at + 4 <= n) {
-      const float4 x = __ldcg(reinterpret_cast<const float4*>(z + at));   // (the chosen row is read again, from L2)
+      const float4 x = __ldcg(reinterpret_cast<const float4*>(z + at));
       v[4 * k] = x.x; v[4 * k + 1] = x.y; v[4 * k + 2] = x.z; v[4 * k + 3] = x.w;
     } else {
 #pragma unroll
@@ -104,7 +113,7 @@ __device__ __forceinline__ void ver_load(float (&v)[EACH], const float* z, int n
 // holds no number.
 __device__ __forceinline__ bool ver_one(float T, float m) { return !(T > 0.f && T < INFINITY) || !(m > -INFINITY) || !(m < INFINITY); }
 
-__global__ void __launch_bounds__(VER_THREADS) blink_verify_rows_kernel(const VerifyArgs a) {
+__global__ void __launch_bounds__(VER_THREADS) blink_verify_rows_kernel(const __grid_constant__ VerifyArgs a) {
   __shared__ int s_req;
   __shared__ float s_T;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -176,12 +185,14 @@ __global__ void __launch_bounds__(VER_THREADS) blink_verify_rows_kernel(const Ve
 // (ln 2 / 32)^6 / 6! = 1.4e-13).  64-bit operations are what the kernels below are bound by: twelve here, one of them the conversion.
 struct VerExp {
   const double* table;   // 2^(i / 16)
+  const double* series;
   double scale, shift;   // 16 log2(e) / T, and -top times that
   float top, below;      // entries below this are 0: (z - top) / T < -700
 };
-__device__ __forceinline__ VerExp ver_exp_of(const double* table, float top, float T) {
+__device__ __forceinline__ VerExp ver_exp_of(const VerifyArgs& a, const double* table, float top, float T) {
   VerExp x;
   x.table = table;
+  x.series = a.series;
   x.scale = 16.0 * 1.44269504088896340736 / (double)T;
   x.shift = -(double)top * x.scale;
   x.top = top;
@@ -189,11 +200,10 @@ __device__ __forceinline__ VerExp ver_exp_of(const double* table, float top, flo
   return x;
 }
 __device__ __forceinline__ double ver_exp(const VerExp& x, float z) {
-  constexpr double L = 0.693147180559945309417 / 16, C2 = L * L / 2, C3 = C2 * L / 3, C4 = C3 * L / 4, C5 = C4 * L / 5;
   constexpr double SHIFT = 6755399441055744.0;   // 1.5 * 2^52: adding it leaves the nearest whole number in the low bits
   const double t = fma((double)z, x.scale, x.shift), s = t + SHIFT, f = t - (s - SHIFT);
   const int n = __double2loint(s);
-  const double p = fma(f, fma(f, fma(f, fma(f, fma(f, C5, C4), C3), C2), L), 1.0) * x.table[n & 15];
+  const double p = fma(f, fma(f, fma(f, fma(f, fma(f, x.series[4], x.series[3]), x.series[2]), x.series[1]), x.series[0]), 1.0) * x.table[n & 15];
   return z >= x.below ? __hiloint2double(__double2hiint(p) + ((n >> 4) << 20), __double2loint(p)) : 0.0;   // (no number: 0 too)
 }
 __device__ __forceinline__ void ver_table(double* table, const VerifyArgs& a) {   // before a barrier
@@ -237,7 +247,7 @@ __device__ __forceinline__ VerPicked ver_choose(const VerifyArgs& a, int req, co
     const bool one = ver_one(T, m);
     sum = 0.0;
     if (!one && with_sum) {
-      const VerExp x = ver_exp_of(s_table, m, T);
+      const VerExp x = ver_exp_of(a, s_table, m, T);
 #pragma unroll 4
       for (int j = lane; j < a.chunks; j += 32) sum += c[j].sum * ver_exp(x, c[j].max);
 #pragma unroll
@@ -257,7 +267,7 @@ __device__ __forceinline__ VerPicked ver_choose(const VerifyArgs& a, int req, co
     if (!waited) ops_wait();
     waited = true;
     const bool one = row_of(row, m, idx, sum, true);
-    const bool ok = one ? x == idx : in && (double)u * (double)q * sum < ver_exp(ver_exp_of(s_table, m, T), z);
+    const bool ok = one ? x == idx : in && (double)u * (double)q * sum < ver_exp(ver_exp_of(a, s_table, m, T), z);
     if (lane == 0 && !ok) atomicMin(&s_out->accepted, i);
   }
   if (!waited) ops_wait();
@@ -285,7 +295,7 @@ __device__ __forceinline__ void ver_write(const VerifyArgs& a, int req, const Ve
     if (i != p.accepted || p.index >= 0) a.tokens[p.start + i] = i < p.accepted ? a.draft[p.start + i] : i == p.accepted ? p.index : -1;
 }
 
-__global__ void __launch_bounds__(VER_THREADS) blink_verify_choose_kernel(const VerifyArgs a) {
+__global__ void __launch_bounds__(VER_THREADS) blink_verify_choose_kernel(const __grid_constant__ VerifyArgs a) {
   __shared__ VerPicked s_out;
   __shared__ double s_table[16];
   const int req = (int)blockIdx.x;
@@ -317,7 +327,7 @@ __device__ __forceinline__ int ver_part(double part, double target, double& base
 // as there is room for clusters at a time that is a launch less, with more each wave of them would choose first.  (Five rows of 32000 a request, us, with
 // the kernel before it | without: 1 request 9.5 | 9.0, 8 11.6 | 10.4, 12 13.1 | 12.0, 16 15.7 | 17.6, 64 34 | 43.)
 template <int EACH, bool CHOOSE>
-__global__ void __launch_bounds__(PICK_THREADS, 2) blink_verify_draw_kernel(const VerifyArgs a) {
+__global__ void __launch_bounds__(PICK_THREADS, 2) blink_verify_draw_kernel(const __grid_constant__ VerifyArgs a) {
   namespace cg = cooperative_groups;
   constexpr int TILE = 32 * EACH;
   cg::cluster_group cluster = cg::this_cluster();
@@ -360,23 +370,24 @@ __global__ void __launch_bounds__(PICK_THREADS, 2) blink_verify_draw_kernel(cons
   const float* q = choice.refused && a.probs ? a.probs + row * a.probs_stride : nullptr;
   float zv[EACH];   // of the warp's first tile
   ver_load(zv, z + w0, V - w0, a.vec, -INFINITY);
-  auto fetch_q = [&](int at) {
+  auto fetch_q = [&](int at) {   // behind the end: zeros
+    const bool whole = a.probs_vec && at + TILE <= V;
 #pragma unroll
     for (int g = 0; g < EACH / 4; ++g) {
       const int o = g * 128 + lane * 4;
       const uint32_t dst = (uint32_t)__cvta_generic_to_shared(&s_q[warp][o]);
-      if (a.probs_vec && at + o + 4 <= V) {
+      if (whole) {
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(q + at + o) : "memory");
       } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (at + o + j < V) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + 4 * j), "l"(q + at + o + j) : "memory");
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst + 4 * j), "l"(q + (at + o + j < V ? at + o + j : 0)), "r"(at + o + j < V ? 4u : 0u) : "memory");
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
   if (q) fetch_q(w0);
-  const VerExp exp = ver_exp_of(s_table, choice.max, T);
+  const VerExp exp = ver_exp_of(a, s_table, choice.max, T);
   double e[EACH];
   auto exps = [&]() {
 #pragma unroll
@@ -426,7 +437,6 @@ __global__ void __launch_bounds__(PICK_THREADS, 2) blink_verify_draw_kernel(cons
   // what is drawn from: p - q where a draft was refused (what is no number or negative in q counts as 0), p otherwise
   int x = choice.refused && !a.probs ? a.draft[row] : -1;
   auto rests = [&](int t) {   // of tile t, whose exponentials are in e
-    const int at = w0 + t * TILE + lane * 4;
     if (q) {
       asm volatile("cp.async.wait_group 0;" ::: "memory");
 #pragma unroll
@@ -435,11 +445,12 @@ __global__ void __launch_bounds__(PICK_THREADS, 2) blink_verify_draw_kernel(cons
         const float w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const double p = e[i + j] * inv_S;
-          e[i + j] = w[j] > 0.f && at + i * 32 + j < V ? fmax(p - (double)w[j], 0.0) : p;   // (behind the end: nothing was fetched, and p is 0)
+          const double r = fma(e[i + j], inv_S, -(double)fmaxf(w[j], 0.f));   // (the larger of 0 and no number is 0)
+          e[i + j] = __double2hiint(r) < 0 ? 0.0 : r;
         }
       }
     } else {
+      const int at = w0 + t * TILE + lane * 4;
 #pragma unroll
       for (int i = 0; i < EACH; ++i) {
         const double p = e[i] * inv_S;
@@ -582,6 +593,9 @@ int blink_verify_drafts(const float* logits, int64_t logits_stride, int rows, in
   a.chunks = (int)space.n_chunks;
   a.groups = (int)((space.n_chunks + VER_WARPS - 1) / VER_WARPS);
   for (int i = 0; i < 16; ++i) a.sixteenths[i] = std::exp2(i / 16.0);
+  const double l = std::log(2.0) / 16;
+  double term = 1.0;
+  for (int i = 0; i < 5; ++i) a.series[i] = term = term * l / (i + 1);
   a.vec = logits_stride % 4 == 0 && ops_aligned(logits, 16);
   a.probs_vec = draft_probs && probs_stride % 4 == 0 && ops_aligned(draft_probs, 16);
   int rc = ops_launch(blink_verify_rows_kernel, (int64_t)rows * a.groups, VER_THREADS, 0, stream, 0, a);
