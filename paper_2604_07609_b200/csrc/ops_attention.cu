@@ -3,7 +3,13 @@
 //   row at position p sees key j <= p when j > p - window (window 0: every j) or j < sinks
 //   o = sum_j softmax_j(q . k_j / sqrt(hd)) v_j,  zeros where nothing is seen
 //
-// attn_few: requests of few rows (a token, a few drafts).  What bounds it: HBM, every visible key and value once.
+// Four ways: the two kernels here (attn_few with its join, attn_near), tiles on the tensor cores (ops_attn_tiles.cu) and 32-bit blocks
+// (ops_attn_block.cu); which requests and calls take which stands at the entry point, with both sides measured.
+//
+// attn_few: requests of few rows (a token, a few drafts).  What bounds it: HBM, every visible key and value once.  (8B shape, a row each: 64 requests
+// behind 5000 keys 195 us, 6.7 TB/s; 256 752 us, 7.0; one behind 120000 keys 87 us, 5.7.)  With more rows, instructions: 48 requests of 4 rows behind
+// 2500 keys 92 us, 5.3 TB/s, of 8 rows 131.  (Tiles copied ahead into shared memory, which leaves registers to more rows, cost time at every number of rows:
+// 5 rows 103 us, 127 so; it is not the loads that a warp waits for.)
 // A unit is a request, a kv head and up to MR (query row, head) rows, its tiles are the visible blocks of 16 keys.  All tiles of all units
 // stand in one sequence that is cut into equal runs, one per CTA, whatever the lengths; lengths are read on the device, so that a
 // captured graph serves growing contexts.  A CTA's warps take its tiles in turn, straight from memory to registers in the layout of the
@@ -31,7 +37,8 @@ constexpr int FEW_MAX_CTAS = 640;    // of a launch; the records are laid out fo
 constexpr int FEW_MIN_TILES = 4;     // of a CTA's run, while there are any
 constexpr int FEW_UNIT_TILES = 4;    // what a unit costs beside its tiles, in tiles
 constexpr int JOIN_THREADS = 256;
-constexpr int ALL_ROWS = 8, ALL_SHORT = 1024, ALL_KEYS = 8192, ALL_KEYS_32 = 256;   // calls that take all requests to the tiles: rows (of a kv head) of the longest; keys that a row sees, at most
+// Calls that take all requests to the tiles (see the entry point): rows (of a kv head) of the longest, keys that a row sees, at most.
+constexpr int ALL_ROWS = 8, ALL_SHORT = 1024, ALL_KEYS = 8192, ALL_KEYS_32 = 256;
 constexpr int NEAR_CTAS = 16, NEAR_KEYS = 4096;   // a cluster per unit: its CTAs, keys that a row sees at most
 
 // What the join needs of a unit that was cut, written by the CTA in whose run it begins.
@@ -365,7 +372,7 @@ __device__ __forceinline__ void few_store(float* p, float4 x) { *reinterpret_cas
 
 // Groups of MR rows of a request, and tiles of each (the same number for all of them, so that a place in the sequence is found by division;
 // a group that has fewer leaves the rest out).  A unit's start and end cost as much as some tiles and count as such, behind its
-// tiles: without them CTAs that got many short units were the last (200 rows of 20 to 5000 keys: 148 us, 92 with them).
+// tiles: without them CTAs that got many short units were the last (200 rows of 20 to 5000 keys, cold: 148 us, 105 with them).
 struct FewShape {
   int groups, tiles;
 };
@@ -516,7 +523,7 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) blink_attn_few_kernel(const
 }
 
 // The parts of the unit that begins, but does not end, in the run of CTA blockIdx.x.  A row's parts are shared out over warps, and these joined
-// in order.
+// in order: m = max m_i, l = sum l_i 2^(m_i - m), o = sum o_i 2^(m_i - m) / l.  Latency: 2 to 3 us behind a batch, 2.3 MB for 200 rows.
 template <typename T, int HD, int MR>
 __global__ void __launch_bounds__(JOIN_THREADS) blink_attn_join_kernel(const __grid_constant__ AttnArgs a) {
   constexpr int WARPS = JOIN_THREADS / 32, V = HD / 32;   // values of a row per lane
@@ -586,9 +593,9 @@ __global__ void __launch_bounds__(JOIN_THREADS) blink_attn_join_kernel(const __g
 }
 
 // The same for few units and short contexts, where latency is all there is: a cluster of CTAs per unit, which share its tiles and join their records
-// through distributed shared memory.  One kernel instead of two, no sequence to be added up first: a row of 1024 keys of the 8B shape
-// NEAR_US us, 12.3 with the kernels above.  a.few as there; `groups` clusters per (request, kv head), a group of rows each, or every
-// groups-th where there are more.
+// through distributed shared memory.  One kernel instead of two, no sequence to be added up first: a row of 1028 keys of the 8B shape
+// 8.0 us, 12.3 with the kernels above (some 3 us are the launch, the rest loads that wait for one another: lengths, block ids, keys).
+// a.few as there; `groups` clusters per (request, kv head), a group of rows each, or every groups-th where there are more.
 template <typename T, int HD, typename W>
 __global__ void __launch_bounds__(FEW_THREADS) blink_attn_near_kernel(const __grid_constant__ AttnArgs a, const int groups) {
   namespace cg = cooperative_groups;

@@ -1,4 +1,4 @@
-// blink_window_attention in 32 bits for requests of more than a few rows, on the CUDA cores.
+// blink_window_attention in 32 bits for requests of more than a few rows, on the CUDA cores: there is no matrix instruction of that precision.
 //
 // A unit is a request, a kv head and 32 or 16 (query row, head) rows, a CTA each.  Keys come in tiles of 64, the visible blocks of the unit, sinks first,
 // four to a tile; keys and values through shared memory by asynchronous copies, the next keys on their way while the output is formed
@@ -6,8 +6,8 @@
 // shared memory for 64 multiply-adds a warp, which then take as long.  The 16 threads of a row are half a warp, so maxima and sums are shuffles.
 //
 // What bounds it: multiply-adds, and in small calls the cold instructions: the loops are not unrolled further than that.  (As units of 8 rows
-// in registers, with everything unrolled, the small configuration's batch took 22.5 us, BLOCK_US us here; a prompt of 1000 rows of the 8B shape
-// 1024 us, BLOCK_LONG here.)
+// in registers, with everything unrolled, the small configuration's batch took 22.5 us, 12.6 here; a prompt of 1000 rows of the 8B shape
+// 1024 us, 336 here: 25 of 74 TFLOP/s that the multiply-adds could do.)
 #include <cmath>
 
 #include "ops_attention.cuh"

@@ -1,4 +1,7 @@
-// blink_window_attention for requests of many rows (prompts and their chunks), on tcgen05.
+// blink_window_attention for requests of many rows (prompts and their chunks), and for batches that are sent here whole (drafts; the rule is beside the
+// entry point), on tcgen05.
+//
+//   s = q k / sqrt(hd) * log2(e) of 128 rows and 128 keys;  p = 2^(s - m), l += sum p,  o += p v;  m follows the largest s;  output o / l
 //
 // A unit is a request, a kv head and 2 * 128 (query row, head) rows: two streams of 128, the rep heads of the kv head beside one another, so that a
 // narrow window wastes little (4 heads: 64 query rows read the keys of their window once).  Keys come in tiles of 128: the visible
@@ -8,17 +11,24 @@
 //                     over the same scores
 //   warps 16 | 17     issue the MMAs of stream 0 | 1: scores = Q K^T (operands in shared memory), output += P V (P in TMEM, V as it lies in the
 //                     cache)
-//   warps 18 | 19     copies of the keys | of the values, eight a tile (with 24, four of a KB or two a block, these warps were the slowest: 4096
-//                     rows 170 us).  Warp 18 also hands out the units, heaviest of a request first, from a counter
+//   warps 18 | 19     copies of the keys | of the values, eight a tile (with twice as many smaller ones for the keys that warp was the slowest of
+//                     all: 4096 rows 170 us, 145 so).  Warp 18 also hands out the units, heaviest of a request first, from a counter
 //
 // While one stream is in its softmax the tensor core works for the other; the next scores of a stream are issued behind its output MMAs, so a
 // stream's scores being complete also says that its accumulator is.  The maximum in use, the same for both threads of a row, follows the
 // largest score only when that has grown by more than 2^8 (the sum takes up smaller growth); then the scores, still in TMEM, are gone over once
 // more and the accumulator is rescaled.  CTAs are persistent; keys of the next unit are on their way while the last tile of one is worked on.
 //
-// What bounds it: the chain of a stream, softmax -> output -> next scores, of which two overlap.  With one thread per row (eight warps) the
-// softmax alone took 1900 cycles a tile, at four cycles an instruction with one warp of a stream on a scheduler.  Exponentials on the
-// multiply-adds (a quarter to a half of them, degree 3) made it longer, not shorter: they are not what it waits for.
+// A unit with rows for one stream only is worked on by both, stream 0 the even tiles and stream 1 the odd ones, and joined in the epilogue:
+// stream 0 reads both accumulators, once stream 1 has said that its own is there, with its rows' maxima and sums (48 requests of 12
+// rows behind 2500 keys, 8B shape: 131 us with one stream, 98 so).
+//
+// What bounds it.  Prompts: the chain of a stream, softmax -> output -> next scores, of which two overlap: 8192 rows of the 8B shape 507 us, 1085
+// TFLOP/s of the pairs that are seen, the tensor pipe busy half of the time.  With one thread per row (eight warps) the softmax alone took 1900 cycles a
+// tile, at four cycles an instruction with one warp of a stream on a scheduler.  Exponentials on the multiply-adds (a quarter to a half of
+// them, degree 3) made it longer, not shorter: they are not what it waits for.  Few rows: HBM (48 requests of 1 to 6 rows behind 300 to
+// 5000 keys 68 us, 4.8 TB/s, cold), and that units are whole.  Narrow windows: what a unit costs beside its tiles, some 4000 cycles (4096 rows with a
+// window of 128 40 us).
 #include <cuda.h>
 
 #include <cmath>

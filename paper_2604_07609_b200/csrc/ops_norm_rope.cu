@@ -5,7 +5,8 @@
 //   (y_i, y_{i+hd/2}) turned by position * theta^(-2 i / hd)
 //   q -> q_out, k -> the pool's key of the row's slot; v -> its value as it is
 //
-// What bounds it: HBM, every element in once and out once.  A lane takes 8 elements of either half of a head, so that the two
+// What bounds it: HBM, every element in once and out once (8B shape: 16000 rows in 16 bits 70 us, 5.6 TB/s; 4099 rows of 32 bits, cold, 31 us, 4.9
+// TB/s); 64 rows 6 us, latency.  A lane takes 8 elements of either half of a head, so that the two
 // partners of a rotation meet in one thread, loads and stores are 16 bytes, and a head is 8 lanes (head_dim 128; 4 at 64): its sum of
 // squares takes three shuffles.  A warp turns U groups of heads of one row; their loads are all on their way before the angles,
 // which the warp's lanes share out (two each at most) and pass on through shared memory.  Angles in 64 bits, reduced there to less than
