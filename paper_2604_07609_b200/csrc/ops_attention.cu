@@ -38,7 +38,7 @@ constexpr int FEW_MIN_TILES = 4;     // of a CTA's run, while there are any
 constexpr int FEW_UNIT_TILES = 4;    // what a unit costs beside its tiles, in tiles
 constexpr int JOIN_THREADS = 256;
 // Calls that take all requests to the tiles (see the entry point): rows (of a kv head) of the longest, keys that a row sees, at most.
-constexpr int ALL_ROWS = 8, ALL_SHORT = 1024, ALL_KEYS = 8192, ALL_KEYS_32 = 256;
+constexpr int ALL_ROWS = 8, ALL_SHORT = 1536, ALL_KEYS = 8192, ALL_KEYS_32 = 256;
 constexpr int NEAR_CTAS = 16, NEAR_KEYS = 4096;   // a cluster per unit: its CTAs, keys that a row sees at most
 
 // What the join needs of a unit that was cut, written by the CTA in whose run it begins.
@@ -768,13 +768,16 @@ int blink_window_attention(const blink_model_cfg* model, const blink_kv_pool* kv
   const bool bf16 = model->dtype == BLINK_DTYPE_BF16;
   const bool tiles = (int64_t)max_new * a.pool.rep > (bf16 ? 32 : 8);   // there may be requests of more than a few rows
   if (tiles) a.few = (bf16 ? 8 * nt : 8) / a.pool.rep;
-  const int64_t keys = std::min<int64_t>((int64_t)table_stride * OPS_BLOCK, window > 0 ? (int64_t)window + sinks + max_new : INT64_MAX);
+  // keys that a request of few rows, or the rows of a unit of the tiles, see at most
+  const int64_t keys = std::min<int64_t>((int64_t)table_stride * OPS_BLOCK, window > 0 ? (int64_t)window + sinks + std::min(max_new, 256) : INT64_MAX);
   // Everything to the tiles, which share nothing out over CTAs, where there are units enough and none can be very long: a tile's rows cost the same
   // however few they are, but its copies run by themselves.  (8B shape, us, with the kernels for few rows | without: 48 requests of 1 to 6 rows behind
   // 300 to 5000 keys 116 | 86, of 1 to 3 91 | 86; 28 of them 77 | 60, 19 55 | 55, 10 34 | 46; 40 of 1 to 300 rows with a window of 256 51 | 41.  20 of 5
-  // rows behind 10000 keys 151 | 205.  10 of 1 to 6 rows behind 200 to 900 keys 23 | 17.  Eight rows of a head or less, one instruction of those
-  // kernels: 64 rows behind 5000 keys 197 us, 6.7 TB/s, which the tiles do not reach.)
-  const int64_t least = keys <= ALL_SHORT ? sms / 2 : sms + sms / 2;
+  // rows behind 10000 keys 151 | 205.  Evenly long ones end later where they do not fill the CTAs: 48 of 4 rows behind 2500 keys 92 | 95.  Eight rows of a
+  // head or less, one instruction of those kernels: 64 rows behind 5000 keys 197 us, 6.7 TB/s, which the tiles do not reach.)  Where no row sees more
+  // than some 1500 keys fewer units will do, and none have to be there when the tiles are called anyway: 10 of 1 to 6 rows behind 200 to 900
+  // keys 23 | 17; with a window of 1024 8 rows beside a prompt of 64 27 | 19, beside two of 1000 50 | 43, whole prompts of three requests 177 | 174.
+  const int64_t least = keys > ALL_SHORT ? sms + sms / 2 : tiles ? 0 : sms / 2;
   if (bf16 && (int64_t)max_new * a.pool.rep > ALL_ROWS && (int64_t)n_requests * a.pool.Hkv >= least && keys <= ALL_KEYS) {
     a.few = 0;
     return attn_tiles(a, sms, stream);
