@@ -299,6 +299,16 @@ def test_attention_few_rows_behind_many_keys(rep, hkv, hd, window, sinks):
     assert torch.equal(out, run_attention(c))
 
 
+@pytest.mark.parametrize("rep,hkv,hd", [(4, 1, 128), (4, 4, 128), (8, 2, 64), (1, 8, 128)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1600, 5)])
+def test_attention_single_rows_drafts_and_prompts_in_one_call(rep, hkv, hd, window, sinks):
+    """Long enough contexts that few rows and many have kernels of their own, which share a workspace."""
+    c = attention_case(shape(rep, hkv, hd), [2000, 100, 1700, 0, 5], [1, 70, 4, 33, 0], window, sinks, seed=rep)
+    out = run_attention(c)
+    check_attention(c, out)
+    assert all(torch.equal(out, run_attention(c)) for _ in range(3))
+
+
 @pytest.mark.parametrize("n,window,top", [(30, 0, 700), (12, 0, 400), (30, 200, 9000), (9, 3000, 5000)])
 def test_attention_batches_of_drafts(n, window, top):
     """Calls that go to the tiles whole, to the kernels for few rows, or to both, by requests, rows and keys."""
