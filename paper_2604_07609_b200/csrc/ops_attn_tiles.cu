@@ -58,8 +58,8 @@ struct TilShared {
   float2 other[128];         // maxima and sums of stream 1's rows then
   uint32_t tmem;
   int dead;
-  int warp_sum[TIL_WARPS];
-  int weight[TIL_SORTED], count[TIL_SORTED];   // of requests: tiles of their last unit; units (by place)
+  unsigned long long warp_sum[TIL_WARPS];
+  int weight[TIL_SORTED], rows[TIL_SORTED];    // of requests: blocks that their last unit sees; rows (by place)
   uint16_t order[TIL_SORTED];                  // request of a place
 };
 
@@ -323,18 +323,20 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
   // The sequence of units: requests of more keys first, so that no CTA is left with a long unit at the end (48 requests of 300 to 5000 keys: in their
 // own order 99 us, so 86); beyond TIL_SORTED requests units are many and their order matters less.  A run of requests (or places) per thread.
   const bool sorted = a.n <= TIL_SORTED;
-  auto units_of = [&](const AttnReq& q) { return q.rows > a.few ? (q.rows + 2 * P - 1) / (2 * P) * a.pool.Hkv : 0; };
+  // Rows of a unit: two streams' worth, or one's, which both share, where there are few: twice the CTAs at half the time.  (8B shape, us, two | one: 512
+  // rows behind 3500 keys 76 | 45, 40 behind 1000 28 | 19.  Between one and two units a CTA: 1024 rows 27 | 23, two of 512 behind 3500 80 | 81.  Between
+  // two and three: 1500 rows 35.6 | 37.3.)
+  int unit_shift = 8 - lr;   // (powers of two)
   {
     const int each = (a.n + TIL_THREADS - 1) / TIL_THREADS;
     const int r0 = min(a.n, (int)threadIdx.x * each), r1 = min(a.n, r0 + each);
-    int mine = 0;
     if (sorted) {
       const int r = threadIdx.x;
-      int weight = 0, count = 0;
+      int weight = 0, rows = 0;
       if (r < a.n) {
         const AttnReq q = attn_req(a, a.row_start[r], a.row_start[r + 1], a.kv_len[r]);
-        count = units_of(q);
-        if (count > 0) weight = attn_span(a, q.ctx + (q.rows - 1) / (2 * P) * (2 * P), q.ctx + q.rows - 1).n;
+        rows = q.rows > a.few ? q.rows : 0;
+        if (rows > 0) weight = attn_span(a, q.ctx + ((rows - 1) & -(2 * P)), q.ctx + rows - 1).n;
         sh.weight[r] = weight;
       }
       __syncthreads();
@@ -345,30 +347,42 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
           place += other > weight || (other == weight && k < r);
         }
         sh.order[place] = (uint16_t)r;
-        sh.count[place] = count;
+        sh.rows[place] = rows;
       }
       __syncthreads();
-      if (r < a.n) {
-        s_pre[r] = 0;
-        mine = sh.count[r];
-      }
-    } else {
-      for (int r = r0; r < r1; ++r) {
-        s_pre[r] = mine;
-        mine += units_of(attn_req(a, a.row_start[r], a.row_start[r + 1], a.kv_len[r]));
-      }
     }
-    int x = mine;
+    auto rows_of = [&](int r) {
+      if (sorted) return sh.rows[r];
+      const AttnReq q = attn_req(a, a.row_start[r], a.row_start[r + 1], a.kv_len[r]);
+      return q.rows > a.few ? q.rows : 0;
+    };
+    unsigned long long mine = 0;   // units: of two streams, and (above) of one
+    for (int r = r0; r < r1; ++r) {
+      const int rows = rows_of(r);
+      mine += (unsigned long long)(((rows + 2 * P - 1) >> (8 - lr)) * a.pool.Hkv) | (unsigned long long)(((rows + P - 1) >> (7 - lr)) * a.pool.Hkv) << 32;
+    }
+    unsigned long long x = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, x, d);
+      const unsigned long long y = __shfl_up_sync(0xffffffffu, x, d);
       if (lane >= d) x += y;
     }
     if (lane == 31) sh.warp_sum[w] = x;
     __syncthreads();
-    for (int i = 0; i < w; ++i) x += sh.warp_sum[i];
-    for (int r = r0; r < r1; ++r) s_pre[r] += x - mine;
-    if (threadIdx.x == TIL_THREADS - 1) s_pre[a.n] = x;
+    unsigned long long total = 0;
+    const int warps = sorted ? (a.n + 31) / 32 : TIL_WARPS;   // that have any
+    for (int i = 0; i < warps; ++i) {
+      if (i < w) x += sh.warp_sum[i];
+      total += sh.warp_sum[i];
+    }
+    const bool one = (total >> 32) <= 2u * gridDim.x;
+    if (one) unit_shift = 7 - lr;
+    int at = (int)((x - mine) >> (one ? 32 : 0));
+    for (int r = r0; r < r1; ++r) {
+      s_pre[r] = at;
+      at += ((rows_of(r) + (1 << unit_shift) - 1) >> unit_shift) * a.pool.Hkv;
+    }
+    if (threadIdx.x == 0) s_pre[a.n] = (int)(total >> (one ? 32 : 0));
   }
   til_fence_before();
   __syncthreads();
@@ -390,15 +404,15 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
     }
     const int r = sorted ? sh.order[lo] : lo;
     const AttnReq q = attn_req(a, a.row_start[r], a.row_start[r + 1], a.kv_len[r]);
-    const int blocks = (q.rows + 2 * P - 1) / (2 * P);
+    const int unit_rows = 1 << unit_shift, blocks = (q.rows + unit_rows - 1) >> unit_shift;
     const int i = u - s_pre[lo], b = max(0, blocks - 1 - i / a.pool.Hkv);   // later rows, which see more, first
     t.req = r;
     t.h = i % a.pool.Hkv;
-    t.row = q.start + b * 2 * P;
-    const int rows = min(2 * P, q.rows - b * 2 * P);
+    t.row = q.start + b * unit_rows;
+    const int rows = min(unit_rows, q.rows - b * unit_rows);
     t.live[0] = min(P, rows);
     t.live[1] = rows - t.live[0];
-    t.pos = q.ctx + b * 2 * P;
+    t.pos = q.ctx + b * unit_rows;
     t.last = t.pos + rows - 1;
     t.span = attn_span(a, t.pos, t.last);
 #pragma unroll
@@ -836,7 +850,7 @@ static int tiles_run(const AttnArgs& a, int sms, int64_t most_units, void* strea
 }
 
 int attn_tiles(const AttnArgs& a, int sms, void* stream) {
-  const int64_t most_units = ((int64_t)a.rows * a.pool.rep / 256 + a.n) * a.pool.Hkv;
+  const int64_t most_units = ((int64_t)a.rows * a.pool.rep / 128 + a.n) * a.pool.Hkv;   // of one stream each
   return a.pool.hd == 128 ? tiles_run<128>(a, sms, most_units, stream) : tiles_run<64>(a, sms, most_units, stream);
 }
 

@@ -324,6 +324,19 @@ def test_attention_batches_of_drafts(n, window, top):
         assert torch.equal(out, run_attention(c))
 
 
+@pytest.mark.parametrize("window,sinks", [(0, 0), (500, 20)])
+def test_attention_units_of_one_stream_and_of_two(window, sinks):
+    """Around the numbers of units at which their size changes, with requests in their own order and put in order."""
+    m = shape(8, 8, 64)
+    for n, rows in ((1, 16), (1, 17), (1, 300), (2, 290), (2, 300), (3, 310), (300, 17), (300, 1)):
+        new = np.full(n, rows)
+        new[n // 2:] = np.maximum(1, new[n // 2:] // 2)
+        c = attention_case(m, np.arange(n) * 37 % 200 + (900 if n == 1 else 0), new, window, sinks, seed=n)
+        out = run_attention(c, max_new=max(rows, 5))
+        check_attention(c, out, only=range(0, n, max(1, n // 3)))
+        assert torch.equal(out, run_attention(c, max_new=max(rows, 5)))
+
+
 def test_attention_many_units_per_cta():
     """More units than a CTA has records for, in every CTA."""
     c = attention_case(shape(8, 8, 64), [3] * 45, [140] * 45, 40, 3, seed=7)
