@@ -36,10 +36,10 @@ constexpr int FEW_WARPS = 4, FEW_THREADS = FEW_WARPS * 32;
 constexpr int FEW_MAX_CTAS = 640;    // of a launch; the records are laid out for so many
 constexpr int FEW_MIN_TILES = 4;     // of a CTA's run, while there are any
 constexpr int FEW_UNIT_TILES = 4;    // what a unit costs beside its tiles, in tiles
-constexpr int JOIN_THREADS = 256;
+constexpr int JOIN_UNITS = 16;        // up to so many units: large CTAs for the join (see there)
 // Calls that take all requests to the tiles (see the entry point): rows (of a kv head) of the longest, keys that a row sees, at most.
 constexpr int ALL_ROWS = 8, ALL_SHORT = 1536, ALL_KEYS = 8192, ALL_KEYS_32 = 256;
-constexpr int NEAR_CTAS = 16, NEAR_KEYS = 4096;   // a cluster per unit: its CTAs, keys that a row sees at most
+constexpr int NEAR_CTAS = 16;        // a cluster per unit
 
 // What the join needs of a unit that was cut, written by the CTA in whose run it begins.
 struct FewCut {
@@ -524,9 +524,13 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) blink_attn_few_kernel(const
 
 // The parts of the unit that begins, but does not end, in the run of CTA blockIdx.x.  A row's parts are shared out over warps, and these joined
 // in order: m = max m_i, l = sum l_i 2^(m_i - m), o = sum o_i 2^(m_i - m) / l.  Latency: 2 to 3 us behind a batch, 2.3 MB for 200 rows.
-template <typename T, int HD, int MR>
+// Few units have many parts each, and CTAs of 1024 threads for them; many would wait for such CTAs to be launched, most of them with nothing to do.  (us, with 256
+// | 1024 threads: one row behind 30000 keys 33.5 | 28.3, four of heads in eights 51 | 26, four of the 8B shape behind 1000 12.6 | 13.5, 64 behind 600 31 | 41;
+// with 128 38, 67, 13.6 and 31.)
+template <typename T, int HD, int MR, int JOIN_THREADS>
 __global__ void __launch_bounds__(JOIN_THREADS) blink_attn_join_kernel(const __grid_constant__ AttnArgs a) {
   constexpr int WARPS = JOIN_THREADS / 32, V = HD / 32;   // values of a row per lane
+  constexpr int AHEAD = JOIN_THREADS > 256 ? 8 : 4;       // records on their way
   __shared__ float s_acc[WARPS][HD];
   __shared__ float2 s_ml[WARPS];
   ops_next();
@@ -550,7 +554,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) blink_attn_join_kernel(const __g
       for (int p = part + share * lane; p < cut.parts; p += share * 32) M = fmaxf(M, ml[record(p)].x);
 #pragma unroll
       for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-#pragma unroll 4
+#pragma unroll AHEAD
       for (int p = part; p < cut.parts; p += share) {
         const float2 x = ml[record(p)];
         const float f = x.x == -INFINITY ? 0.f : exp2f(x.x - M);
@@ -703,7 +707,8 @@ static int few_run(const AttnArgs& a, int sms, void* stream) {
   const int grid = sms * CTAS < FEW_MAX_CTAS ? sms * CTAS : FEW_MAX_CTAS;
   const int rc = ops_launch(blink_attn_few_kernel<T, HD, W, CTAS>, grid, FEW_THREADS, smem, stream, 0, a);
   if (rc != BLINK_OK) return rc;
-  return ops_launch(blink_attn_join_kernel<T, HD, W::MR>, grid, JOIN_THREADS, 0, stream, 0, a);
+  if ((int64_t)a.n * a.pool.Hkv <= JOIN_UNITS) return ops_launch(blink_attn_join_kernel<T, HD, W::MR, 1024>, grid, 1024, 0, stream, 0, a);
+  return ops_launch(blink_attn_join_kernel<T, HD, W::MR, 256>, grid, 256, 0, stream, 0, a);
 }
 
 template <int HD>
@@ -782,13 +787,14 @@ int blink_window_attention(const blink_model_cfg* model, const blink_kv_pool* kv
     a.few = 0;
     return attn_tiles(a, sms, stream);
   }
-  // So few units that each can have a cluster of 16 CTAs, and rows that see no more than NEAR_KEYS keys.  (8B shape, rows x keys, us, the sequence | clusters
-  // of 16, 8, 4: 1 x 1000 12.5 | 8.9, 4 x 1000 14.6 | 17.7, 8 x 1000 16.7 | 16.9, 16 x 1000 20.8 | 22.9.)
+  // So few units that each can have a cluster of 16 CTAs, and rows that do not see too many keys.  (8B shape, rows x keys, us, the sequence | clusters
+  // of 16, 8, 4: 1 x 1000 12.5 | 8.9, 4 x 1000 14.6 | 17.7, 8 x 1000 16.7 | 16.9, 16 x 1000 20.8 | 22.9.  Of 16: 1 x 4000 18.4 | 10.9, 16000 25.9 | 24.3, 30000 33.9 |
+  // 39.9; heads of 64, 8000 17.3 | 13.4, 16000 18.9 | 22.5; 32 bits, 4000 20.9 | 19.7.)
   const int64_t mr = few_rows_of(model, max_new), rows_few = std::min<int64_t>(max_new, a.few);
   const int64_t groups = (rows_few * a.pool.rep + mr - 1) / mr, units = (int64_t)n_requests * a.pool.Hkv * groups;
   a.near_ctas = 0;
   a.first = bf16 || !tiles;
-  if (keys <= NEAR_KEYS && units * NEAR_CTAS <= sms) {
+  if (keys <= (bf16 ? 128 : 32) * a.pool.hd && units * NEAR_CTAS <= sms) {
     a.near_groups = (int)groups;
     a.near_ctas = NEAR_CTAS;
   }

@@ -245,6 +245,16 @@ def test_attention_a_long_context_is_shared_out_and_joined(rep, hkv, hd, dtype):
         check_attention(c, run_attention(c))
 
 
+@pytest.mark.parametrize("rep,hkv,hd,dtype,new", [(4, 2, 128, "bf16", 1), (4, 1, 128, "bf16", 6), (8, 1, 64, "bf16", 3), (1, 4, 64, "bf16", 1), (4, 1, 128, "fp32", 1)])
+def test_attention_one_request_from_short_to_very_long(rep, hkv, hd, dtype, new):
+    """A cluster for each unit, or pieces that are joined by small CTAs or large ones."""
+    for ctx in (0, 255, 4093, 8190, 16380, 20000):
+        c = attention_case(shape(rep, hkv, hd, dtype, layers=2), [ctx], [new], 0, 0, seed=ctx)
+        out = run_attention(c)
+        check_attention(c, out)
+        assert torch.equal(out, run_attention(c))
+
+
 def test_attention_rows_that_see_nothing_are_zeros():
     """More rows than cached tokens: positions below zero."""
     for dtype in ("bf16", "fp32"):
