@@ -7,7 +7,7 @@
 // (ops_attn_block.cu); which requests and calls take which stands at the entry point, with both sides measured.
 //
 // attn_few: requests of few rows (a token, a few drafts).  What bounds it: HBM, every visible key and value once.  (8B shape, a row each: 64 requests
-// behind 5000 keys 195 us, 6.7 TB/s; 256 752 us, 7.0; one behind 120000 keys 87 us, 5.7.)  With more rows, instructions: 48 requests of 4 rows behind
+// behind 5000 keys 195 us, 6.7 TB/s; 256 752 us, 7.0; one behind 120000 keys 82 us, 6.0.)  With more rows, instructions: 48 requests of 4 rows behind
 // 2500 keys 92 us, 5.3 TB/s, of 8 rows 131.  (Tiles copied ahead into shared memory, which leaves registers to more rows, cost time at every number of rows:
 // 5 rows 103 us, 127 so; it is not the loads that a warp waits for.)
 // A unit is a request, a kv head and up to MR (query row, head) rows, its tiles are the visible blocks of 16 keys.  All tiles of all units
