@@ -36,19 +36,19 @@ constexpr int FEW_WARPS = 4, FEW_THREADS = FEW_WARPS * 32;
 constexpr int FEW_MAX_CTAS = 640;    // of a launch; the records are laid out for so many
 constexpr int FEW_MIN_TILES = 4;     // of a CTA's run, while there are any
 constexpr int FEW_UNIT_TILES = 4;    // what a unit costs beside its tiles, in tiles
-constexpr int JOIN_UNITS = 16;        // up to so many units: large CTAs for the join (see there)
+constexpr int JOIN_THREADS = 256, JOIN_FEW = 4;   // parts that the CTA in whose run a unit begins joins by itself
 // Calls that take all requests to the tiles (see the entry point): rows (of a kv head) of the longest, keys that a row sees, at most.
 constexpr int ALL_ROWS = 8, ALL_SHORT = 1536, ALL_KEYS = 8192, ALL_KEYS_32 = 256;
 constexpr int NEAR_CTAS = 16;        // a cluster per unit
 
-// What the join needs of a unit that was cut, written by the CTA in whose run it begins.
+// What the join needs of a unit that was cut.  A CTA leaves two: of the unit in which its run begins, and of the one in which it ends.
 struct FewCut {
-  int parts;             // records: this CTA's second, the first of each of the following ones; 0: none
+  int first, parts;      // the CTA in whose run it begins; records, that CTA's second and the first of each of the following ones.  0: none
   int row, m0, m1, h;    // first row of the request, rows (of row * rep + head) m0 .. m1 - 1, kv head
 };
 
-// workspace: status, cuts [FEW_MAX_CTAS], (maximum, sum) [2 * FEW_MAX_CTAS][MR], values [2 * FEW_MAX_CTAS][MR][HD]
-__host__ __device__ constexpr size_t few_ml_at() { return ATTN_STATUS_BYTES + (sizeof(FewCut) * FEW_MAX_CTAS + 255) / 256 * 256; }
+// workspace: status, cuts [FEW_MAX_CTAS][2], (maximum, sum) [2 * FEW_MAX_CTAS][MR], values [2 * FEW_MAX_CTAS][MR][HD]
+__host__ __device__ constexpr size_t few_ml_at() { return ATTN_STATUS_BYTES + (sizeof(FewCut) * 2 * FEW_MAX_CTAS + 255) / 256 * 256; }
 __host__ __device__ constexpr size_t few_acc_at(int mr) { return few_ml_at() + (size_t)2 * FEW_MAX_CTAS * mr * 8; }
 __host__ __device__ constexpr size_t few_bytes(int mr, int hd) { return few_acc_at(mr) + (size_t)2 * FEW_MAX_CTAS * mr * hd * 4; }
 
@@ -438,7 +438,7 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) blink_attn_few_kernel(const
   const long long per = max((total + gridDim.x - 1) / gridDim.x, (long long)FEW_MIN_TILES);
   long long at = blockIdx.x * per;
   const long long end = min(total, at + per);
-  FewCut cut = {0, 0, 0, 0, 0};
+  FewCut begins = {}, ends = {};
   int r = 0;
   if (at < end) {
     int hi = a.n;
@@ -515,84 +515,99 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) blink_attn_few_kernel(const
         if (d == 0) rec_ml[row] = make_float2(M, L);
       }
     }
-    if (t0 == 0 && !whole) cut = FewCut{(int)((at + span.n - 1) / per) - (int)blockIdx.x + 1, req.start, m0, m1, h};
+    if (!whole) {
+      auto runs = [&](long long x) { return per < (1ll << 30) ? (int)((unsigned)x / (unsigned)per) : (int)(x / per); };   // (x: not much above per, or a unit's tiles)
+      const int before = t0 == 0 ? 0 : runs(t0 + per - 1);   // CTAs before this one that have a part
+      const FewCut cut = {(int)blockIdx.x - before, before + runs(at - blockIdx.x * per + span.n - t0 - 1) + 1, req.start, m0, m1, h};
+      if (t0 == 0) ends = cut; else begins = cut;
+    }
     at += t1 - t0;
   }
-  if (tid == 0) reinterpret_cast<FewCut*>(a.ws + ATTN_STATUS_BYTES)[blockIdx.x] = cut;
+  if (tid == 0) {
+    FewCut* cuts = reinterpret_cast<FewCut*>(a.ws + ATTN_STATUS_BYTES) + 2 * blockIdx.x;
+    cuts[0] = begins;
+    cuts[1] = ends;
+  }
   ops_wait();   // (a kernel before it in the call may still run)
 }
 
-// The parts of the unit that begins, but does not end, in the run of CTA blockIdx.x.  A row's parts are shared out over warps, and these joined
-// in order: m = max m_i, l = sum l_i 2^(m_i - m), o = sum o_i 2^(m_i - m) / l.  Latency: 2 to 3 us behind a batch, 2.3 MB for 200 rows.
-// Few units have many parts each, and CTAs of 1024 threads for them; many would wait for such CTAs to be launched, most of them with nothing to do.  (us, with 256
-// | 1024 threads: one row behind 30000 keys 33.5 | 28.3, four of heads in eights 51 | 26, four of the 8B shape behind 1000 12.6 | 13.5, 64 behind 600 31 | 41;
-// with 128 38, 67, 13.6 and 31.)
-template <typename T, int HD, int MR, int JOIN_THREADS>
+// The units that were cut: m = max m_i, l = sum l_i 2^(m_i - m), o = sum o_i 2^(m_i - m) / l over a row's parts.  The rows of a unit are dealt to the CTAs
+// whose runs it spans (as many as there are parts; up to JOIN_FEW, which many units have, one CTA has all of them, instead of two units one after the
+// other), a row's parts to warps, and these joined in order.  Latency: 2 to 3 us behind a batch.
+// (With a CTA per unit: three requests of 2 to 4 rows behind 2000 keys 26.5 us, 14.7 so; one row behind 30000 keys 33.5 and 28.  All dealt out: 64 rows behind 600 keys
+// 33.9, 31.4 so.)
+template <typename T, int HD, int MR>
 __global__ void __launch_bounds__(JOIN_THREADS) blink_attn_join_kernel(const __grid_constant__ AttnArgs a) {
   constexpr int WARPS = JOIN_THREADS / 32, V = HD / 32;   // values of a row per lane
-  constexpr int AHEAD = JOIN_THREADS > 256 ? 8 : 4;       // records on their way
   __shared__ float s_acc[WARPS][HD];
   __shared__ float2 s_ml[WARPS];
   ops_next();
   ops_wait();
-  const FewCut cut = reinterpret_cast<const FewCut*>(a.ws + ATTN_STATUS_BYTES)[blockIdx.x];
-  if (cut.parts == 0) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const float2* ml = reinterpret_cast<const float2*>(a.ws + few_ml_at());
   const float* acc = reinterpret_cast<const float*>(a.ws + few_acc_at(MR));
-  const int rows = cut.m1 - cut.m0;
-  const int share = rows >= WARPS ? 1 : WARPS / rows;   // warps of a row
-  const int at_once = WARPS / share;                     // rows at a time
-  for (int r0 = 0; r0 < rows; r0 += at_once) {
-    const int row = r0 + warp / share, part = warp % share;
-    const bool mine = warp / share < at_once && row < rows;
-    float M = -INFINITY, L = 0.f, o[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) o[v] = 0.f;
-    auto record = [&](int p) { return (size_t)(2 * (blockIdx.x + p) + (p == 0 ? 1 : 0)) * MR + row; };
-    if (mine) {
-      for (int p = part + share * lane; p < cut.parts; p += share * 32) M = fmaxf(M, ml[record(p)].x);
-#pragma unroll
-      for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-#pragma unroll AHEAD
-      for (int p = part; p < cut.parts; p += share) {
-        const float2 x = ml[record(p)];
-        const float f = x.x == -INFINITY ? 0.f : exp2f(x.x - M);
-        const float* z = acc + record(p) * HD + lane * V;
-        L = fmaf(x.y, f, L);
-        if constexpr (V == 4) {
-          const float4 y = *reinterpret_cast<const float4*>(z);
-          o[0] = fmaf(y.x, f, o[0]); o[1] = fmaf(y.y, f, o[1]); o[2] = fmaf(y.z, f, o[2]); o[3] = fmaf(y.w, f, o[3]);
-        } else {
-          const float2 y = *reinterpret_cast<const float2*>(z);
-          o[0] = fmaf(y.x, f, o[0]); o[1] = fmaf(y.y, f, o[1]);
-        }
-      }
-#pragma unroll
-      for (int v = 0; v < V; ++v) s_acc[warp][lane * V + v] = o[v];
-      if (lane == 0) s_ml[warp] = make_float2(M, L);
-    }
-    __syncthreads();
-    if (mine && part == 0) {
-      float top = -INFINITY, sum = 0.f;
-      for (int k = 0; k < share; ++k) top = fmaxf(top, s_ml[warp + k].x);
+  const FewCut* cuts = reinterpret_cast<const FewCut*>(a.ws + ATTN_STATUS_BYTES) + 2 * blockIdx.x;
+  const FewCut both[2] = {cuts[0], cuts[1]};
+#pragma unroll 1
+  for (int e = 0; e < 2; ++e) {
+    const FewCut cut = e ? both[1] : both[0];
+    if (cut.parts == 0) continue;
+    const int hands = cut.parts > JOIN_FEW ? cut.parts : 1, mine_first = (int)blockIdx.x - cut.first;   // rows mine_first, mine_first + hands, ..
+    const int rows = hands == 1 ? (mine_first == 0 ? cut.m1 - cut.m0 : 0) : (cut.m1 - cut.m0 - mine_first + hands - 1) / hands;
+    if (rows <= 0) continue;
+    const int share = rows >= WARPS ? 1 : WARPS / rows;   // warps of a row
+    const int at_once = WARPS / share;                     // rows at a time
+    for (int r0 = 0; r0 < rows; r0 += at_once) {
+      const int r = r0 + warp / share, part = warp % share, row = mine_first + r * hands;
+      const bool mine = warp / share < at_once && r < rows;
+      float M = -INFINITY, L = 0.f, o[V];
 #pragma unroll
       for (int v = 0; v < V; ++v) o[v] = 0.f;
-      for (int k = 0; k < share; ++k) {
-        const float2 x = s_ml[warp + k];
-        const float f = x.x == -INFINITY ? 0.f : exp2f(x.x - top);
-        sum = fmaf(x.y, f, sum);
+      auto record = [&](int p) { return (size_t)(2 * (cut.first + p) + (p == 0 ? 1 : 0)) * MR + row; };
+      if (mine) {
+        for (int p = part + share * lane; p < cut.parts; p += share * 32) M = fmaxf(M, ml[record(p)].x);
 #pragma unroll
-        for (int v = 0; v < V; ++v) o[v] = fmaf(s_acc[warp + k][lane * V + v], f, o[v]);
+        for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+#pragma unroll 4
+        for (int p = part; p < cut.parts; p += share) {
+          const float2 x = ml[record(p)];
+          const float f = x.x == -INFINITY ? 0.f : exp2f(x.x - M);
+          const float* z = acc + record(p) * HD + lane * V;
+          L = fmaf(x.y, f, L);
+          if constexpr (V == 4) {
+            const float4 y = *reinterpret_cast<const float4*>(z);
+            o[0] = fmaf(y.x, f, o[0]); o[1] = fmaf(y.y, f, o[1]); o[2] = fmaf(y.z, f, o[2]); o[3] = fmaf(y.w, f, o[3]);
+          } else {
+            const float2 y = *reinterpret_cast<const float2*>(z);
+            o[0] = fmaf(y.x, f, o[0]); o[1] = fmaf(y.y, f, o[1]);
+          }
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) s_acc[warp][lane * V + v] = o[v];
+        if (lane == 0) s_ml[warp] = make_float2(M, L);
       }
-      const float inv = sum > 0.f ? 1.f / sum : 0.f;
-      const int mr = cut.m0 + row;
-      T* dst = static_cast<T*>(a.out) + (cut.row + mr / a.pool.rep) * a.out_stride + (cut.h * a.pool.rep + mr % a.pool.rep) * HD + lane * V;
-      if constexpr (V == 4) few_store(dst, make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv));
-      else if constexpr (sizeof(T) == 2) *reinterpret_cast<__nv_bfloat162*>(dst) = __floats2bfloat162_rn(o[0] * inv, o[1] * inv);
-      else *reinterpret_cast<float2*>(dst) = make_float2(o[0] * inv, o[1] * inv);
+      __syncthreads();
+      if (mine && part == 0) {
+        float top = -INFINITY, sum = 0.f;
+        for (int k = 0; k < share; ++k) top = fmaxf(top, s_ml[warp + k].x);
+#pragma unroll
+        for (int v = 0; v < V; ++v) o[v] = 0.f;
+        for (int k = 0; k < share; ++k) {
+          const float2 x = s_ml[warp + k];
+          const float f = x.x == -INFINITY ? 0.f : exp2f(x.x - top);
+          sum = fmaf(x.y, f, sum);
+#pragma unroll
+          for (int v = 0; v < V; ++v) o[v] = fmaf(s_acc[warp + k][lane * V + v], f, o[v]);
+        }
+        const float inv = sum > 0.f ? 1.f / sum : 0.f;
+        const int mr = cut.m0 + row;
+        T* dst = static_cast<T*>(a.out) + (cut.row + mr / a.pool.rep) * a.out_stride + (cut.h * a.pool.rep + mr % a.pool.rep) * HD + lane * V;
+        if constexpr (V == 4) few_store(dst, make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv));
+        else if constexpr (sizeof(T) == 2) *reinterpret_cast<__nv_bfloat162*>(dst) = __floats2bfloat162_rn(o[0] * inv, o[1] * inv);
+        else *reinterpret_cast<float2*>(dst) = make_float2(o[0] * inv, o[1] * inv);
+      }
+      __syncthreads();
     }
-    __syncthreads();
   }
 }
 
@@ -707,8 +722,7 @@ static int few_run(const AttnArgs& a, int sms, void* stream) {
   const int grid = sms * CTAS < FEW_MAX_CTAS ? sms * CTAS : FEW_MAX_CTAS;
   const int rc = ops_launch(blink_attn_few_kernel<T, HD, W, CTAS>, grid, FEW_THREADS, smem, stream, 0, a);
   if (rc != BLINK_OK) return rc;
-  if ((int64_t)a.n * a.pool.Hkv <= JOIN_UNITS) return ops_launch(blink_attn_join_kernel<T, HD, W::MR, 1024>, grid, 1024, 0, stream, 0, a);
-  return ops_launch(blink_attn_join_kernel<T, HD, W::MR, 256>, grid, 256, 0, stream, 0, a);
+  return ops_launch(blink_attn_join_kernel<T, HD, W::MR>, grid, JOIN_THREADS, 0, stream, 0, a);
 }
 
 template <int HD>
