@@ -803,7 +803,8 @@ int blink_window_attention(const blink_model_cfg* model, const blink_kv_pool* kv
   }
   // So few units that each can have a cluster of 16 CTAs, and rows that do not see too many keys.  (8B shape, rows x keys, us, the sequence | clusters
   // of 16, 8, 4: 1 x 1000 12.5 | 8.9, 4 x 1000 14.6 | 17.7, 8 x 1000 16.7 | 16.9, 16 x 1000 20.8 | 22.9.  Of 16: 1 x 4000 18.4 | 10.9, 16000 25.9 | 24.3, 30000 33.9 |
-  // 39.9; heads of 64, 8000 17.3 | 13.4, 16000 18.9 | 22.5; 32 bits, 4000 20.9 | 19.7.)
+  // 39.9; heads of 64, 8000 17.3 | 13.4, 16000 18.9 | 22.5; 32 bits, 4000 20.9 | 19.7.  Of one CTA: 4 x 100 9.2 | 5.9, 16 x 100
+  // 11.3 | 6.3, 16 x 400 14.4 | 10.5, 16 x 800 17.2 | 18.0, 64 x 50 13.7 | 11.2, 64 x 200 18.6 | 19.3, 200 x 200 37.8 | 40.1; heads of 64, 64 x 200 14.0 | 10.3.)
   const int64_t mr = few_rows_of(model, max_new), rows_few = std::min<int64_t>(max_new, a.few);
   const int64_t groups = (rows_few * a.pool.rep + mr - 1) / mr, units = (int64_t)n_requests * a.pool.Hkv * groups;
   a.near_ctas = 0;
@@ -811,6 +812,9 @@ int blink_window_attention(const blink_model_cfg* model, const blink_kv_pool* kv
   if (keys <= (bf16 ? 128 : 32) * a.pool.hd && units * NEAR_CTAS <= sms) {
     a.near_groups = (int)groups;
     a.near_ctas = NEAR_CTAS;
+  } else if (units <= 2 * sms ? keys <= 512 : units <= 4 * sms && keys <= 128) {   // or short enough for one CTA each, without a join
+    a.near_groups = (int)groups;
+    a.near_ctas = 1;
   }
   // In 32 bits where a row sees so little that the kernels for few rows only add their launches.  (us, with them | without: the small shape, 8 requests of
   // 40 rows behind 30 keys 17.1 | 13.1, 64 of one row and one of 40 behind 200 keys 46 | 26; the 8B shape, 4 and one 43 | 35, but behind 450 keys 24 | 62

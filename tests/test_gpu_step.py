@@ -245,6 +245,18 @@ def test_attention_a_long_context_is_shared_out_and_joined(rep, hkv, hd, dtype):
         check_attention(c, run_attention(c))
 
 
+@pytest.mark.parametrize("rep,hkv,hd,dtype", SHAPES)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (513, 20), (700, 4), (600, 64)])
+def test_attention_wide_tables(rep, hkv, hd, dtype, window, sinks):
+    """Tables with room for long contexts, of which requests use little, or as much as a window: pieces of units, joined."""
+    for new in ([1] * 9, [3, 1, 0, 2, 4, 1, 2, 1, 2]):
+        c = attention_case(shape(rep, hkv, hd, dtype), [0, 1400, 15, 16, 800, 47, 1203, 200, 333], new, window, sinks, seed=window + len(set(new)))
+        c["table"] = torch.nn.functional.pad(c["table"], (0, 1200), value=-1)
+        out = run_attention(c)
+        check_attention(c, out)
+        assert torch.equal(out, run_attention(c))
+
+
 @pytest.mark.parametrize("rep,hkv,hd,dtype,new", [(4, 2, 128, "bf16", 1), (4, 1, 128, "bf16", 6), (8, 1, 64, "bf16", 3), (1, 4, 64, "bf16", 1), (4, 1, 128, "fp32", 1)])
 def test_attention_one_request_from_short_to_very_long(rep, hkv, hd, dtype, new):
     """A cluster for each unit, or pieces that are joined by small CTAs or large ones."""
