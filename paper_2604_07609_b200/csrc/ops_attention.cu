@@ -39,7 +39,6 @@ constexpr int FEW_UNIT_TILES = 4;    // what a unit costs beside its tiles, in t
 constexpr int JOIN_THREADS = 256, JOIN_FEW = 4;   // parts that the CTA in whose run a unit begins joins by itself
 // Calls that take all requests to the tiles (see the entry point): rows (of a kv head) of the longest, keys that a row sees, at most.
 constexpr int ALL_ROWS = 8, ALL_SHORT = 1536, ALL_KEYS = 8192, ALL_KEYS_32 = 256;
-constexpr int NEAR_CTAS = 16;        // a cluster per unit
 
 // What the join needs of a unit that was cut.  A CTA leaves two: of the unit in which its run begins, and of the one in which it ends.
 struct FewCut {
@@ -613,7 +612,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) blink_attn_join_kernel(const __g
 
 // The same for few units and short contexts, where latency is all there is: a cluster of CTAs per unit, which share its tiles and join their records
 // through distributed shared memory.  One kernel instead of two, no sequence to be added up first: a row of 1028 keys of the 8B shape
-// 8.0 us, 12.3 with the kernels above (some 3 us are the launch, the rest loads that wait for one another: lengths, block ids, keys).
+// 7.5 us, 12.3 with the kernels above (some 3 us are the launch, the rest loads that wait for one another: lengths, block ids, keys).
 // a.few as there; `groups` clusters per (request, kv head), a group of rows each, or every groups-th where there are more.
 template <typename T, int HD, typename W>
 __global__ void __launch_bounds__(FEW_THREADS) blink_attn_near_kernel(const __grid_constant__ AttnArgs a, const int groups) {
@@ -801,20 +800,22 @@ int blink_window_attention(const blink_model_cfg* model, const blink_kv_pool* kv
     a.few = 0;
     return attn_tiles(a, sms, stream);
   }
-  // So few units that each can have a cluster of 16 CTAs, and rows that do not see too many keys.  (8B shape, rows x keys, us, the sequence | clusters
-  // of 16, 8, 4: 1 x 1000 12.5 | 8.9, 4 x 1000 14.6 | 17.7, 8 x 1000 16.7 | 16.9, 16 x 1000 20.8 | 22.9.  Of 16: 1 x 4000 18.4 | 10.9, 16000 25.9 | 24.3, 30000 33.9 |
-  // 39.9; heads of 64, 8000 17.3 | 13.4, 16000 18.9 | 22.5; 32 bits, 4000 20.9 | 19.7.  Of one CTA: 4 x 100 9.2 | 5.9, 16 x 100
-  // 11.3 | 6.3, 16 x 400 14.4 | 10.5, 16 x 800 17.2 | 18.0, 64 x 50 13.7 | 11.2, 64 x 200 18.6 | 19.3, 200 x 200 37.8 | 40.1; heads of 64, 64 x 200 14.0 | 10.3.)
   const int64_t mr = few_rows_of(model, max_new), rows_few = std::min<int64_t>(max_new, a.few);
   const int64_t groups = (rows_few * a.pool.rep + mr - 1) / mr, units = (int64_t)n_requests * a.pool.Hkv * groups;
   a.near_ctas = 0;
   a.first = bf16 || !tiles;
-  if (keys <= (bf16 ? 128 : 32) * a.pool.hd && units * NEAR_CTAS <= sms) {
+  // A cluster for each unit, of as many CTAs as its keys are worth and there is room for; the sequence of tiles where units are many or long.  (One row of the 8B
+  // shape, us, clusters of 1 | 4 | 8 | 16: behind 15 keys 4.8 | 5.4 | 5.9 | 6.9, 250 7.4 | 6.0 | 6.4 | 7.7, 1000 15.0 | 8.0 | 7.1 | 7.7, 2000 25 | 10.5 | 8.5 | 8.8; 32 bits, 500
+  // 22 | 10.1 | 8.6 | 10.4, 1000 39 | 14.3 | 10.9 | 10.5.  The sequence | so: 1 x 4000 18.4 | 10.9, 16000 25.9 | 24.3, 30000 33.9 | 39.9; heads of 64, 8000
+  // 17.3 | 13.4, 16000 18.9 | 22.5; 4 x 100 9.2 | 5.9, 3 x 1000 of 4 rows 13.1 | 9.6, 8 x 1000 14.7 | 11.7, 16 x 400 14.4 | 10.5, 16 x 800 17.3 | 16.4, 64 x 50 13.7 | 11.2,
+  // 64 x 200 18.6 | 19.3.)
+  int ctas = keys <= 64 ? 1 : keys <= 256 ? 4 : keys <= (bf16 ? 2048 : 512) ? 8 : 16;
+  while (ctas > 1 && units * ctas > (ctas == 16 ? sms : 2 * sms)) ctas /= 2;
+  if (ctas == 2 && keys <= 512) ctas = 1;   // (16 x 200: 8.5 | 7.8)
+  const int64_t limit = ctas == 16 ? (bf16 ? 128 : 32) * a.pool.hd : units > 2 * sms ? (units > 4 * sms ? 0 : 128) : (bf16 ? 512 : 256) * ctas;
+  if (keys <= limit) {
     a.near_groups = (int)groups;
-    a.near_ctas = NEAR_CTAS;
-  } else if (units <= 2 * sms ? keys <= 512 : units <= 4 * sms && keys <= 128) {   // or short enough for one CTA each, without a join
-    a.near_groups = (int)groups;
-    a.near_ctas = 1;
+    a.near_ctas = ctas;
   }
   // In 32 bits where a row sees so little that the kernels for few rows only add their launches.  (us, with them | without: the small shape, 8 requests of
   // 40 rows behind 30 keys 17.1 | 13.1, 64 of one row and one of 40 behind 200 keys 46 | 26; the 8B shape, 4 and one 43 | 35, but behind 450 keys 24 | 62
