@@ -369,9 +369,12 @@ __global__ void __launch_bounds__(PICK_THREADS, 2) blink_verify_draw_kernel(cons
   const int w0 = (rank * PICK_WARPS + warp) * tiles * TILE;
   const float* z = a.logits + row * a.logits_stride;
   const float* q = choice.refused && a.probs ? a.probs + row * a.probs_stride : nullptr;
+  const float* const q_rests = q;
+  if (tiles > 1) q = nullptr;   // (of several tiles each is copied when its rests are taken: the sum of exponentials does without q)
   float zv[EACH];   // of the warp's first tile
   ver_load(zv, z + w0, V - w0, a.vec, -INFINITY);
   auto fetch_q = [&](int at) {   // behind the end: zeros
+    asm volatile("cp.async.wait_group 0;" ::: "memory");   // (copies that are on their way into the same place have no order among themselves)
     const bool whole = a.probs_vec && at + TILE <= V;
 #pragma unroll
     for (int g = 0; g < EACH / 4; ++g) {
@@ -459,6 +462,7 @@ __global__ void __launch_bounds__(PICK_THREADS, 2) blink_verify_draw_kernel(cons
       }
     }
   };
+  q = q_rests;
   bool have = tiles == 1;   // the exponentials of the only tile are in e
   auto rest_sum = [&]() {
     double r = 0.0;

@@ -75,3 +75,13 @@ def test_registers_of_a_tensor_memory_load_are_not_touched_before_the_wait():
                 head = text[:call.start()].rstrip()
                 assert head[-1] in ";{}", f"{f}: {call.group(0)} under a condition"
                 assert re.search(r"tmem_wait_ld\w*\([^;]*\b%s\b[^;]*\);" % call.group(2), text[call.end():i]), f"{f}: {call.group(0)} is not waited for in its block"
+
+
+def test_copies_into_one_place_do_not_overtake_one_another():
+    """Asynchronous copies of different groups have no order among themselves: before another is begun into the place of a warp's
+    tile of draft probabilities, what was on its way there has landed."""
+    body = _body(re.sub(r"//[^\n]*", "", _text("ops_verify.cu")), "blink_verify_draw_kernel")
+    fetch = body[body.index("auto fetch_q = "):]
+    fetch = fetch[:fetch.index("cp.async.commit_group")]
+    assert 0 < fetch.find("cp.async.wait_group 0") < fetch.index("cp.async.c")
+    assert body.count("cp.async.c") == fetch.count("cp.async.c") + 1      # (and its commit) nobody else copies there

@@ -722,3 +722,18 @@ def test_the_binding_refuses_what_does_not_fit():
         B.blink_window_attention(*args, workspace=torch.empty(1024, dtype=torch.uint8, device="cuda"))
     with pytest.raises(ValueError):
         B.blink_window_attention(*args, out=c["q"][:1].clone())
+
+
+# ---- vocabularies that a draw goes over in several tiles --------------------------------------------------------------
+@pytest.mark.parametrize("V", [131073, 150000, 393217])
+def test_verify_refused_drafts_of_a_vocabulary_of_several_tiles(V):
+    """The token comes from p - q, tile by tile: each with its own q."""
+    rng = np.random.default_rng(V)
+    k = [2, 1, 3]
+    c = verify_case(rng, k, V, True, [1.0, 0.8, 1.2], spread=1.0)
+    c["ua"][:] = 1e9                         # the first draft of each is refused
+    tokens, accepted = run_verify(c)
+    assert accepted.tolist() == [0, 0, 0]
+    check_verify(c, tokens, accepted)
+    for _ in range(10):
+        assert torch.equal(run_verify(c)[0], tokens)
