@@ -52,7 +52,7 @@ struct TilShape {
 
 struct TilShared {
   uint64_t q_full[2], s_full[2], p_full[2], o_full[2];
-  uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], v_land, unit_full[8];
+  uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], v_land, unit_full[8], unit_empty[8];
   float row[2][2][128];   // of a stream's rows, from either of their threads: maxima, or sums
   uint64_t x_full, x_done;   // a unit that the streams share: stream 1's results are there; have been read
   float2 other[128];         // maxima and sums of stream 1's rows then
@@ -281,7 +281,7 @@ struct alignas(16) TilUnit {
   __device__ __forceinline__ int begin_of(int s) const { return s ? begin[1] : begin[0]; }
   __device__ __forceinline__ int end_of(int s) const { return s ? end[1] : end[0]; }
 };
-constexpr int TIL_UNITS = 8;   // records of a CTA's units, used in turn: nobody is more than a few behind the warp that writes them
+constexpr int TIL_UNITS = 8;   // records of a CTA's units, used in turn: one is written again when all warps have read it
 
 template <int HD>
 __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap map) {
@@ -312,7 +312,10 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
     til_init(&sh.v_land, 1);
     til_init(&sh.x_full, TIL_SOFT / 2);
     til_init(&sh.x_done, TIL_SOFT / 2);
-    for (int i = 0; i < TIL_UNITS; ++i) til_init(&sh.unit_full[i], 1);
+    for (int i = 0; i < TIL_UNITS; ++i) {
+      til_init(&sh.unit_full[i], 1);
+      til_init(&sh.unit_empty[i], TIL_WARPS);
+    }
     sh.dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -437,6 +440,8 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
     const int slot = i % TIL_UNITS;
     wait(&sh.unit_full[slot], (uint32_t)(i / TIL_UNITS) & 1u);
     TilUnit t = s_unit[slot];
+    __syncwarp();
+    if (lane == 0) til_arrive(&sh.unit_empty[slot]);
     if (!ok) t.live[0] = 0;
     return t;
   };
@@ -445,7 +450,8 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
     TilUnit t;
     if (u < n_units) t = make_unit(u);
     else t.live[0] = 0;
-    if (lane == 0) {
+    if (i >= TIL_UNITS) wait(&sh.unit_empty[i % TIL_UNITS], (uint32_t)(i / TIL_UNITS - 1) & 1u);
+    if (ok && lane == 0) {
       s_unit[i % TIL_UNITS] = t;
       til_arrive(&sh.unit_full[i % TIL_UNITS]);
     }

@@ -85,3 +85,18 @@ def test_copies_into_one_place_do_not_overtake_one_another():
     fetch = fetch[:fetch.index("cp.async.commit_group")]
     assert 0 < fetch.find("cp.async.wait_group 0") < fetch.index("cp.async.c")
     assert body.count("cp.async.c") == fetch.count("cp.async.c") + 1      # (and its commit) nobody else copies there
+
+
+def test_a_unit_is_written_over_when_all_warps_have_read_it():
+    """The records of a CTA's units are used in turn.  Every warp says that it has read one, and whoever writes waits for all of them."""
+    text = re.sub(r"//[^\n]*", "", _text("ops_attn_tiles.cu"))
+    assert re.search(r"til_init\(&sh\.unit_empty\[i\], TIL_WARPS\)", text)
+    read = text[text.index("auto unit_of = "):]
+    read = read[:read.index("return t;")]
+    at = [read.index(x) for x in ("wait(&sh.unit_full[slot]", "t = s_unit[slot]", "__syncwarp()", "til_arrive(&sh.unit_empty[slot])")]
+    assert at == sorted(at)
+    write = text[text.index("auto hand_out = "):]
+    at = [write.index(x) for x in ("if (i >= TIL_UNITS) wait(&sh.unit_empty[i % TIL_UNITS], (uint32_t)(i / TIL_UNITS - 1) & 1u)", "s_unit[i % TIL_UNITS] = t",
+                                   "til_arrive(&sh.unit_full[i % TIL_UNITS])")]
+    assert at == sorted(at)
+    assert text.count("s_unit[") == 2         # nobody else reads or writes them

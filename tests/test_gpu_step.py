@@ -737,3 +737,18 @@ def test_verify_refused_drafts_of_a_vocabulary_of_several_tiles(V):
     check_verify(c, tokens, accepted)
     for _ in range(10):
         assert torch.equal(run_verify(c)[0], tokens)
+
+
+# ---- a long run of short units ----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("rep,hkv,hd,window", [(4, 8, 64, 0), (8, 2, 128, 0), (4, 4, 128, 9)])
+def test_attention_runs_of_short_units_and_long_ones_among_them(rep, hkv, hd, window):
+    """Many units of one tile of keys a CTA, with rows for one stream only: the other one passes them by."""
+    rng = np.random.default_rng(hd + rep)
+    n = 3000
+    new = rng.integers(2, 5, n)
+    new[::97] = 300                          # two streams, several tiles
+    c = attention_case(shape(rep, hkv, hd, layers=1), rng.integers(0, 60, n), new, window, 1, seed=n, layer=0)
+    out = run_attention(c)
+    check_attention(c, out, only=[0, 1, 2, 96, 97, 98] + rng.permutation(n)[:60].tolist())
+    for _ in range(5):
+        assert torch.equal(run_attention(c), out)
