@@ -55,7 +55,7 @@ template <typename... P, typename... A>
 inline int ops_launch(void (*kernel)(P...), int64_t grid, int threads, size_t smem, void* stream, int cluster, A... args) {
   if (grid < 1) return BLINK_OK;
   if (grid > 0x7fffffffll) return BLINK_ETOOBIG;
-  if (smem > 48 * 1024) {
+  if (smem > 40 * 1024) {   // (48 KB are free to a kernel, its static shared memory among them, of which none that takes dynamic memory has more than 8 KB)
     const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return ops_launched(e);
   }

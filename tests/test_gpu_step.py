@@ -752,3 +752,35 @@ def test_attention_runs_of_short_units_and_long_ones_among_them(rep, hkv, hd, wi
     check_attention(c, out, only=[0, 1, 2, 96, 97, 98] + rng.permutation(n)[:60].tolist())
     for _ in range(5):
         assert torch.equal(run_attention(c), out)
+
+
+# ---- launches ---------------------------------------------------------------------------------------------------------
+def fresh_process(code):
+    """Runs code in a process of its own (the state of a kernel's attributes outlives a call); it prints nothing when it is right."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", "import sys; sys.path[:0] = [%r, %r]\n" % (root, os.path.join(root, "tests")) + code], capture_output=True, text=True,
+                       timeout=300, cwd=root)
+    assert r.returncode == 0 and r.stdout == "", r.stdout + r.stderr
+
+
+def test_tables_where_dynamic_and_static_shared_memory_reach_48_kb_together():
+    fresh_process("""
+import numpy as np
+from test_gpu_step import check_tables, tables_case
+for n in (3037, 3038, 3039, 3055, 3070, 3071):
+    check_tables(*tables_case(np.random.default_rng(n), n, 20, 2, 3))
+""")
+
+
+@pytest.mark.parametrize("hd,sizes", [(128, (1996, 1997, 1998, 1999, 2000)), (64, (2508, 2509, 2510, 2511, 2512))])
+def test_attention_where_dynamic_and_static_shared_memory_reach_48_kb_together(hd, sizes):
+    fresh_process(f"""
+import numpy as np
+from test_gpu_step import attention_case, check_attention, run_attention, shape
+for n in {sizes}:
+    c = attention_case(shape(1, 1, {hd}, layers=1), np.random.default_rng(n).integers(1, 90, n), [1] * n, 0, 0, seed=n, layer=0)
+    check_attention(c, run_attention(c), only=[0, 1, n // 2, n - 1])
+""")
