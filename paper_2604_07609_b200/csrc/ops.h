@@ -48,15 +48,23 @@ inline int ops_launched(cudaError_t e) {
   return e == cudaSuccess ? BLINK_OK : BLINK_ECUDA;
 }
 
+// Dynamic shared memory of a launch, and the most that the same kernel is ever launched with.  The limit of a kernel is the device's, whoever calls: were
+// it set to what one call needs, the launch of another host thread that needs more could come right behind that and be refused.
+struct OpsShared {
+  size_t bytes, most;
+  OpsShared(size_t always) : bytes(always), most(always) {}
+  OpsShared(size_t now, size_t at_most) : bytes(now), most(at_most) {}
+};
+
 // cluster > 0: CTAs of a cluster.  Kernels are set up while the one before them in the stream still runs (1 to 2 us less a launch) and wait for
 // it themselves: the first kernel of a call in all of its threads before anything else (ops_begin), the later ones before they read what it
 // wrote, or at their end at the latest, so that a kernel that is done says that all before it are.
 template <typename... P, typename... A>
-inline int ops_launch(void (*kernel)(P...), int64_t grid, int threads, size_t smem, void* stream, int cluster, A... args) {
+inline int ops_launch(void (*kernel)(P...), int64_t grid, int threads, OpsShared smem, void* stream, int cluster, A... args) {
   if (grid < 1) return BLINK_OK;
   if (grid > 0x7fffffffll) return BLINK_ETOOBIG;
-  if (smem > 40 * 1024) {   // (48 KB are free to a kernel, its static shared memory among them, of which none that takes dynamic memory has more than 8 KB)
-    const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (smem.bytes > 40 * 1024) {   // (48 KB are free to a kernel, its static shared memory among them, of which none that takes dynamic memory has more than 8 KB)
+    const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem.most);
     if (e != cudaSuccess) return ops_launched(e);
   }
   if (cluster > 8) {   // more than every device takes
@@ -66,7 +74,7 @@ inline int ops_launch(void (*kernel)(P...), int64_t grid, int threads, size_t sm
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3((unsigned)threads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = smem.bytes;
   cfg.stream = static_cast<cudaStream_t>(stream);
   cudaLaunchAttribute at[2];
   int n = 0;

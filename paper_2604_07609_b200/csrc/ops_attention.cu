@@ -717,7 +717,8 @@ static int few_run(const AttnArgs& a, int sms, void* stream) {
     const size_t need = (size_t)FEW_WARPS * W::MR * (W::PITCH * 4 + 8) + W::MR * 8 + W::Q_BYTES;
     return ops_launch(blink_attn_near_kernel<T, HD, W>, ctas, FEW_THREADS, need, stream, a.near_ctas, a, a.near_groups);
   }
-  const size_t smem = (size_t)FEW_WARPS * W::MR * (W::PITCH * 4 + 8) + W::Q_BYTES + (size_t)(a.n + 1) * 16;
+  const size_t unit = (size_t)FEW_WARPS * W::MR * (W::PITCH * 4 + 8) + W::Q_BYTES;
+  const OpsShared smem(unit + (size_t)(a.n + 1) * 16, unit + (size_t)(OPS_MAX_REQUESTS + 1) * 16);
   const int grid = sms * CTAS < FEW_MAX_CTAS ? sms * CTAS : FEW_MAX_CTAS;
   const int rc = ops_launch(blink_attn_few_kernel<T, HD, W, CTAS>, grid, FEW_THREADS, smem, stream, 0, a);
   if (rc != BLINK_OK) return rc;

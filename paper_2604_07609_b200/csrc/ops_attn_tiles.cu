@@ -846,7 +846,8 @@ static int tiles_run(const AttnArgs& a, int sms, int64_t most_units, void* strea
   if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, a.pool.k, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return BLINK_ECUDA;
-  const size_t smem = (size_t)S::END + 1024 + TIL_UNITS * sizeof(TilUnit) + (size_t)(a.n + 1) * 4;
+  const size_t fixed = (size_t)S::END + 1024 + TIL_UNITS * sizeof(TilUnit);
+  const OpsShared smem(fixed + (size_t)(a.n + 1) * 4, fixed + (size_t)(OPS_MAX_REQUESTS + 1) * 4);
   const int64_t grid = most_units < sms ? most_units : sms;
   if (a.few == 0) {
     const int rc = ops_launch(blink_attn_begin_kernel, 1, 32, 0, stream, 0, reinterpret_cast<int*>(a.ws));

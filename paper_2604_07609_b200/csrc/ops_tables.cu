@@ -179,6 +179,6 @@ extern "C" int blink_build_tables(const int32_t* ctx_len, const int32_t* new_len
                         block_table, blocks_held_out, free_count_out, row_start, kv_len, positions, slot_map, status};
   // (four rows a thread: 110 thousand rows of 256 requests 6.9 us with eight CTAs, 5.3 with 16)
   const int cluster = max_rows > 32 * TAB_THREADS ? 16 : max_rows > 4 * TAB_THREADS || n_requests > TAB_THREADS ? 8 : 1;
-  const size_t smem = (size_t)(4 * n_requests + 2) * 4;
+  const OpsShared smem((size_t)(4 * n_requests + 2) * 4, (size_t)(4 * OPS_MAX_REQUESTS + 2) * 4);
   return ops_launch(blink_tables_kernel, cluster, TAB_THREADS, smem, stream, cluster, a);
 }

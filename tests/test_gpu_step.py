@@ -784,3 +784,42 @@ for n in {sizes}:
     c = attention_case(shape(1, 1, {hd}, layers=1), np.random.default_rng(n).integers(1, 90, n), [1] * n, 0, 0, seed=n, layer=0)
     check_attention(c, run_attention(c), only=[0, 1, n // 2, n - 1])
 """)
+
+
+def in_two_threads(calls, times=2000):
+    """Both calls again and again, each by a host thread with a stream of its own (ctypes lets go of the interpreter); the codes other
+    than BLINK_OK."""
+    import threading
+    bad, gate = [], threading.Barrier(len(calls))
+
+    def loop(call):
+        stream = torch.cuda.Stream()
+        gate.wait()
+        for i in range(times):
+            rc = call(stream.cuda_stream)
+            if rc != B.BLINK_OK:
+                bad.append(rc)
+            if i % 100 == 99:
+                stream.synchronize()
+    threads = [threading.Thread(target=loop, args=(c,)) for c in calls]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    return bad
+
+
+def test_tables_of_different_sizes_from_two_host_threads():
+    def caller(n):
+        rows = 64
+        zero, one = torch.zeros(n, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+        out = B.make_step_tables(n, rows, "cuda")
+        table = torch.zeros(n, 1, dtype=torch.int32, device="cuda")
+        p = lambda t: t.data_ptr()
+        return lambda stream, keep=(zero, one, out, table): B.lib().blink_build_tables(
+            p(zero), p(zero), p(zero), n, p(one), 1, p(one), p(table), 1, rows, p(out.blocks_held), p(out.free_count), p(out.row_start), p(out.kv_len),
+            p(out.positions), p(out.slot_map), p(out.status), stream)
+    calls = [caller(4096), caller(2700)]
+    torch.cuda.synchronize()
+    assert in_two_threads(calls) == []
