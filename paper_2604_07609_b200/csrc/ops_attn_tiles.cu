@@ -836,6 +836,11 @@ __global__ void blink_attn_begin_kernel(int* ws) {
 template <int HD>
 static int tiles_run(const AttnArgs& a, int sms, int64_t most_units, void* stream) {
   using S = TilShape<HD>;
+  // (first of all: a host thread that comes here before it has used the device has no context for the tensor map until something is launched)
+  if (a.few == 0) {
+    const int rc = ops_launch(blink_attn_begin_kernel, 1, 32, 0, stream, 0, reinterpret_cast<int*>(a.ws));
+    if (rc != BLINK_OK) return rc;
+  }
   const TilEncode encode = til_encode();
   if (!encode) return BLINK_ECUDA;
   // the layer's keys and values as {64 dims, 8 keys, slabs of dims, groups of 8 keys, keys | values}; a copy brings two groups
@@ -849,10 +854,6 @@ static int tiles_run(const AttnArgs& a, int sms, int64_t most_units, void* strea
   const size_t fixed = (size_t)S::END + 1024 + TIL_UNITS * sizeof(TilUnit);
   const OpsShared smem(fixed + (size_t)(a.n + 1) * 4, fixed + (size_t)(OPS_MAX_REQUESTS + 1) * 4);
   const int64_t grid = most_units < sms ? most_units : sms;
-  if (a.few == 0) {
-    const int rc = ops_launch(blink_attn_begin_kernel, 1, 32, 0, stream, 0, reinterpret_cast<int*>(a.ws));
-    if (rc != BLINK_OK) return rc;
-  }
   return ops_launch(blink_attn_tiles_kernel<HD>, grid, TIL_THREADS, smem, stream, 0, a, map);
 }
 

@@ -820,6 +820,45 @@ def test_tables_of_different_sizes_from_two_host_threads():
         return lambda stream, keep=(zero, one, out, table): B.lib().blink_build_tables(
             p(zero), p(zero), p(zero), n, p(one), 1, p(one), p(table), 1, rows, p(out.blocks_held), p(out.free_count), p(out.row_start), p(out.kv_len),
             p(out.positions), p(out.slot_map), p(out.status), stream)
-    calls = [caller(4096), caller(2700)]
+    calls = [caller(4096), caller(3200)]
     torch.cuda.synchronize()
-    assert in_two_threads(calls) == []
+    assert in_two_threads(calls, 20000) == []
+
+
+def test_attention_of_different_sizes_from_two_host_threads():
+    import ctypes as C
+
+    def caller(n, new):
+        c = attention_case(shape(4, 1, 128, layers=1), [5] * n, [new] * n, 0, 0, seed=n, layer=0)
+        cfg = B.make_model_cfg(c["m"])
+        kv = B.blink_kv_pool(C.sizeof(B.blink_kv_pool), 16, c["pool"].data_ptr(), c["pool"].numel() * 2)
+        out, ws = torch.zeros_like(c["q"]), torch.zeros(B.blink_window_attention_workspace(c["m"], new), dtype=torch.uint8, device="cuda")
+        p = lambda t: t.data_ptr()
+        return (lambda stream: B.lib().blink_window_attention(C.byref(cfg), C.byref(kv), 0, p(c["q"]), 512, n * new, p(c["row_start"]), p(c["kv_len"]), n, p(c["table"]),
+                                                              c["table"].shape[1], 0, 0, new, p(out), 512, p(ws), ws.numel(), stream)), c, out
+    many, few = caller(300, 9), caller(2, 9)
+    torch.cuda.synchronize()
+    assert in_two_threads([many[0], few[0]], 500) == []
+    for _, c, out in (many, few):
+        check_attention(c, out, only=[0, 1])
+
+
+@pytest.mark.parametrize("dtype,new", [("bf16", 9), ("bf16", 1), ("fp32", 9)])
+def test_attention_from_a_host_thread_that_has_not_used_the_device(dtype, new):
+    import threading
+    c = attention_case(shape(4, 2, 128, dtype), [50, 3], [new, 1], 0, 0)
+    want, out = run_attention(c), torch.zeros_like(c["q"])
+    ws = torch.zeros(B.blink_window_attention_workspace(c["m"], new), dtype=torch.uint8, device="cuda")
+    failed = []
+
+    def call():
+        try:
+            run_attention(c, out=out, workspace=ws)
+        except B.BlinkError as e:
+            failed.append(e)
+    torch.cuda.synchronize()
+    t = threading.Thread(target=call)
+    t.start()
+    t.join()
+    torch.cuda.synchronize()
+    assert failed == [] and torch.equal(out, want)
