@@ -431,7 +431,8 @@ int blink_qk_norm_rope(const blink_model_cfg* model, const blink_kv_pool* kv, in
                        int64_t qkv_stride, const float* q_gain, const float* k_gain, const int32_t* positions,
                        const int32_t* slot_map, int rows, void* q_out, int64_t q_stride, void* stream);
 
-/* Bytes of workspace that blink_window_attention needs for a model and requests of up to max_new rows (0: bad argument). */
+/* Bytes of workspace that blink_window_attention needs for a model and requests of up to max_new rows, thus for any smaller max_new too
+ * (0: bad argument). */
 uint64_t blink_window_attention_workspace(const blink_model_cfg* model, int max_new);
 
 /* Attention of the step's rows over layer `layer` of the pool, whose keys and values hold those rows already.  Row i of request r is at

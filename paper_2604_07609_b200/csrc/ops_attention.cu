@@ -747,7 +747,10 @@ extern "C" {
 
 uint64_t blink_window_attention_workspace(const blink_model_cfg* model, int max_new) {
   if (blink_weights_bytes(model) == 0 || max_new < 1) return 0;   // (no such model)
-  return blink::few_bytes(blink::few_rows_of(model, max_new), model->head_dim);
+  // (a unit of up to 24 rows of a head takes as many instructions as it needs, of more 4, and of more than 32 two: requests of up to max_new rows need the most of these)
+  const int64_t m_rows = (int64_t)max_new * (model->n_q_heads / model->n_kv_heads);
+  const int rows = model->dtype == BLINK_DTYPE_BF16 && m_rows > 24 ? 32 : blink::few_rows_of(model, max_new);
+  return blink::few_bytes(rows, model->head_dim);
 }
 
 int blink_window_attention(const blink_model_cfg* model, const blink_kv_pool* kv, int layer, const void* q, int64_t q_stride, int rows,
@@ -764,7 +767,7 @@ int blink_window_attention(const blink_model_cfg* model, const blink_kv_pool* kv
   if (rows < 1 || n_requests < 1 || table_stride < 1 || window < 0 || sinks < 0 || max_new < 1) return BLINK_EINVAL;
   if (q_stride < q_dim || out_stride < q_dim || q_stride % 8 || out_stride % 8) return BLINK_EINVAL;
   if (n_requests > OPS_MAX_REQUESTS || rows > 0x3ffffff || table_stride > 0x3ffffff || sinks > 0x3fffffff || window > 0x3fffffff) return BLINK_ETOOBIG;
-  if (!ops_aligned(workspace, 256) || workspace_bytes < blink_window_attention_workspace(model, max_new)) return BLINK_EINVAL;
+  if (!ops_aligned(workspace, 256) || workspace_bytes < few_bytes(few_rows_of(model, max_new), model->head_dim)) return BLINK_EINVAL;
   int dev = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return BLINK_ECUDA;
   a.q = q;

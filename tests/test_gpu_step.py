@@ -862,3 +862,12 @@ def test_attention_from_a_host_thread_that_has_not_used_the_device(dtype, new):
     t.join()
     torch.cuda.synchronize()
     assert failed == [] and torch.equal(out, want)
+
+
+@pytest.mark.parametrize("rep,hkv,hd,dtype", [(4, 2, 128, "bf16"), (8, 1, 64, "bf16"), (1, 2, 128, "bf16"), (4, 2, 64, "fp32")])
+def test_attention_a_workspace_for_long_requests_serves_shorter_ones(rep, hkv, hd, dtype):
+    m = shape(rep, hkv, hd, dtype)
+    ws = torch.empty(B.blink_window_attention_workspace(m, 4096), dtype=torch.uint8, device="cuda")
+    for new in (1, 2, 3, 4, 5, 6, 7, 8, 9, 13, 29, 32, 33):
+        c = attention_case(m, [40, 3, 900], [new, 1, new], 0, 0, seed=new)
+        check_attention(c, run_attention(c, workspace=ws))

@@ -98,3 +98,13 @@ def test_the_binding_refuses_host_tensors_and_wrong_shapes():
         B.blink_build_tables(i, i, i, i, i[:1], torch.zeros(2, 3, dtype=torch.int32), max_rows=4)
     with pytest.raises(ValueError, match="CUDA"):
         B.blink_verify_drafts(torch.zeros(3, 9), torch.zeros(3, dtype=torch.int32), torch.zeros(3, dtype=torch.int32), None, f, torch.zeros(3), f)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("rep", [1, 2, 4, 8])
+def test_a_workspace_for_long_requests_serves_shorter_ones(rep, hd, dtype):
+    """The size never falls as max_new grows."""
+    m = model_cfg(1, n_q_heads=rep * 2, n_kv_heads=2, head_dim=hd, dtype=dtype)
+    sizes = [B.blink_window_attention_workspace(m, k) for k in list(range(1, 80)) + [100, 1000, 4096, 1 << 24, (1 << 31) - 1]]
+    assert sizes[0] > 0 and sizes == sorted(sizes)
