@@ -183,26 +183,26 @@ __global__ void __launch_bounds__(VER_THREADS) blink_verify_rows_kernel(const __
 
 // exp((z - top) / T) in 64 bits, as 2^(n / 16) 2^(f / 16): n whole, its sixteenths from a table in shared memory (16 entries: two banks
 // each, no conflicts) and the rest into the exponent; |f| <= 1/2, by the series of exp(f ln 2 / 16) up to its fifth power (off by
-// (ln 2 / 32)^6 / 6! = 1.4e-13).  64-bit operations are what the kernels below are bound by: twelve here, one of them the conversion.
+// (ln 2 / 32)^6 / 6! = 1.4e-13).  The largest entry is taken away first: it is exactly 1 at every temperature, where the rounding of top * scale
+// alone would be many powers of two at 1e-18.  64-bit operations are what the kernels below are bound by: twelve here, one of them the conversion.
 struct VerExp {
   const double* table;   // 2^(i / 16)
   const double* series;
-  double scale, shift;   // 16 log2(e) / T, and -top times that
-  float top, below;      // entries below this are 0: (z - top) / T < -700
+  double scale, top;     // 16 log2(e) / T
+  float below;         // entries below this are 0: (z - top) / T < -700
 };
 __device__ __forceinline__ VerExp ver_exp_of(const VerifyArgs& a, const double* table, float top, float T) {
   VerExp x;
   x.table = table;
   x.series = a.series;
   x.scale = 16.0 * 1.44269504088896340736 / (double)T;
-  x.shift = -(double)top * x.scale;
-  x.top = top;
+  x.top = (double)top;
   x.below = fmaxf(__double2float_ru((double)top - 700.0 * (double)T), -3.402823466e38f);   // (rounded up: no less than -700; above -inf)
   return x;
 }
 __device__ __forceinline__ double ver_exp(const VerExp& x, float z) {
   constexpr double SHIFT = 6755399441055744.0;   // 1.5 * 2^52: adding it leaves the nearest whole number in the low bits
-  const double t = fma((double)z, x.scale, x.shift), s = t + SHIFT, f = t - (s - SHIFT);
+  const double t = ((double)z - x.top) * x.scale, s = t + SHIFT, f = t - (s - SHIFT);
   const int n = __double2loint(s);
   const double p = fma(f, fma(f, fma(f, fma(f, fma(f, x.series[4], x.series[3]), x.series[2]), x.series[1]), x.series[0]), 1.0) * x.table[n & 15];
   return z >= x.below ? __hiloint2double(__double2hiint(p) + ((n >> 4) << 20), __double2loint(p)) : 0.0;   // (no number: 0 too)

@@ -871,3 +871,28 @@ def test_attention_a_workspace_for_long_requests_serves_shorter_ones(rep, hkv, h
     for new in (1, 2, 3, 4, 5, 6, 7, 8, 9, 13, 29, 32, 33):
         c = attention_case(m, [40, 3, 900], [new, 1, new], 0, 0, seed=new)
         check_attention(c, run_attention(c, workspace=ws))
+
+
+# ---- temperatures -----------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("V", [50, 5000, 40000, 100000])
+@pytest.mark.parametrize("T", [1e-6, 1e-12, 1e-18, 1e-20, 1e-30, 1.2e-38])
+def test_verify_small_temperatures_share_a_row_among_its_largest(T, V):
+    """Largest entries that are no short binary fractions, twice in a row: half the weight each, whatever the temperature."""
+    rng = np.random.default_rng(int(-np.log10(T)) * 7 + V)
+    n = 40
+    z = (rng.normal(size=(2 * n, V)) * 2).astype(np.float32)
+    a, b = rng.permutation(V)[:2 * n].reshape(2, n) if V >= 2 * n else (np.arange(n) % 25, 25 + np.arange(n) % 25)
+    for r in range(n):
+        z[2 * r:2 * r + 2, [a[r], b[r]]] = np.float32(5 + 25 * rng.random())
+    draft = np.zeros(2 * n, np.int64)
+    draft[::2] = a
+    c = dict(z=z, V=V, start=2 * np.arange(n + 1), draft=draft, q=None, T=np.full(n, T, np.float32), ua=np.tile(np.float32([0.4, 0.0, 0.6, 0.0]), n // 2),
+             up=rng.random(n).astype(np.float32))
+    tokens, accepted = run_verify(c)
+    check_verify(c, tokens, accepted)
+    planted = z[2 * np.arange(n), a] == z.reshape(n, 2 * V).max(1)                  # (in some rows another entry came out larger)
+    odd = np.arange(n) % 2 == 1
+    assert planted.sum() > 20 and np.array_equal(accepted.cpu().numpy()[planted], 1 - odd[planted])
+    want = np.where(odd, b, np.where(c["up"] < 0.5, np.minimum(a, b), np.maximum(a, b)))   # refused: the other one; else either half
+    tokens = tokens.cpu().numpy().reshape(n, 2)
+    assert np.array_equal(np.where(odd, tokens[:, 0], tokens[:, 1])[planted], want[planted])
