@@ -155,8 +155,15 @@ __global__ void __launch_bounds__(VER_THREADS) blink_verify_rows_kernel(const __
 #pragma unroll
     for (int d = 16; d; d >>= 1) idx = min(idx, __shfl_xor_sync(0xffffffffu, idx, d));
   } else {
-    const float scale = fminf(1.4426950408889634f / T, 3e38f);
-    const float base = mine == -INFINITY ? 0.f : mine;
+    // At the ends of T's range entries are taken times a power of two, and the scale by that less: their differences, or the scale itself, would leave
+    // 32 bits.  (With entries above 1 there is no need at the lower end: what is not the largest has no weight there.)
+    const float unit = T > 0x1p100f ? 0x1p-8f : T < 0x1p-100f && fabsf(mine) < 1.f ? 0x1p64f : 1.f;
+    if (unit != 1.f) {
+#pragma unroll
+      for (int k = 0; k < VER_EACH; ++k) v[k] *= unit;
+    }
+    const float scale = fminf(1.4426950408889634f / (T * unit), 3e38f);
+    const float base = mine == -INFINITY ? 0.f : mine * unit;
     const float2 scale2 = make_float2(scale, scale), base2 = make_float2(-base, -base);
     auto lane_sum = [&]() {
       float2 s0 = make_float2(0.f, 0.f), s1 = s0;
@@ -174,7 +181,7 @@ __global__ void __launch_bounds__(VER_THREADS) blink_verify_rows_kernel(const __
       for (int k = 0; k < VER_EACH; ++k) v[k] = ver_entry(v[k]);
       s = lane_sum();
     }
-    sum = (double)s * (double)ver_ex2((mine - m) * scale);
+    sum = (double)s * (double)ver_ex2((mine * unit - m * unit) * scale);
 #pragma unroll
     for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
   }

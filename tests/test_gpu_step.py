@@ -896,3 +896,33 @@ def test_verify_small_temperatures_share_a_row_among_its_largest(T, V):
     want = np.where(odd, b, np.where(c["up"] < 0.5, np.minimum(a, b), np.maximum(a, b)))   # refused: the other one; else either half
     tokens = tokens.cpu().numpy().reshape(n, 2)
     assert np.array_equal(np.where(odd, tokens[:, 0], tokens[:, 1])[planted], want[planted])
+
+
+def test_verify_the_ends_of_the_temperatures_range_in_the_acceptance():
+    """Differences of entries beyond 32 bits at temperatures as large, and entries a few smallest numbers apart at temperatures as small: a draft is
+    accepted with the probability that these give it."""
+    rows, T = [], []
+    for V in (60, 5000):
+        for t, lo, hi in ((3.4e38, -3.4e38, 3.4e38), (1e37, 3.35e38, 3.4e38), (2e30, -1e30, 3e30), (1e-45, -3e-45, 0.0), (3e-39, 0.0, 5e-39), (1e-40, -2e-40, 1e-40),
+                          (1e-38, -0.5, 0.5), (1e-38, -3e38, 0.9), (1e-44, 1.5, 1.5)):
+            z = np.full(V, lo, np.float32)
+            z[V // 3::7] = hi
+            z[V // 2] = -np.inf
+            rows += [z, z]
+            T.append(t)
+    n = len(T)
+    for V in (60, 5000):
+        sel = [i for i in range(n) if len(rows[2 * i]) == V]
+        for high in (0, 1):                    # the draft is one of the low, or of the high entries
+            z = np.stack([r for i in sel for r in rows[2 * i:2 * i + 2]])
+            x = V // 3 + (0 if high else 1)
+            T32 = np.array([T[i] for i in sel], np.float32)
+            p = np.array([O.target_probs(z[2 * i], T32[i])[0][x] for i in range(len(sel))])
+            for f in (0.97, 1.03):
+                ua = np.zeros(2 * len(sel), np.float32)
+                ua[::2] = p * f
+                c = dict(z=z, V=V, start=2 * np.arange(len(sel) + 1), draft=np.full(2 * len(sel), x), q=None, T=T32, ua=ua, up=np.full(len(sel), 0.37, np.float32))
+                tokens, accepted = run_verify(c)
+                check_verify(c, tokens, accepted)
+                some = p > 1e-30
+                assert some.any() and np.array_equal(accepted.cpu().numpy()[some], np.full(some.sum(), int(f < 1)))
