@@ -41,11 +41,12 @@ inline int ops_pool(const blink_model_cfg* m, const blink_kv_pool* kv, int layer
   return BLINK_OK;
 }
 
-// An error that a launch left behind is taken away, so that no later call reports it as its own.
+// A launch reports its own error.  What it left behind of it is taken away, so that no later call reports it; what another call of the library
+// left (memory that was not to be had) is none of this one's.
 inline int ops_launched(cudaError_t e) {
-  if (e == cudaSuccess) e = cudaGetLastError();
-  else (void)cudaGetLastError();
-  return e == cudaSuccess ? BLINK_OK : BLINK_ECUDA;
+  if (e == cudaSuccess) return BLINK_OK;
+  (void)cudaGetLastError();
+  return BLINK_ECUDA;
 }
 
 // Dynamic shared memory of a launch, and the most that the same kernel is ever launched with.  The limit of a kernel is the device's, whoever calls: were

@@ -926,3 +926,24 @@ def test_verify_the_ends_of_the_temperatures_range_in_the_acceptance():
                 check_verify(c, tokens, accepted)
                 some = p > 1e-30
                 assert some.any() and np.array_equal(accepted.cpu().numpy()[some], np.full(some.sum(), int(f < 1)))
+
+
+def test_an_error_of_another_call_is_not_the_operators():
+    """A loop that is refused for want of memory leaves an error behind in the library; the operators' launches succeed all the same, all
+    of a call's kernels."""
+    import ctypes as C
+    m = shape(4, 2, 128)
+    cfg = B.make_model_cfg(m)
+    sched = B.blink_sched_cfg(size=C.sizeof(B.blink_sched_cfg), max_batch=8, prefill_chunk_tokens=64, n_slots=1024, max_prompt=1 << 30, max_new=16, control_only=1)
+    kv = B.blink_kv_pool(C.sizeof(B.blink_kv_pool), 16, None, 64 * B.kv_bytes_per_block(m))
+    c = attention_case(m, [30000, 3], [1, 1], 0, 0)                       # two kernels
+    v = verify_case(np.random.default_rng(0), [3] * 14, 500, True, [0.9] * 14)   # three
+    want, wv = run_attention(c), run_verify(v)
+
+    def refused():
+        ctx = C.c_void_p()
+        assert B.lib().blink_create(C.byref(cfg), C.byref(sched), C.byref(kv), C.byref(ctx)) == B.BLINK_ENOMEM    # 4 TB of prompts
+    refused()
+    assert torch.equal(run_attention(c), want)
+    refused()
+    assert all(torch.equal(x, y) for x, y in zip(run_verify(v), wv))
