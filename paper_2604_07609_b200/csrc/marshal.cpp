@@ -113,24 +113,38 @@ bool model_of(Args& a, blink_model_cfg* m) {
       a.ok = false;
       break;
     }
-    if (i < 9) *to[i] = (int32_t)PyLong_AsLong(v);
-    else if (i == 9) m->rope_theta = (float)PyFloat_AsDouble(v);
+    if (i < 9) {
+      const long n = PyLong_AsLong(v);
+      *to[i] = (int32_t)n;
+      if (!PyErr_Occurred() && n != *to[i]) a.fail(PyExc_ValueError, "%s: %ld is no 32-bit number", names[i], n);
+    } else if (i == 9) m->rope_theta = (float)PyFloat_AsDouble(v);
     else if (i == 10) m->rms_eps = (float)PyFloat_AsDouble(v);
-    else m->dtype = PyUnicode_Check(v) && PyUnicode_CompareWithASCIIString(v, "bf16") == 0 ? BLINK_DTYPE_BF16 : BLINK_DTYPE_FP32;
+    else if (PyUnicode_Check(v) && PyUnicode_CompareWithASCIIString(v, "bf16") == 0) m->dtype = BLINK_DTYPE_BF16;
+    else if (PyUnicode_Check(v) && PyUnicode_CompareWithASCIIString(v, "fp32") == 0) m->dtype = BLINK_DTYPE_FP32;
+    else a.fail(PyExc_ValueError, "dtype: %R, neither 'bf16' nor 'fp32'", v);
     Py_DECREF(v);
     if (PyErr_Occurred()) a.ok = false;
   }
   return a.ok;
 }
 
-blink_kv_pool pool_of(Args& a) {
+at::ScalarType type_of(const blink_model_cfg& m) { return m.dtype == BLINK_DTYPE_BF16 ? at::kBFloat16 : at::kFloat; }
+
+// The pool as it was carved out: elements of the model's type, or bytes.  One that says its shape has the model's.
+blink_kv_pool pool_of(Args& a, const blink_model_cfg& m) {
   const at::Tensor* t = a.tensor("kv_pool");
   if (!a.ok) return {};
   a.need(t->is_contiguous(), "kv_pool: contiguous");
+  if (t->scalar_type() != type_of(m) && t->scalar_type() != at::kByte)
+    a.fail(PyExc_ValueError, "kv_pool: of %s, neither the model's %s nor bytes", c10::toString(t->scalar_type()), c10::toString(type_of(m)));
+  if (t->dim() == 6 && t->scalar_type() != at::kByte) {
+    const int64_t want[6] = {m.n_layers, 2, t->size(2), m.n_kv_heads, 16, m.head_dim};
+    for (int i = 0; i < 6; ++i)
+      if (t->size(i) != want[i]) a.fail(PyExc_ValueError, "kv_pool: [layers][2][blocks][kv heads][16][head_dim] of the model has %lld elements in dimension %d, not %lld",
+                                        (long long)want[i], i, (long long)t->size(i));
+  }
   return {sizeof(blink_kv_pool), 16, t->data_ptr(), (uint64_t)t->nbytes()};
 }
-
-at::ScalarType type_of(const blink_model_cfg& m) { return m.dtype == BLINK_DTYPE_BF16 ? at::kBFloat16 : at::kFloat; }
 
 at::Tensor make(at::IntArrayRef size, at::ScalarType type, const Args& a) {
   return at::empty(size, at::TensorOptions().dtype(type).device(at::Device(at::kCUDA, a.device)));
@@ -167,7 +181,7 @@ PyObject* qk_norm_rope(PyObject*, PyObject* const* arg, Py_ssize_t nargs) {
   Args a(arg, nargs, 9);
   blink_model_cfg m;
   if (!model_of(a, &m)) return nullptr;
-  const blink_kv_pool kv = pool_of(a);
+  const blink_kv_pool kv = pool_of(a, m);
   const long layer = a.integer();
   const int64_t q_dim = (int64_t)m.n_q_heads * m.head_dim;
   int64_t stride = 0, out_stride = 0;
@@ -192,7 +206,7 @@ PyObject* window_attention(PyObject*, PyObject* const* arg, Py_ssize_t nargs) {
   Args a(arg, nargs, 12);
   blink_model_cfg m;
   if (!model_of(a, &m)) return nullptr;
-  const blink_kv_pool kv = pool_of(a);
+  const blink_kv_pool kv = pool_of(a, m);
   const long layer = a.integer();
   const int64_t q_dim = (int64_t)m.n_q_heads * m.head_dim;
   int64_t stride = 0, out_stride = 0;

@@ -947,3 +947,18 @@ def test_an_error_of_another_call_is_not_the_operators():
     assert torch.equal(run_attention(c), want)
     refused()
     assert all(torch.equal(x, y) for x, y in zip(run_verify(v), wv))
+
+
+def test_the_binding_takes_a_pool_of_the_models_type_and_shape_or_bytes():
+    for dtype, other in (("bf16", torch.float32), ("bf16", torch.float16), ("fp32", torch.bfloat16)):
+        m = shape(4, 2, 128, dtype)
+        c = attention_case(m, [20, 3], [1, 2], 0, 0)
+        want, pool = run_attention(c), c["pool"]
+        assert torch.equal(run_attention(c | {"pool": pool.view(torch.uint8)}), want) and torch.equal(run_attention(c | {"pool": pool.view(-1).view(torch.uint8)}), want) and torch.equal(run_attention(c | {"pool": pool.view(-1)}), want)
+        x = torch.zeros(3, m.qkv_dim, dtype=DT[dtype], device="cuda")
+        for bad in (pool.to(other), pool.view(-1).to(other), pool[:1], pool[:, :, :, :1].contiguous(), pool[..., :64].contiguous(), pool.transpose(3, 4).contiguous(),
+                    pool.transpose(0, 2)):
+            with pytest.raises(ValueError, match="kv_pool"):
+                run_attention(c | {"pool": bad})
+            with pytest.raises(ValueError, match="kv_pool"):
+                B.blink_qk_norm_rope(m, bad, 0, x, None, None, ints([0, 1, 2]), ints([0, 1, 2]))

@@ -108,3 +108,17 @@ def test_a_workspace_for_long_requests_serves_shorter_ones(rep, hd, dtype):
     m = model_cfg(1, n_q_heads=rep * 2, n_kv_heads=2, head_dim=hd, dtype=dtype)
     sizes = [B.blink_window_attention_workspace(m, k) for k in list(range(1, 80)) + [100, 1000, 4096, 1 << 24, (1 << 31) - 1]]
     assert sizes[0] > 0 and sizes == sorted(sizes)
+
+
+@pytest.mark.parametrize("kw,what", [(dict(dtype="fp16"), "dtype"), (dict(dtype="float32"), "dtype"), (dict(dtype=torch.float32), "dtype"),
+                                     (dict(n_layers=(1 << 32) + 2), "n_layers"), (dict(vocab=-(1 << 40)), "vocab"), (dict(head_dim=1 << 31), "head_dim")])
+def test_the_binding_refuses_models_that_it_would_have_to_guess(kw, what):
+    m = model_cfg(1, dtype="fp32")
+    q, i = torch.zeros(2, m.q_dim), torch.zeros(2, dtype=torch.int32)
+    bad = m.with_(**kw)
+    with pytest.raises(ValueError, match=what):
+        B._marshal().qk_norm_rope(bad, q, 0, q, None, None, i, i, q)
+    with pytest.raises(ValueError, match=what):
+        B._marshal().window_attention(bad, q, 0, q, i, i[:1], torch.zeros(1, 2, dtype=torch.int32), 0, 0, 1, q, None)
+    with pytest.raises(ValueError, match="CUDA"):      # the model itself is taken
+        B._marshal().qk_norm_rope(m, q, 0, q, None, None, i, i, q)
