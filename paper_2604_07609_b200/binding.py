@@ -272,6 +272,9 @@ def _marshal():
         except ImportError as e:
             raise RuntimeError("_marshal.so is missing or was built for another torch: run `python -m paper_2604_07609_b200.build` "
                                f"(there is no fallback): {e}") from e
+        from .build import marshal_for
+        if module.built != f"built for {marshal_for()}.":
+            raise RuntimeError(f"_marshal.so was {module.built[:-1]}, this is {marshal_for()}: run `python -m paper_2604_07609_b200.build`")
         _marshal_module = module
     return _marshal_module
 

@@ -1,6 +1,9 @@
-"""Build libblink.so (CUDA kernels + C ABI) in-tree for sm_100a with nvcc, and beside it _marshal.so, which hands torch tensors to it."""
+"""Build libblink.so (CUDA kernels + C ABI) in-tree for sm_100a with nvcc, and beside it, where there is torch, _marshal.so, which hands torch
+tensors to it."""
 from __future__ import annotations
 
+import importlib.metadata
+import importlib.util
 import os
 import subprocess
 import sys
@@ -24,15 +27,23 @@ def sources():
     return out
 
 
+def marshal_for() -> str:
+    """What _marshal.so is built for: this torch and this Python.  It says so in itself."""
+    return f"torch {importlib.metadata.version('torch')}, {sysconfig.get_config_var('SOABI')}"
+
+
 def build_marshal(force: bool = False) -> str:
     """The operators' argument marshalling, against torch's headers (g++; no device code)."""
     src = os.path.join(CSRC, "marshal.cpp")
     if not force and os.path.exists(MARSHAL) and os.path.getmtime(MARSHAL) >= _newest([src, os.path.join(os.path.dirname(HERE), "include", "blink.h")]):
-        return MARSHAL
+        with open(MARSHAL, "rb") as f:
+            if f"built for {marshal_for()}.".encode() in f.read():
+                return MARSHAL
     import torch
     home = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           f'-DBLINK_BUILT_FOR="{marshal_for()}"']
     cmd += ["-isystem" + d for d in (os.path.join(home, "include"), os.path.join(cuda, "include"), sysconfig.get_paths()["include"])]
     cmd += [src, "-o", MARSHAL, "-L" + HERE, "-l:libblink.so", "-Wl,-rpath,$ORIGIN", "-L" + os.path.join(home, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu",
             "-ltorch_python"]
@@ -45,7 +56,10 @@ def build_marshal(force: bool = False) -> str:
 
 def build(force: bool = False, verbose: bool = False) -> str:
     lib = build_library(force, verbose)
-    build_marshal(force)
+    if importlib.util.find_spec("torch"):
+        build_marshal(force)
+    else:   # the library, and all of it but the operators' calls with tensors, does without
+        sys.stderr.write("no torch: _marshal.so is not built\n")
     return lib
 
 

@@ -277,4 +277,11 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Argument marshalling o
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__marshal() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__marshal() {
+  PyObject* m = PyModule_Create(&module);
+  if (m && PyModule_AddStringConstant(m, "built", "built for " BLINK_BUILT_FOR ".") != 0) {
+    Py_DECREF(m);
+    return nullptr;
+  }
+  return m;
+}
