@@ -320,7 +320,7 @@ def blink_qk_norm_rope(m, kv_pool, layer: int, qkv, q_gain, k_gain, positions, s
     """Norms of queries and keys per head (gains fp32 [head_dim], or None), rotation, new keys and values into the pool's layer.
     qkv [rows][(Hq + 2 Hkv) * hd] of the model dtype, or fp32.  Returns the queries, [rows][Hq * hd] of the model dtype."""
     if out is None:
-        out = qkv.new_empty(qkv.shape[0], m.n_q_heads * m.head_dim, dtype=_torch_dtype(m))
+        out = qkv.new_zeros(qkv.shape[0], m.n_q_heads * m.head_dim, dtype=_torch_dtype(m))   # (rows with a negative position are not written)
     rc = (_marshal_module or _marshal()).qk_norm_rope(m, kv_pool, layer, qkv, q_gain, k_gain, positions, slot_map, out)
     if rc != BLINK_OK:
         raise BlinkError(rc, "blink_qk_norm_rope")
@@ -337,7 +337,7 @@ def blink_window_attention(m, kv_pool, layer: int, q, row_start, kv_len, block_t
     `window` of them (0: all) and the first `sinks`.  max_new: rows of the longest request.  workspace: bytes on the device
     (blink_window_attention_workspace), one is taken from torch when None."""
     if out is None:
-        out = q.new_empty(q.shape)
+        out = q.new_zeros(q.shape)   # (rows that belong to nobody are not written)
     rc = (_marshal_module or _marshal()).window_attention(m, kv_pool, layer, q, row_start, kv_len, block_table, window, sinks, max_new, out, workspace)
     if rc != BLINK_OK:
         raise BlinkError(rc, "blink_window_attention")
@@ -352,12 +352,14 @@ def blink_verify_drafts(logits, row_start, draft_tokens, draft_probs, temperatur
                         workspace=None):
     """Drafted tokens against the target's logits [rows][vocab] (fp32), from given random numbers: u_accept [rows], u_pick [n], fp32.
     draft_probs: fp32 [rows][vocab], or None when drafts are certain.  temperature fp32 [n], 0: greedy.  Returns
-    (tokens [rows]: accepted drafts, the token drawn, -1; number of accepted drafts [n])."""
-    if out_tokens is None:
+    (tokens [rows]: accepted drafts, the token drawn, -1; number of accepted drafts [n]); rows that belong to nobody are -1 when
+    out_tokens is None."""
+    new = out_tokens is None
+    if new:
         out_tokens = draft_tokens.new_empty(draft_tokens.shape)
     if n_accepted is None:
         n_accepted = draft_tokens.new_empty(temperature.shape)
-    rc = (_marshal_module or _marshal()).verify_drafts(logits, row_start, draft_tokens, draft_probs, temperature, u_accept, u_pick, out_tokens, n_accepted, workspace)
+    rc = (_marshal_module or _marshal()).verify_drafts(logits, row_start, draft_tokens, draft_probs, temperature, u_accept, u_pick, out_tokens, n_accepted, workspace, new)
     if rc != BLINK_OK:
         raise BlinkError(rc, "blink_verify_drafts")
     return out_tokens, n_accepted

@@ -35,7 +35,7 @@ def marshal_for() -> str:
 def build_marshal(force: bool = False) -> str:
     """The operators' argument marshalling, against torch's headers (g++; no device code)."""
     src = os.path.join(CSRC, "marshal.cpp")
-    if not force and os.path.exists(MARSHAL) and os.path.getmtime(MARSHAL) >= _newest([src, os.path.join(os.path.dirname(HERE), "include", "blink.h")]):
+    if not force and os.path.exists(MARSHAL) and os.path.getmtime(MARSHAL) >= _newest([src, os.path.join(CSRC, "ops.h"), os.path.join(os.path.dirname(HERE), "include", "blink.h")]):
         with open(MARSHAL, "rb") as f:
             if f"built for {marshal_for()}.".encode() in f.read():
                 return MARSHAL

@@ -7,6 +7,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/blink.h"
+#include "ops.h"
 
 namespace {
 
@@ -232,9 +233,10 @@ PyObject* window_attention(PyObject*, PyObject* const* arg, Py_ssize_t nargs) {
   });
 }
 
-// logits, row_start, draft_tokens, draft_probs or None, temperature, u_accept, u_pick, out_tokens, n_accepted, workspace or None -> error code
+// logits, row_start, draft_tokens, draft_probs or None, temperature, u_accept, u_pick, out_tokens, n_accepted, workspace or None, 1 when the tokens'
+// memory is new -> error code
 PyObject* verify_drafts(PyObject*, PyObject* const* arg, Py_ssize_t nargs) {
-  Args a(arg, nargs, 10);
+  Args a(arg, nargs, 11);
   int64_t stride = 0, probs_stride = 0;
   const at::Tensor* z = a.matrix("logits", -1, -1, at::kFloat, &stride);
   const int64_t rows = a.ok ? z->size(0) : 0, vocab = a.ok ? z->size(1) : 0;
@@ -243,6 +245,7 @@ PyObject* verify_drafts(PyObject*, PyObject* const* arg, Py_ssize_t nargs) {
   const int64_t n = a.ok ? row_start->numel() - 1 : 0;
   const at::Tensor *T = a.floats("temperature", n), *ua = a.floats("u_accept", rows), *up = a.floats("u_pick", n);
   const at::Tensor *tokens = a.ints("out_tokens", rows), *accepted = a.ints("n_accepted", n), *given = a.tensor("workspace", true);
+  const bool clear = a.integer() != 0;
   if (a.ok && given) a.need(given->is_contiguous(), "workspace: contiguous");
   if (a.ok) a.need(std::max({n, rows, vocab}) <= 0x7fffffff, "sizes beyond 31 bits");
   if (!a.ok) return nullptr;
@@ -252,8 +255,8 @@ PyObject* verify_drafts(PyObject*, PyObject* const* arg, Py_ssize_t nargs) {
     given = &mine;
   }
   return call(a, [&](void* stream) {
-    return blink_verify_drafts(in<float>(z), stride, (int)rows, (int)vocab, in<int32_t>(row_start), (int)n, in<int32_t>(draft), in<float>(probs), probs_stride, in<float>(T),
-                               in<float>(ua), in<float>(up), out<int32_t>(tokens), out<int32_t>(accepted), out<void>(given), given->nbytes(), stream);
+    return blink::verify_drafts(in<float>(z), stride, (int)rows, (int)vocab, in<int32_t>(row_start), (int)n, in<int32_t>(draft), in<float>(probs), probs_stride, in<float>(T),
+                                in<float>(ua), in<float>(up), out<int32_t>(tokens), out<int32_t>(accepted), out<void>(given), given->nbytes(), clear, stream);
   });
 }
 

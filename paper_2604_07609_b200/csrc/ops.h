@@ -10,6 +10,11 @@ namespace blink {
 constexpr int OPS_BLOCK = 16;            // tokens of a KV block
 constexpr int OPS_MAX_REQUESTS = 4096;   // their prefix sums are kept in shared memory
 
+// blink_verify_drafts; with `clear` rows that belong to nobody get the token -1 (for tokens in memory that nobody has written yet).
+int verify_drafts(const float* logits, int64_t logits_stride, int rows, int vocab, const int32_t* row_start, int n_requests, const int32_t* draft_tokens,
+                  const float* draft_probs, int64_t probs_stride, const float* temperature, const float* u_accept, const float* u_pick, int32_t* out_tokens,
+                  int32_t* n_accepted, void* workspace, uint64_t workspace_bytes, bool clear, void* stream);
+
 // One layer of a paged KV pool, [2][n_blocks][Hkv][16][hd] each, as the kernels address it.
 struct OpsPool {
   char* k;           // block 0 of the layer's keys

@@ -53,6 +53,7 @@ struct VerifyArgs {
   VerChoice* choice;     // [n]
   int n, rows, vocab, chunks, groups;
   bool vec, probs_vec;   // rows on 16-byte boundaries
+  bool clear;            // rows that belong to nobody get the token -1
   double sixteenths[16]; // 2^(i / 16)
   double series[5];      // (ln 2 / 16)^i / i!, i = 1 .. 5 (as operands from the constant bank: written out they take two moves each at every use)
 };
@@ -133,6 +134,7 @@ __global__ void __launch_bounds__(VER_THREADS) blink_verify_rows_kernel(const __
   }
   __syncthreads();
   const int req = s_req;
+  if (req < 0 && a.clear && chunk == 0 && lane == 0) a.tokens[row] = -1;
   if (req < 0 || chunk >= a.chunks) return;   // (whole warps) a row behind the last request
   const float T = s_T;
   float m0 = -INFINITY, m1 = -INFINITY;   // (the larger of a number and none is the number)
@@ -562,20 +564,9 @@ static VerifySpace verify_space(int64_t rows, int64_t n, int64_t vocab) {
   return s;
 }
 
-}  // namespace blink
-
-extern "C" {
-
-uint64_t blink_verify_workspace(int rows, int n_requests, int vocab) {
-  if (rows < 1 || n_requests < 1 || vocab < 2) return 0;
-  return blink::verify_space(rows, n_requests, vocab).end;
-}
-
-int blink_verify_drafts(const float* logits, int64_t logits_stride, int rows, int vocab, const int32_t* row_start, int n_requests,
-                        const int32_t* draft_tokens, const float* draft_probs, int64_t probs_stride, const float* temperature,
-                        const float* u_accept, const float* u_pick, int32_t* out_tokens, int32_t* n_accepted, void* workspace,
-                        uint64_t workspace_bytes, void* stream) {
-  using namespace blink;
+int verify_drafts(const float* logits, int64_t logits_stride, int rows, int vocab, const int32_t* row_start, int n_requests, const int32_t* draft_tokens,
+                  const float* draft_probs, int64_t probs_stride, const float* temperature, const float* u_accept, const float* u_pick, int32_t* out_tokens,
+                  int32_t* n_accepted, void* workspace, uint64_t workspace_bytes, bool clear, void* stream) {
   const void* must[] = {logits, row_start, draft_tokens, temperature, u_accept, u_pick, out_tokens, n_accepted};
   for (const void* p : must)
     if (!ops_aligned(p, 4)) return BLINK_EINVAL;
@@ -586,6 +577,7 @@ int blink_verify_drafts(const float* logits, int64_t logits_stride, int rows, in
   if (!ops_aligned(workspace, 16) || workspace_bytes < space.end) return BLINK_EINVAL;
   char* ws = static_cast<char*>(workspace);
   VerifyArgs a;
+  a.clear = clear;
   a.logits = logits;
   a.probs = draft_probs;
   a.logits_stride = logits_stride;
@@ -618,6 +610,23 @@ int blink_verify_drafts(const float* logits, int64_t logits_stride, int rows, in
   if (vocab <= 32768) return choose ? verify_draw<4, false>(a, stream) : verify_draw<4, true>(a, stream);
   if (vocab <= 65536) return choose ? verify_draw<8, false>(a, stream) : verify_draw<8, true>(a, stream);
   return choose ? verify_draw<16, false>(a, stream) : verify_draw<16, true>(a, stream);
+}
+
+}  // namespace blink
+
+extern "C" {
+
+uint64_t blink_verify_workspace(int rows, int n_requests, int vocab) {
+  if (rows < 1 || n_requests < 1 || vocab < 2) return 0;
+  return blink::verify_space(rows, n_requests, vocab).end;
+}
+
+int blink_verify_drafts(const float* logits, int64_t logits_stride, int rows, int vocab, const int32_t* row_start, int n_requests,
+                        const int32_t* draft_tokens, const float* draft_probs, int64_t probs_stride, const float* temperature,
+                        const float* u_accept, const float* u_pick, int32_t* out_tokens, int32_t* n_accepted, void* workspace,
+                        uint64_t workspace_bytes, void* stream) {
+  return blink::verify_drafts(logits, logits_stride, rows, vocab, row_start, n_requests, draft_tokens, draft_probs, probs_stride, temperature, u_accept, u_pick,
+                              out_tokens, n_accepted, workspace, workspace_bytes, false, stream);
 }
 
 }  // extern "C"

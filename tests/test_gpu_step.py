@@ -962,3 +962,32 @@ def test_the_binding_takes_a_pool_of_the_models_type_and_shape_or_bytes():
                 run_attention(c | {"pool": bad})
             with pytest.raises(ValueError, match="kv_pool"):
                 B.blink_qk_norm_rope(m, bad, 0, x, None, None, ints([0, 1, 2]), ints([0, 1, 2]))
+
+
+def test_rows_that_belong_to_nobody_are_defined_in_outputs_that_the_binding_makes():
+    """Memory that was used before, as a captured step with spare rows would read it on: zeros, and tokens of -1."""
+    def dirty(*shape_of, dtype):
+        t = [torch.full(shape_of, 7 if dtype == torch.int32 else float("nan"), dtype=dtype, device="cuda") for _ in range(4)]
+        torch.cuda.synchronize()
+        del t
+    for dtype in ("bf16", "fp32"):
+        m = shape(4, 2, 128, dtype)
+        c = attention_case(m, [50, 3], [3, 40], 0, 0, pad=9)
+        dirty(*c["q"].shape, dtype=DT[dtype])
+        out = run_attention(c)
+        check_attention(c, out)
+        assert (out[43:] == 0).all()
+        x = torch.randn(30, m.qkv_dim, device="cuda").to(DT[dtype])
+        dirty(30, m.q_dim, dtype=DT[dtype])
+        q = B.blink_qk_norm_rope(m, new_pool(m, 3), 0, x, None, None, ints([1] * 20 + [-1] * 10), ints([-1] * 30))
+        assert (q[20:] == 0).all() and (q[:20] != 0).any()
+    for n in (3, 20):                       # two kernels, three
+        v = verify_case(np.random.default_rng(n), [2] * n, 3000, True, [0.9] * n)
+        v["start"] = v["start"][:-1]
+        v["T"], v["up"] = v["T"][:-1], v["up"][:-1]
+        dirty(3 * n, dtype=torch.int32)
+        tokens, accepted = run_verify(v)
+        check_verify(v, tokens, accepted)
+        assert (tokens[3 * n - 3:] == -1).all()
+        kept = torch.full((3 * n,), 77, dtype=torch.int32, device="cuda")
+        assert (run_verify(v, out_tokens=kept)[0][3 * n - 3:] == 77).all() and torch.equal(kept[:3 * n - 3], tokens[:3 * n - 3])
