@@ -211,7 +211,7 @@ __device__ __forceinline__ VerExp ver_exp_of(const VerifyArgs& a, const double* 
 }
 __device__ __forceinline__ double ver_exp(const VerExp& x, float z) {
   constexpr double SHIFT = 6755399441055744.0;   // 1.5 * 2^52: adding it leaves the nearest whole number in the low bits
-  const double t = ((double)z - x.top) * x.scale, s = t + SHIFT, f = t - (s - SHIFT);
+  const double d = (double)z - x.top, s = fma(d, x.scale, SHIFT), f = fma(d, x.scale, -(s - SHIFT));
   const int n = __double2loint(s);
   const double p = fma(f, fma(f, fma(f, fma(f, fma(f, x.series[4], x.series[3]), x.series[2]), x.series[1]), x.series[0]), 1.0) * x.table[n & 15];
   return z >= x.below ? __hiloint2double(__double2hiint(p) + ((n >> 4) << 20), __double2loint(p)) : 0.0;   // (no number: 0 too)
