@@ -444,8 +444,8 @@ uint64_t blink_window_attention_workspace(const blink_model_cfg* model, int max_
  * the request sees it (the rest of the last block, keys before the window) does not matter; an infinity or NaN that one of
  * its rows sees may reach all of its rows.  A kv_len beyond the table's row counts as the row's end.  max_new: rows of the longest
  * request, for the choice of kernels; longer ones are served too.  bf16 rounds probabilities to bf16 for their product with the values; all
- * else is in 32 bits.  The workspace's first word is 0 after the call, or BLINK_ETIMEDOUT when a wait inside the kernels ran out (outputs are then
- * incomplete).  Pointers 16-byte (workspace 256-byte) aligned, strides multiples of 8. */
+ * else is in 32 bits.  The workspace's first word is 0 after the call, or BLINK_ETIMEDOUT when a wait inside the kernels ran out: rows
+ * that are not done are then NaN, and others may be.  Pointers 16-byte (workspace 256-byte) aligned, strides multiples of 8. */
 int blink_window_attention(const blink_model_cfg* model, const blink_kv_pool* kv, int layer, const void* q, int64_t q_stride, int rows,
                            const int32_t* row_start, const int32_t* kv_len, int n_requests, const int32_t* block_table, int table_stride,
                            int window, int sinks, int max_new, void* out, int64_t out_stride, void* workspace, uint64_t workspace_bytes,

@@ -335,7 +335,8 @@ def blink_window_attention(m, kv_pool, layer: int, q, row_start, kv_len, block_t
                            workspace=None):
     """Attention of the step's rows q [rows][Hq * hd] over a layer of the paged pool: a row sees the keys up to its own position, the last
     `window` of them (0: all) and the first `sinks`.  max_new: rows of the longest request.  workspace: bytes on the device
-    (blink_window_attention_workspace), one is taken from torch when None."""
+    (blink_window_attention_workspace), one is taken from torch when None.  Its first word is BLINK_OK after the call, or BLINK_ETIMEDOUT when
+    a wait inside the kernels ran out; rows that are not done are then NaN."""
     if out is None:
         out = q.new_zeros(q.shape)   # (rows that belong to nobody are not written)
     rc = (_marshal_module or _marshal()).window_attention(m, kv_pool, layer, q, row_start, kv_len, block_table, window, sinks, max_new, out, workspace)

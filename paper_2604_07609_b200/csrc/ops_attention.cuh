@@ -50,7 +50,7 @@ __device__ __forceinline__ bool attn_sees(const AttnArgs& a, int key, int pos) {
   return key <= pos && (a.window == 0 || key > pos - a.window || key < a.sinks);
 }
 
-// The workspace begins with a word that is 0, or BLINK_ETIMEDOUT when a wait inside the kernels ran out.
+// The workspace begins with a word that is 0, or BLINK_ETIMEDOUT when a wait inside the kernels ran out (rows that are not done are then NaN).
 constexpr size_t ATTN_STATUS_BYTES = 256;
 // Requests of more than a.few rows on tcgen05 (ops_attn_tiles.cu); the others are in the stream before it.
 int attn_tiles(const AttnArgs& a, int sms, void* stream);

@@ -57,7 +57,7 @@ struct TilShared {
   uint64_t x_full, x_done;   // a unit that the streams share: stream 1's results are there; have been read
   float2 other[128];         // maxima and sums of stream 1's rows then
   uint32_t tmem;
-  int dead;
+  int dead, first;
   unsigned long long warp_sum[TIL_WARPS];
   int weight[TIL_SORTED], rows[TIL_SORTED];    // of requests: blocks that their last unit sees; rows (by place)
   uint16_t order[TIL_SORTED];                  // request of a place
@@ -81,8 +81,8 @@ __device__ __forceinline__ bool til_try(uint64_t* bar, uint32_t parity) {
                : "memory");
   return ok != 0;
 }
-// A whole warp waits, with one answer for all lanes; bounded.  Whoever runs out of time says so, and everybody gives up.
-static __device__ __noinline__ bool til_wait_slow(uint64_t* bar, uint32_t parity, int* dead, int* status) {
+// A whole warp waits, with one answer for all lanes; bounded.  Whoever runs out of time says so, and everybody gives up (see til_give_up).
+static __device__ __noinline__ bool til_wait_slow(uint64_t* bar, uint32_t parity, int* dead) {
   const long long t0 = clock64();
   unsigned spins = 0;
   while (!__all_sync(0xffffffffu, til_try(bar, parity))) {
@@ -90,7 +90,6 @@ static __device__ __noinline__ bool til_wait_slow(uint64_t* bar, uint32_t parity
       bool stop = *(volatile int*)dead != 0;
       if (!stop && clock64() - t0 > TIL_WAIT_CYCLES) {
         *(volatile int*)dead = 1;
-        *(volatile int*)status = BLINK_ETIMEDOUT;
         stop = true;
       }
       if (__any_sync(0xffffffffu, stop)) return false;
@@ -283,6 +282,21 @@ struct alignas(16) TilUnit {
 };
 constexpr int TIL_UNITS = 8;   // records of a CTA's units, used in turn: one is written again when all warps have read it
 
+// By all threads of a CTA in which a wait has run out, the first of the call: the status, and no number in every row that the call has here.  Units that are
+// not done stay so, and cannot be taken for results where nobody reads the status; what other CTAs store from here on is right.
+static __device__ __noinline__ void til_give_up(const AttnArgs& a, int* first) {
+  if (threadIdx.x == 0) *first = atomicExch(reinterpret_cast<int*>(a.ws), BLINK_ETIMEDOUT) == BLINK_OK;
+  __syncthreads();
+  if (!*first) return;
+  const int pieces = a.pool.Hq * a.pool.hd / 8;   // 16 bytes each, of a row
+  for (int r = 0; r < a.n; ++r) {
+    const AttnReq q = attn_req(a, a.row_start[r], a.row_start[r + 1], a.kv_len[r]);
+    if (q.rows <= a.few) continue;
+    for (long long i = threadIdx.x; i < (long long)q.rows * pieces; i += TIL_THREADS)
+      reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.out) + (q.start + i / pieces) * a.out_stride)[i % pieces] = make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);
+  }
+}
+
 template <int HD>
 __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap map) {
   using S = TilShape<HD>;
@@ -395,7 +409,7 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
 
   bool ok = true;   // false once a wait has run out
   auto wait = [&](uint64_t* bar, uint32_t parity) {
-    if (ok && !__all_sync(0xffffffffu, til_try(bar, parity))) ok = til_wait_slow(bar, parity, &sh.dead, status);
+    if (ok && !__all_sync(0xffffffffu, til_try(bar, parity))) ok = til_wait_slow(bar, parity, &sh.dead);
     return ok;
   };
   auto make_unit = [&](int u) {
@@ -602,7 +616,7 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
           f0 = g0 * inv;
           f1 = g1 * inv;
         }
-        const bool store = mine && ok;
+        const bool store = mine && ok && *(volatile int*)&sh.dead == 0;   // (who has given up goes on arriving: what comes of that is nobody's output)
         char* dst = static_cast<char*>(a.out) + ((long long)(t_row0 + (store ? r : 0)) * a.out_stride + t_head * HD + half * (HD / 2)) * 2;
 #pragma unroll 1
         for (int k = 0; k < HD / 2; k += 32) {
@@ -812,6 +826,7 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
   ops_wait();   // the kernels before it in the call may still run; this one is not done before they are
+  if (sh.dead) til_give_up(a, &sh.first);
 }
 
 typedef CUresult (*TilEncode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,

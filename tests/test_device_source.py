@@ -100,3 +100,16 @@ def test_a_unit_is_written_over_when_all_warps_have_read_it():
                                    "til_arrive(&sh.unit_full[i % TIL_UNITS])")]
     assert at == sorted(at)
     assert text.count("s_unit[") == 2         # nobody else reads or writes them
+
+
+def test_attention_that_gave_up_leaves_no_rows_that_look_like_results():
+    """A call without a workspace of the caller's has no status that could be read: what a wait that ran out leaves undone has to show in the
+    rows.  The first CTA that gives up fills all of them; none stores what a warp that gave up may have spoilt."""
+    text = re.sub(r"//[^\n]*", "", _text("ops_attn_tiles.cu"))
+    kernel = _body(text, "blink_attn_tiles_kernel")
+    end = kernel[kernel.rindex("__syncthreads();"):]
+    assert re.search(r"ops_wait\(\);\s+if \(sh\.dead\) til_give_up\(a, &sh\.first\);", end)
+    assert re.search(r"const bool store = mine && ok && \*\(volatile int\*\)&sh\.dead == 0;", kernel) and kernel.count("store &&") + kernel.count("(store)") == 2
+    assert "*(volatile int*)dead = 1" in text and text.count("BLINK_ETIMEDOUT") == 1     # the status is set by whoever fills the rows
+    fill = _body(text, "til_give_up")
+    assert "atomicExch(reinterpret_cast<int*>(a.ws), BLINK_ETIMEDOUT) == BLINK_OK" in fill and "0x7fff7fffu" in fill and "q.rows <= a.few" in fill
