@@ -156,13 +156,13 @@ __global__ void __launch_bounds__(NR_WARPS * 32) blink_norm_rope_kernel(const __
 }
 
 template <typename TI, typename TO>
-int norm_rope_launch(const NormRopeArgs& a, void* stream) {
+int norm_rope_launch(const NormRopeArgs& a, int sms, void* stream) {
   const int heads = a.pool.Hq + 2 * a.pool.Hkv;
   // Few rows: a warp per group of heads, so that a row is spread over as many SMs as it can be.  Many: several groups a warp, which share the
   // row's angles and have more on its way: 1.5 KB a lane's worth in 32 bits or of heads of 64, 3 KB of wide heads in 16 bits.  (16000 rows of the 8B
   // shape, us, with 2 | 3 | 4 | 6 groups: fp32 in 113 | 105 | 105 | 109, bf16 in 92 | 80 | 77 | 72; 4099 rows of the 1B shape in bf16 14.4 | 12.7 | 14.5 | 14.4.)
   const int group = a.pool.hd == 128 ? 4 : 8;
-  const bool few = (long long)a.rows * ((heads + group - 1) / group) <= 4 * 148 * 16;
+  const bool few = (long long)a.rows * ((heads + group - 1) / group) <= 4ll * sms * 16;
   constexpr int WIDE = sizeof(TI) == 2 ? 6 : 3;
   const int u = few ? 1 : a.pool.hd == 128 ? WIDE : 3;
   const long long tasks = (long long)a.rows * ((heads + group * u - 1) / (group * u));
@@ -204,7 +204,9 @@ extern "C" int blink_qk_norm_rope(const blink_model_cfg* model, const blink_kv_p
   for (int i = 0; i < a.pool.hd / 2; ++i) a.turns[i] = std::pow((double)model->rope_theta, -2.0 * i / a.pool.hd) / 6.283185307179586476925;
   for (int i = a.pool.hd / 2; i < 64; ++i) a.turns[i] = 0.0;
   if (rows == 0) return BLINK_OK;
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return BLINK_ECUDA;
   if (qkv_dtype == BLINK_DTYPE_FP32)
-    return model->dtype == BLINK_DTYPE_FP32 ? norm_rope_launch<float, float>(a, stream) : norm_rope_launch<float, __nv_bfloat16>(a, stream);
-  return norm_rope_launch<__nv_bfloat16, __nv_bfloat16>(a, stream);
+    return model->dtype == BLINK_DTYPE_FP32 ? norm_rope_launch<float, float>(a, sms, stream) : norm_rope_launch<float, __nv_bfloat16>(a, sms, stream);
+  return norm_rope_launch<__nv_bfloat16, __nv_bfloat16>(a, sms, stream);
 }

@@ -113,3 +113,9 @@ def test_attention_that_gave_up_leaves_no_rows_that_look_like_results():
     assert "*(volatile int*)dead = 1" in text and text.count("BLINK_ETIMEDOUT") == 1     # the status is set by whoever fills the rows
     fill = _body(text, "til_give_up")
     assert "atomicExch(reinterpret_cast<int*>(a.ws), BLINK_ETIMEDOUT) == BLINK_OK" in fill and "0x7fff7fffu" in fill and "q.rows <= a.few" in fill
+
+
+def test_operators_ask_the_device_for_its_sms():
+    for f in sorted(os.listdir(CSRC)):
+        if f.startswith("ops"):
+            assert not re.search(r"\b148\b", re.sub(r"//[^\n]*", "", _text(f))), f
