@@ -426,7 +426,8 @@ int blink_build_tables(const int32_t* ctx_len, const int32_t* new_len, const int
  * [hd]; NULL: not normed), then pairs (i, i + hd/2) are turned by position * rope_theta^(-2i/hd) (angles in 64 bits).  q
  * goes to q_out [rows][Hq * hd] (model dtype, q_stride), which may be qkv itself (same dtype and stride) but not overlap it
  * otherwise; k and v to the row's slot.  A row whose slot is not one of the pool's is not cached; a row with a negative
- * position is left alone.  Two rows of one slot: each head of it is of either.  Pointers 16-byte aligned, strides multiples of 8. */
+ * position is left alone.  Two rows of one slot: each head of it is of either.  Squares are summed in 32 bits, as everything but the angles: entries
+ * above 1e18, or without an epsilon below 1e-18, leave their range.  Pointers 16-byte aligned, strides multiples of 8. */
 int blink_qk_norm_rope(const blink_model_cfg* model, const blink_kv_pool* kv, int layer, const void* qkv, int qkv_dtype,
                        int64_t qkv_stride, const float* q_gain, const float* k_gain, const int32_t* positions,
                        const int32_t* slot_map, int rows, void* q_out, int64_t q_stride, void* stream);
