@@ -64,7 +64,9 @@ struct OpsShared {
 
 // cluster > 0: CTAs of a cluster.  Kernels are set up while the one before them in the stream still runs (1 to 2 us less a launch) and wait for
 // it themselves: the first kernel of a call in all of its threads before anything else (ops_begin), the later ones before they read what it
-// wrote, or at their end at the latest, so that a kernel that is done says that all before it are.
+// wrote, or at their end at the latest, so that a kernel that is done says that all before it are.  What the caller's earlier kernels wrote (lengths, tables,
+// queries, the cache) a later kernel reads before its own wait, on the strength of the first one's: it cannot begin before that wait is over.  The instruction's
+// description promises visibility behind a kernel's own wait only; that a kernel which begins later sees it too is an assumption about the device.
 template <typename... P, typename... A>
 inline int ops_launch(void (*kernel)(P...), int64_t grid, int threads, OpsShared smem, void* stream, int cluster, A... args) {
   if (grid < 1) return BLINK_OK;

@@ -7,8 +7,8 @@
 // (ops_attn_block.cu); which requests and calls take which stands at the entry point, with both sides measured.
 //
 // attn_few: requests of few rows (a token, a few drafts).  What bounds it: HBM, every visible key and value once.  (8B shape, a row each: 64 requests
-// behind 5000 keys 195 us, 6.7 TB/s; 256 752 us, 7.0; one behind 120000 keys 82 us, 6.0.)  With more rows, instructions: 48 requests of 4 rows behind
-// 2500 keys 92 us, 5.3 TB/s, of 8 rows 131.  (Tiles copied ahead into shared memory, which leaves registers to more rows, cost time at every number of rows:
+// behind 5000 keys 196 us, 6.7 TB/s; 256 754 us, 7.0; one behind 120000 keys 82 us, 6.0.)  With more rows, instructions: 48 requests of 4 rows behind
+// 2500 keys 92 us, 5.3 TB/s, of 8 rows 133.  (Tiles copied ahead into shared memory, which leaves registers to more rows, cost time at every number of rows:
 // 5 rows 103 us, 127 so; it is not the loads that a warp waits for.)
 // A unit is a request, a kv head and up to MR (query row, head) rows, its tiles are the visible blocks of 16 keys.  All tiles of all units
 // stand in one sequence that is cut into equal runs, one per CTA, whatever the lengths; lengths are read on the device, so that a
@@ -533,7 +533,7 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) blink_attn_few_kernel(const
 // The units that were cut: m = max m_i, l = sum l_i 2^(m_i - m), o = sum o_i 2^(m_i - m) / l over a row's parts.  The rows of a unit are dealt to the CTAs
 // whose runs it spans (as many as there are parts; up to JOIN_FEW, which many units have, one CTA has all of them, instead of two units one after the
 // other), a row's parts to warps, and these joined in order.  Latency: 2 to 3 us behind a batch.
-// (With a CTA per unit: three requests of 2 to 4 rows behind 2000 keys 26.5 us, 14.7 so; one row behind 30000 keys 33.5 and 28.  All dealt out: 64 rows behind 600 keys
+// (With a CTA per unit: three requests of 2 to 4 rows behind 2000 keys 26.5 us, 14.7 so (a cluster each takes 12); one row behind 30000 keys 33.5 and 28.  All dealt out: 64 rows behind 600 keys
 // 33.9, 31.4 so.)
 template <typename T, int HD, int MR>
 __global__ void __launch_bounds__(JOIN_THREADS) blink_attn_join_kernel(const __grid_constant__ AttnArgs a) {
@@ -794,11 +794,11 @@ int blink_window_attention(const blink_model_cfg* model, const blink_kv_pool* kv
   const int64_t keys = std::min<int64_t>((int64_t)table_stride * OPS_BLOCK, window > 0 ? (int64_t)window + sinks + std::min(max_new, 256) : INT64_MAX);
   // Everything to the tiles, which share nothing out over CTAs, where there are units enough and none can be very long: a tile's rows cost the same
   // however few they are, but its copies run by themselves.  (8B shape, us, with the kernels for few rows | without: 48 requests of 1 to 6 rows behind
-  // 300 to 5000 keys 116 | 86, of 1 to 3 91 | 86; 28 of them 77 | 60, 19 55 | 55, 10 34 | 46; 40 of 1 to 300 rows with a window of 256 51 | 41.  20 of 5
-  // rows behind 10000 keys 151 | 205.  Evenly long ones end later where they do not fill the CTAs: 48 of 4 rows behind 2500 keys 92 | 95.  Eight rows of a
-  // head or less, one instruction of those kernels: 64 rows behind 5000 keys 197 us, 6.7 TB/s, which the tiles do not reach.)  Where no row sees more
+  // 300 to 5000 keys 113 | 88, of 1 to 3 92 | 87; 28 of them (1 to 6 rows) 76 | 60, 19 57 | 55, 10 32 | 46; 40 of 1 to 300 rows with a window of 256 49 | 42.  20 of 5
+  // rows behind 10000 keys 150 | 202.  Evenly long ones end later where they do not fill the CTAs: 48 of 4 rows behind 2500 keys 92 | 96, of 8 133 | 96.  Eight rows of a
+  // head or less, one instruction of those kernels: 64 rows behind 5000 keys 196 | 225.)  Where no row sees more
   // than some 1500 keys fewer units will do, and none have to be there when the tiles are called anyway: 10 of 1 to 6 rows behind 200 to 900
-  // keys 23 | 17; with a window of 1024 8 rows beside a prompt of 64 27 | 19, beside two of 1000 50 | 43, whole prompts of three requests 177 | 174.
+  // keys 16.7 | 17.1; with a window of 1024 8 rows beside a prompt of 64 21 | 19, beside two of 1000 51 | 43, whole prompts of three requests 175 | 175.
   const int64_t least = keys > ALL_SHORT ? sms + sms / 2 : tiles ? 0 : sms / 2;
   if (bf16 && (int64_t)max_new * a.pool.rep > ALL_ROWS && (int64_t)n_requests * a.pool.Hkv >= least && keys <= ALL_KEYS) {
     a.few = 0;

@@ -9,10 +9,10 @@
 //
 //   warps 0-7 | 8-15  softmax of stream 0 | 1, two threads per row (64 keys of a tile each): scores from TMEM, probabilities back to TMEM
 //                     over the same scores
-//   warps 16 | 17     issue the MMAs of stream 0 | 1: scores = Q K^T (operands in shared memory), output += P V (P in TMEM, V as it lies in the
+//   warp 16           issues the MMAs of both streams: scores = Q K^T (operands in shared memory), output += P V (P in TMEM, V as it lies in the
 //                     cache)
-//   warps 18 | 19     copies of the keys | of the values, eight a tile (with twice as many smaller ones for the keys that warp was the slowest of
-//                     all: 4096 rows 170 us, 145 so).  Warp 18 also hands out the units, heaviest of a request first, from a counter
+//   warps 17 | 18     copies of the keys | of the values, eight a tile (with twice as many smaller ones for the keys that warp was the slowest of
+//                     all: 4096 rows 170 us, 145 so).  Warp 17 also hands out the units, heaviest of a request first, from a counter
 //
 // While one stream is in its softmax the tensor core works for the other; the next scores of a stream are issued behind its output MMAs, so a
 // stream's scores being complete also says that its accumulator is.  The maximum in use, the same for both threads of a row, follows the
@@ -21,14 +21,14 @@
 //
 // A unit with rows for one stream only is worked on by both, stream 0 the even tiles and stream 1 the odd ones, and joined in the epilogue:
 // stream 0 reads both accumulators, once stream 1 has said that its own is there, with its rows' maxima and sums (48 requests of 12
-// rows behind 2500 keys, 8B shape: 131 us with one stream, 98 so).
+// rows behind 2500 keys, 8B shape: 128 us with one stream, 97 so; 512 rows behind 3500 keys 70 and 45).
 //
-// What bounds it.  Prompts: the chain of a stream, softmax -> output -> next scores, of which two overlap: 8192 rows of the 8B shape 507 us, 1085
+// What bounds it.  Prompts: the chain of a stream, softmax -> output -> next scores, of which two overlap: 8192 rows of the 8B shape 504 us, 1090
 // TFLOP/s of the pairs that are seen, the tensor pipe busy half of the time.  With one thread per row (eight warps) the softmax alone took 1900 cycles a
 // tile, at four cycles an instruction with one warp of a stream on a scheduler.  Exponentials on the multiply-adds (a quarter to a half of
 // them, degree 3) made it longer, not shorter: they are not what it waits for.  Few rows: HBM (48 requests of 1 to 6 rows behind 300 to
-// 5000 keys 68 us, 4.8 TB/s, cold), and that units are whole.  Narrow windows: what a unit costs beside its tiles, some 4000 cycles (4096 rows with a
-// window of 128 40 us).
+// 5000 keys 88 us, 5.5 TB/s; those of 8 rows behind 2500 96 us, 5.1), and that units are whole.  Narrow windows: what a unit costs beside its tiles, some 4000
+// cycles (4096 rows with a window of 128 38 to 43 us from box to box).
 #include <cuda.h>
 
 #include <cmath>
@@ -211,7 +211,7 @@ __device__ __forceinline__ void til_mask(uint32_t (&r)[16], const TilMask& k, in
 }
 
 // Every tile is masked: two instructions a score, which nothing waits for; a second copy of the code for tiles that all rows see whole cost more
-// in calls of a few tiles, where its first instructions come from L2 (4096 rows with a window of 128: 43.9 us, 42.3 with one).
+// in calls of a few tiles, where its first instructions come from L2 (4096 rows with a window of 128: 4 % longer).
 // Half a row of a score tile (blocks block0 .. block0 + 3) -> 32 words of probabilities (bf16 pairs), their sum, and the largest score.
 __device__ __forceinline__ void til_probs(uint32_t t_s, float qscale, float neg, const TilMask& mask, int block0, uint32_t (&p)[32], float& mx, float& sum) {
   const float2 scale2 = make_float2(qscale, qscale), neg2 = make_float2(neg, neg);
@@ -338,11 +338,11 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   // The sequence of units: requests of more keys first, so that no CTA is left with a long unit at the end (48 requests of 300 to 5000 keys: in their
-// own order 99 us, so 86); beyond TIL_SORTED requests units are many and their order matters less.  A run of requests (or places) per thread.
+// own order 99 us, so 88); beyond TIL_SORTED requests units are many and their order matters less.  A run of requests (or places) per thread.
   const bool sorted = a.n <= TIL_SORTED;
   // Rows of a unit: two streams' worth, or one's, which both share, where there are few: twice the CTAs at half the time.  (8B shape, us, two | one: 512
-  // rows behind 3500 keys 76 | 45, 40 behind 1000 28 | 19.  Between one and two units a CTA: 1024 rows 27 | 23, two of 512 behind 3500 80 | 81.  Between
-  // two and three: 1500 rows 35.6 | 37.3.)
+  // rows behind 3500 keys 77 | 45, 40 behind 1000 28 | 19.  Between one and two units a CTA: 1024 rows 27.6 | 23.5, two of 512 behind 3500 79 | 79.  Between
+  // two and three: 1500 rows 36.3 | 38.2.)
   int unit_shift = 8 - lr;   // (powers of two)
   {
     const int each = (a.n + TIL_THREADS - 1) / TIL_THREADS;

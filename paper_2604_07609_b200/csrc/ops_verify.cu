@@ -11,10 +11,12 @@
 //           64: the acceptance test is off by some 1e-8 where the entries differ, and by 1e-6 at worst (most of the weight on entries that are
 //           all alike, 12 below the largest: an argument's rounding of 2^-24 of itself, and the exponential's own 2^-22).
 //   choose  a CTA per request: the first refused draft, from the pieces (with few requests every CTA of the draw does so for itself)
-//   draw    a cluster of 16 CTAs per request: the exponentials of that row, which stay in registers (up to 16 a thread), their sum, then the weights
+//   draw    a cluster of 16 CTAs per request: the exponentials of that row, which stay in registers (up to 16 a thread; beyond 131072 entries they are
+//           made again from tile to tile), their sum, then the weights
 //           max(0, p - q), their sum, and the entry at which the running sum passes its target.  Sums go from CTA to CTA through
-//           distributed shared memory.  What bounds it: instructions, some 70 an entry, and the chain load, sum, exchange, sum, exchange, search of
-//           each of the waves that many requests take: 57 rows of 128256 42 us in four waves, one of 32000 5.
+//           distributed shared memory.  What bounds it: latency, the chain load, sum, exchange, sum, exchange, search of each of the waves that many
+//           requests take, with some 70 instructions an entry (issue slots 47 % busy, the 64-bit pipe 21 %, 40 % of the warps resident): 57 rows of 128256
+//           42 us in four waves, one of 32000 5.
 // The chosen row's sums decide between neighbours that are as close as 1e-6, so its exponentials, sums and running sum are in 64 bits.  Sums are
 // taken in an order that sizes alone fix: the same call gives the same token.
 #include <cooperative_groups.h>
