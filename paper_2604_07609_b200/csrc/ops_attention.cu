@@ -397,7 +397,7 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) blink_attn_few_kernel(const
   int2* s_len = reinterpret_cast<int2*>(s_pre + a.n + 1);                                // [n] first row, kv_len
   __shared__ long long s_warp[FEW_WARPS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (a.first) ops_wait();
+  ops_wait();
   if (blockIdx.x == 0 && tid == 0) {
     reinterpret_cast<int*>(a.ws)[0] = 0;
     reinterpret_cast<int*>(a.ws)[1] = 0;   // units that the tiles' CTAs have taken from the counter
@@ -527,7 +527,6 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) blink_attn_few_kernel(const
     cuts[0] = begins;
     cuts[1] = ends;
   }
-  ops_wait();   // (a kernel before it in the call may still run)
 }
 
 // The units that were cut: m = max m_i, l = sum l_i 2^(m_i - m), o = sum o_i 2^(m_i - m) / l over a row's parts.  The rows of a unit are dealt to the CTAs
@@ -625,7 +624,7 @@ __global__ void __launch_bounds__(FEW_THREADS) blink_attn_near_kernel(const __gr
   cg::cluster_group cluster = cg::this_cluster();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
-  if (a.first) ops_wait();
+  ops_wait();
   if (blockIdx.x == 0 && tid == 0) {
     reinterpret_cast<int*>(a.ws)[0] = 0;
     reinterpret_cast<int*>(a.ws)[1] = 0;   // units that the tiles' CTAs have taken from the counter
@@ -634,10 +633,7 @@ __global__ void __launch_bounds__(FEW_THREADS) blink_attn_near_kernel(const __gr
   ops_next();
   const int unit = (int)blockIdx.x / ctas, h = unit % a.pool.Hkv, r = unit / a.pool.Hkv / groups, g0 = unit / a.pool.Hkv % groups;
   const AttnReq req = attn_req(a, a.row_start[r], a.row_start[r + 1], a.kv_len[r]);
-  if (req.rows == 0 || req.rows > a.few) {   // (the whole cluster)
-    ops_wait();
-    return;
-  }
+  if (req.rows == 0 || req.rows > a.few) return;   // (the whole cluster)
   const int32_t* table = a.table + (long long)r * a.stride;
   W w;
   for (int m0 = g0 * MR; m0 < req.rows * a.pool.rep; m0 += groups * MR) {
@@ -707,7 +703,6 @@ __global__ void __launch_bounds__(FEW_THREADS) blink_attn_near_kernel(const __gr
     }
     cluster.sync();   // (the records have been read)
   }
-  ops_wait();   // (a kernel before it in the call may still run)
 }
 
 template <typename T, int HD, typename W, int CTAS>
@@ -807,7 +802,6 @@ int blink_window_attention(const blink_model_cfg* model, const blink_kv_pool* kv
   const int64_t mr = few_rows_of(model, max_new), rows_few = std::min<int64_t>(max_new, a.few);
   const int64_t groups = (rows_few * a.pool.rep + mr - 1) / mr, units = (int64_t)n_requests * a.pool.Hkv * groups;
   a.near_ctas = 0;
-  a.first = bf16 || !tiles;
   // A cluster for each unit, of as many CTAs as its keys are worth and there is room for; the sequence of tiles where units are many or long.  (One row of the 8B
   // shape, us, clusters of 1 | 4 | 8 | 16: behind 15 keys 4.8 | 5.4 | 5.9 | 6.9, 250 7.4 | 6.0 | 6.4 | 7.7, 1000 15.0 | 8.0 | 7.1 | 7.7, 2000 25 | 10.5 | 8.5 | 8.8; 32 bits, 500
   // 22 | 10.1 | 8.6 | 10.4, 1000 39 | 14.3 | 10.9 | 10.5.  The sequence | so: 1 x 4000 18.4 | 10.9, 16000 25.9 | 24.3, 30000 33.9 | 39.9; heads of 64, 8000

@@ -17,7 +17,6 @@ struct AttnArgs {
   int few;                          // requests of up to so many rows go to attn_few, longer ones to the tiles
   float qscale;                     // 1 / sqrt(hd) * log2(e)
   int near_ctas, near_groups;       // > 0: a cluster of so many CTAs per unit; clusters per (request, kv head)
-  bool first;                       // attn_few is the call's first kernel
   bool out_32;                      // rows of out begin on 32-byte boundaries
   char* ws;
 };

@@ -337,6 +337,7 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(til_smem(&sh.tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  ops_wait();
   // The sequence of units: requests of more keys first, so that no CTA is left with a long unit at the end (48 requests of 300 to 5000 keys: in their
 // own order 99 us, so 88); beyond TIL_SORTED requests units are many and their order matters less.  A run of requests (or places) per thread.
   const bool sorted = a.n <= TIL_SORTED;
@@ -768,7 +769,6 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
           if (use > 0) wait(empty, (use - 1u) & 1u);
           if (!ok) break;
           if (part == 0 && j == max(0, tiles - 2)) {   // the next unit, late, so that the CTAs end together; the counter was zeroed by a kernel before this one
-            if (u == 0) ops_wait();
             int next = 0;
             if (lane == 0) next = (int)gridDim.x + atomicAdd(status + 1, 1);
             hand_out(u + 1, __shfl_sync(0xffffffffu, next, 0));
@@ -825,7 +825,6 @@ __global__ void __launch_bounds__(TIL_THREADS, 1) blink_attn_tiles_kernel(const 
     til_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
-  ops_wait();   // the kernels before it in the call may still run; this one is not done before they are
   if (sh.dead) til_give_up(a, &sh.first);
 }
 

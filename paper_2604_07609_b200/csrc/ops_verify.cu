@@ -4,7 +4,7 @@
 //   first refused i: a token from max(0, p_i - q_i), none refused: from p of the last row; by the inverse of its running sum in the order of
 //   the indexes: the first j with sum_{<= j} > v * sum
 //
-// Three kernels (or two), each waiting for the one before it only where it needs its results.
+// Three kernels (or two).
 //   rows    largest value and sum of exponentials of pieces of 1024 entries of every row, a warp each: one pass over the logits
 //           (HBM, 4 bytes an entry: 215 rows of 128256 23 us, cold, 4.8 TB/s).  A lane has its 32 entries on their way at once and sums against its own largest
 //           value, so that nothing waits for another warp.  Exponentials in 32 bits, sums of a lane's entries in 32, everything above in
@@ -237,14 +237,14 @@ struct VerPicked {
 template <int WARPS>
 __device__ __forceinline__ VerPicked ver_choose(const VerifyArgs& a, int req, const double* s_table, VerPicked* s_out) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  // (all but the pieces is there before the first kernel is done)
+  ops_wait();
   const int2 rows = ver_rows(a, req);
   const int start = rows.x, k = rows.y - rows.x - 1;
   const float T = a.temperature[req];
   if (tid == 0) s_out->accepted = max(k, 0);
   __syncthreads();
-  // A row from its pieces: largest value, its index, sum.
-  auto row_of = [&](int row, float& m, int& idx, double& sum, bool with_sum) {
+  // A row from its pieces: largest value and its index (and whether the row stands for that entry alone); then its sum.
+  auto top_of = [&](int row, float& m, int& idx) {
     const VerChunk* c = a.chunks_of + (size_t)row * a.chunks;
     m = -INFINITY;
     idx = 0x7fffffff;
@@ -256,40 +256,36 @@ __device__ __forceinline__ VerPicked ver_choose(const VerifyArgs& a, int req, co
       const int i2 = __shfl_xor_sync(0xffffffffu, idx, d);
       ver_larger(m, idx, m2, i2);
     }
-    const bool one = ver_one(T, m);
-    sum = 0.0;
-    if (!one && with_sum) {
-      const VerExp x = ver_exp_of(a, s_table, m, T);
-#pragma unroll 4
-      for (int j = lane; j < a.chunks; j += 32) sum += c[j].sum * ver_exp(x, c[j].max);
-#pragma unroll
-      for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    }
-    return one;
+    return ver_one(T, m);
   };
-  bool waited = false;
-  for (int i = warp; i < k; i += WARPS) {
+  auto sum_of = [&](int row, float m) {
+    const VerChunk* c = a.chunks_of + (size_t)row * a.chunks;
+    const VerExp x = ver_exp_of(a, s_table, m, T);
+    double sum = 0.0;
+#pragma unroll 4
+    for (int j = lane; j < a.chunks; j += 32) sum += c[j].sum * ver_exp(x, c[j].max);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    return sum;
+  };
+  for (int i = warp; i < k; i += WARPS) {   // (loads that wait for one another: those of the draft are on their way beside those of the pieces)
     float m;
     int idx;
-    double sum;
     const int row = start + i, x = a.draft[row];
+    const float u = a.u_accept[row];
+    const bool one = top_of(row, m, idx);
     const bool in = x >= 0 && x < a.vocab;
     const float z = in ? ver_entry(__ldcg(a.logits + row * a.logits_stride + x)) : -INFINITY, q = in && a.probs ? a.probs[row * a.probs_stride + x] : 1.f;
-    const float u = a.u_accept[row];
-    if (!waited) ops_wait();
-    waited = true;
-    const bool one = row_of(row, m, idx, sum, true);
+    const double sum = one ? 0.0 : sum_of(row, m);
     const bool ok = one ? x == idx : in && (double)u * (double)q * sum < ver_exp(ver_exp_of(a, s_table, m, T), z);
     if (lane == 0 && !ok) atomicMin(&s_out->accepted, i);
   }
-  if (!waited) ops_wait();
   __syncthreads();
   if (warp == 0) {
     const int acc = s_out->accepted, row = start + acc;
     float top = 0.f;
     int index = -1;
-    double unused;
-    const bool one = k < 0 || row_of(row, top, index, unused, false);
+    const bool one = k < 0 || top_of(row, top, index);
     if (lane == 0) {
       s_out->start = start;
       s_out->k = k;
@@ -350,7 +346,6 @@ __global__ void __launch_bounds__(PICK_THREADS, 2) blink_verify_draw_kernel(cons
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = (int)cluster.block_rank(), req = (int)(blockIdx.x / PICK_CTAS);
   const int V = a.vocab;
-  const float T = a.temperature[req], u = a.u_pick[req];
   ver_table(s_table, a);
   __shared__ VerPicked s_out;
   VerPicked picked;
@@ -365,6 +360,7 @@ __global__ void __launch_bounds__(PICK_THREADS, 2) blink_verify_draw_kernel(cons
     ops_next();
     choice = a.choice[req];
   }
+  const float T = a.temperature[req], u = a.u_pick[req];
   const int row = choice.row;
   if (!CHOOSE && row < 0) return;   // (the whole cluster)
   cg::cluster_group::arrival_token there = cluster.barrier_arrive();   // all CTAs have to be there before they are written to

@@ -108,7 +108,7 @@ def test_attention_that_gave_up_leaves_no_rows_that_look_like_results():
     text = re.sub(r"//[^\n]*", "", _text("ops_attn_tiles.cu"))
     kernel = _body(text, "blink_attn_tiles_kernel")
     end = kernel[kernel.rindex("__syncthreads();"):]
-    assert re.search(r"ops_wait\(\);\s+if \(sh\.dead\) til_give_up\(a, &sh\.first\);", end)
+    assert re.search(r"if \(sh\.dead\) til_give_up\(a, &sh\.first\);", end)
     assert re.search(r"const bool store = mine && ok && \*\(volatile int\*\)&sh\.dead == 0;", kernel) and kernel.count("store &&") + kernel.count("(store)") == 2
     assert "*(volatile int*)dead = 1" in text and text.count("BLINK_ETIMEDOUT") == 1     # the status is set by whoever fills the rows
     fill = _body(text, "til_give_up")
@@ -119,3 +119,22 @@ def test_operators_ask_the_device_for_its_sms():
     for f in sorted(os.listdir(CSRC)):
         if f.startswith("ops"):
             assert not re.search(r"\b148\b", re.sub(r"//[^\n]*", "", _text(f))), f
+
+
+def test_operators_kernels_touch_nothing_before_their_own_wait():
+    """A kernel may begin while those before it in the stream still run: what they wrote (the caller's lengths and queries, or an earlier kernel of
+    the call) is sure to be seen behind its own griddepcontrol.wait only."""
+    memory = re.compile(r"\ba\.(row_start|kv_len|table|temperature|u_pick|u_accept|draft|choice|chunks_of|logits|positions|slot_map|qkv|ctx_len|new_len|held|"
+                        r"free_count|free_blocks|block_table|ws|q|out|pool)\b|\battn_req\(|\bws\[")
+    found = 0
+    for f in sorted(os.listdir(CSRC)):
+        if not (f.startswith("ops_") and f.endswith(".cu")):
+            continue
+        text = re.sub(r"//[^\n]*", "", _text(f)).replace("int* status = reinterpret_cast<int*>(a.ws);", "")   # (its address)
+        for name in re.findall(r"__global__ void (?:__launch_bounds__\([^)]*\) )?(\w+)\(", text) + (["ver_choose"] if f == "ops_verify.cu" else []):
+            body = _body(text, name)
+            waits = [m.start() for m in re.finditer(r"\bops_wait\(\);|\bops_begin\(\);|\bver_choose<", body)]
+            touched = memory.search(re.sub(r"a\.pool\.(rep|hd|Hq|Hkv|n_blocks|dtype)\b", "shape", body[:waits[0]]))
+            assert touched is None, (f, name, touched.group(0))
+            found += 1
+    assert found >= 11
