@@ -15,7 +15,7 @@
 //           made again from tile to tile), their sum, then the weights
 //           max(0, p - q), their sum, and the entry at which the running sum passes its target.  Sums go from CTA to CTA through
 //           distributed shared memory.  What bounds it: latency, the chain load, sum, exchange, sum, exchange, search of each of the waves that many
-//           requests take, with some 70 instructions an entry (issue slots 47 % busy, the 64-bit pipe 21 %, 40 % of the warps resident): 57 rows of 128256
+//           requests take, with some 70 instructions an entry (issue slots 45 % busy, the 64-bit pipe 21 %, 40 % of the warps resident): 57 rows of 128256
 //           42 us in four waves, one of 32000 5.
 // The chosen row's sums decide between neighbours that are as close as 1e-6, so its exponentials, sums and running sum are in 64 bits.  Sums are
 // taken in an order that sizes alone fix: the same call gives the same token.
