@@ -29,7 +29,12 @@ def sources():
 
 def marshal_for() -> str:
     """What _marshal.so is built for: this torch and this Python.  It says so in itself."""
-    return f"torch {importlib.metadata.version('torch')}, {sysconfig.get_config_var('SOABI')}"
+    try:
+        version = importlib.metadata.version("torch")
+    except importlib.metadata.PackageNotFoundError:   # (one that was not installed as a package)
+        import torch
+        version = torch.__version__
+    return f"torch {version}, {sysconfig.get_config_var('SOABI')}"
 
 
 def build_marshal(force: bool = False) -> str:

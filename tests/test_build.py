@@ -47,3 +47,12 @@ def test_a_marshaller_for_another_torch_is_not_used(monkeypatch):
     monkeypatch.setattr(build, "marshal_for", lambda: "torch 0.0, another")
     with pytest.raises(RuntimeError, match="torch 0.0, another"):
         B._marshal()
+
+
+def test_a_torch_that_is_no_installed_package_has_a_version_too(monkeypatch):
+    import torch
+
+    def none(name):
+        raise build.importlib.metadata.PackageNotFoundError(name)
+    monkeypatch.setattr(build.importlib.metadata, "version", none)
+    assert build.marshal_for().startswith(f"torch {torch.__version__}, ")
